@@ -59,10 +59,14 @@ typedef enum {
   MALA_OK = 0,
   MALA_ERR_INVALID_ARG = -1, /* null required pointer, non-positive size, Hq % Hkv != 0,
                                 Nq > Nk, tau < 0 or NaN, scale not finite or <= 0,
-                                num_splits < 1, an output type not MALA_OUT_* */
+                                num_splits < 1, an output type not MALA_OUT_*; paged cache:
+                                misaligned rows, a stride below D, split_tokens not a
+                                positive multiple of B_k, outputs that are inputs */
   MALA_ERR_UNSUPPORTED = -2, /* head_dim not in {64, 128}, causal == 0 (the paper's
-                                traversal is defined for causal attention only), or a
-                                forward/backward K/V slice of 2^32 bytes or more */
+                                traversal is defined for causal attention only), a
+                                forward/backward K/V slice of 2^32 bytes or more, a page
+                                size that is not a multiple of 16, or a pool, table or
+                                grid of 2^31 tokens, entries or workgroups or more */
   MALA_ERR_WORKSPACE = -3,   /* workspace NULL or smaller than the *_workspace_size query */
   MALA_ERR_HIP = -4          /* a HIP launch/runtime call failed; see mala_last_error() */
 } mala_status;
@@ -296,6 +300,135 @@ int mala_decode_noalloc(const void* q, const void* k_cache, const void* v_cache,
                         const int32_t* cache_lens, void* o, float* lse, int32_t* head_tiles,
                         int64_t* counters, int num_splits, int B, int Hq, int Hkv, int Nk, int D,
                         float scale, float tau, int out_dtype, void* stream);
+
+/*
+ * Paged KV cache.
+ *
+ * K and V rows of every sequence live in pages of page_size tokens of one pool, so that
+ * sequences of different and growing lengths share it.  Position i of sequence b is row
+ * i % page_size of page block_table[b][i / page_size]; its slot is block_table[b][i /
+ * page_size] * page_size + i % page_size.  The functions that belong together:
+ *   mala_paged_update  page tables, slots and positions of a step from the lengths
+ *   mala_paged_write   new K / V rows into their slots
+ *   mala_paged_read    cached rows of a packed batch, for mala_fwd_varlen (prefill against
+ *                      cached keys)
+ *   mala_paged_decode  mala_decode over the pages
+ */
+
+/* Element type of a cache: bf16, or OCP e4m3 (4 exponent, 3 mantissa bits, no infinities)
+ * with one fp32 scale per KV head, an element standing for e4m3 value x scale. */
+enum { MALA_CACHE_BF16 = 0, MALA_CACHE_E4M3 = 1 };
+
+/* The pool: row r of page i, KV head h starts at element i * page_stride + h * head_stride +
+ * r * token_stride of k_pages and of v_pages (both the same strides; the D elements of a row
+ * are contiguous), e.g. [num_pages, Hkv, page_size, D] or [num_pages, page_size, Hkv, D]
+ * tensors, or K and V halves of one tensor.  Pointers are 16-byte aligned, strides multiples
+ * of 16 bytes, at least D elements, and 16 rows (16 x token_stride) take less than 2^31 bytes.
+ * page_size is a multiple of 16, D 64 or 128, num_pages x page_size below 2^31.
+ * k_scale, v_scale: fp32 [Hkv] device arrays of an e4m3 cache, NULL for scales of 1 (and for
+ * bf16).  The struct itself is host memory, read during the call. */
+typedef struct {
+  void* k_pages;
+  void* v_pages;
+  const float* k_scale;
+  const float* v_scale;
+  int64_t page_stride;
+  int64_t head_stride;
+  int64_t token_stride;
+  int32_t num_pages;
+  int32_t page_size;
+  int32_t Hkv;
+  int32_t D;
+  int32_t dtype; /* MALA_CACHE_* */
+} mala_paged_cache_t;
+
+/*
+ * Page tables of one serving step, built on the GPU.  Request r held lens[r] tokens and holds
+ * new_lens[r] after the step: it grows (a prompt or its next chunk: +n, a decode: +1) and
+ * takes pages, or shrinks (finished: 0, rejected tokens) and gives pages back, or stays.
+ *   lens, new_lens: int32 [num_seqs], clamped into [0, max_pages * page_size]
+ *   block_table: int32 [num_seqs, max_pages] in / out: entries of the pages a request takes
+ *       are written, all others stay (entries past a request's pages mean nothing)
+ *   free_ring: int32 [ring_size] in / out, free_state: int32 [2] = {head, count}: the free
+ *       pages are free_ring[(head + i) % ring_size], i < count (clamped into the ring).
+ *       Pages are taken from the head in the order of requests and positions; pages given
+ *       back go behind the last free one in the same order and can be taken from the next
+ *       call on.  A ring of num_pages entries holds them all.
+ *   A request whose pages do not fit the free ones any more, in the order of requests, is
+ *   refused: it takes none, keeps its length, and its tokens get slot -1.  (Requests that
+ *   need no page are never refused.)  No page belongs to two requests.
+ *   lens_out: int32 [num_seqs] out: new_lens, or lens of a refused request (the cache_lens of
+ *       mala_paged_decode)
+ *   cu_seqlens: int32 [num_seqs + 1] out: starts of the requests' new tokens (max(0, new_lens
+ *       - lens) of them each, refused ones too), packed back to back
+ *   slots: int32 [max_tokens] out: slot of every new token (-1: no page, or a page number
+ *       outside [0, num_pages)); -1 behind the last one
+ *   positions: int32 [max_tokens] or NULL out: its position in its sequence; 0 behind the last
+ *   free_state_out: int32 [4] out: {head, count, refused requests, new tokens}
+ *   No output may share memory with an input (block_table and free_ring are both); tokens
+ *   past max_tokens get pages but no slot.  page_size is a multiple of 16, num_seqs x
+ *   max_pages x page_size and num_pages x page_size are below 2^31, max_tokens may be 0.
+ */
+int mala_paged_update(const int32_t* lens, const int32_t* new_lens, int32_t* block_table,
+                      int32_t* free_ring, const int32_t* free_state, int32_t* lens_out,
+                      int32_t* cu_seqlens, int32_t* slots, int32_t* positions,
+                      int32_t* free_state_out, int num_seqs, int max_pages, int page_size,
+                      int num_pages, int ring_size, int max_tokens, void* stream);
+
+/*
+ * New K and V rows into the cache: token t, head h of k_new and v_new (bf16, row of D elements
+ * at element t * new_token_stride + h * new_head_stride, 16-byte aligned rows) to slot
+ * slots[t].  A slot outside [0, num_pages * page_size) is skipped (padding).  Slots are
+ * distinct: of tokens with the same slot, any one's bytes stay, 16 at a time.
+ *   e4m3: value / scale in fp32, rounded to nearest even, values beyond +-448 to +-448; NaN
+ *   stays NaN.  num_tokens may be 0.
+ */
+int mala_paged_write(const void* k_new, const void* v_new, int64_t new_token_stride,
+                     int64_t new_head_stride, const int32_t* slots,
+                     const mala_paged_cache_t* cache, int num_tokens, void* stream);
+
+/*
+ * Cached rows of a packed batch, contiguous: k, v: bf16 [Hkv, total, D] out, the layout of
+ * mala_fwd_varlen; sequence b's first cu_seqlens[b + 1] - cu_seqlens[b] cached rows at rows
+ * cu_seqlens[b] .. (int32 [num_seqs + 1], non-decreasing, inside [0, total]; a run longer than
+ * max_seqlen is cut to its first max_seqlen rows).  Rows that no sequence covers are not
+ * written.  Rows of a page whose table entry is outside [0, num_pages) are zeros.  e4m3: value
+ * x scale, rounded once.
+ *   block_table: int32 [num_seqs, max_pages]; max_seqlen <= max_pages * page_size.
+ *   total * D * 2 < 2^32, as for mala_fwd_varlen.
+ */
+int mala_paged_read(const mala_paged_cache_t* cache, const int32_t* block_table,
+                    const int32_t* cu_seqlens, void* k, void* v, int num_seqs, int max_pages,
+                    int max_seqlen, int total, void* stream);
+
+/* Bytes of device workspace mala_paged_decode needs at most (0 for invalid sizes). */
+size_t mala_paged_decode_workspace_size(int B, int Hq, int Hkv, int D, int max_len,
+                                        int split_tokens);
+
+/*
+ * mala_decode over a paged cache.
+ *   q: bf16 [B, Hq, D]; block_table: int32 [B, max_pages]; cache_lens: int32 [B]: sequence b
+ *       holds n_b valid tokens, its own included (clamped into [0, max_len]); L = n_b
+ *   max_len: the longest cache (the launch is sized by it), at most max_pages * page_size
+ *   Keys of a page whose table entry is outside [0, num_pages) are masked: pages may be
+ *       missing (a window that has moved on), and a sequence without keys gets o = 0, lse =
+ *       -inf.  A tile of B_k keys of which none is left is not retained.
+ *   split_tokens: a multiple of B_k; the rule of mala_decode runs over every split of
+ *       split_tokens keys (the last one shorter) from an empty normalizer, so the retained
+ *       set depends on it, but not on the batch, and not on how long the cache grows behind a
+ *       split.  At tau = 0 everything is retained whatever it is, and the library cuts the
+ *       cache as it likes.
+ *   o: [B, Hq, D] out (out_dtype; 16-byte aligned, as q); lse: fp32 [B, Hq] out; head_tiles:
+ *       int32 [B, Hq] or NULL out; counters: int64 [MALA_NUM_COUNTERS] or NULL out (every
+ *       V tile with a key is fetched).
+ *   workspace: at least mala_paged_decode_workspace_size(...) bytes, 16-byte aligned; what it
+ *       holds on entry does not matter.  (NULL where that size is 0.)
+ */
+int mala_paged_decode(const void* q, const mala_paged_cache_t* cache, const int32_t* block_table,
+                      const int32_t* cache_lens, void* o, float* lse, int32_t* head_tiles,
+                      int64_t* counters, int split_tokens, void* workspace,
+                      size_t workspace_bytes, int B, int Hq, int max_pages, int max_len,
+                      float scale, float tau, int out_dtype, void* stream);
 
 #ifdef __cplusplus
 }

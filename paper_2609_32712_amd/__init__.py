@@ -7,12 +7,14 @@ GPU is present, the calls raise.
 
 Low-level functions carry the C names and arguments (mala_fwd, mala_bwd,
 mala_fwd_varlen, mala_bwd_varlen, mala_decode, mala_decode_noalloc, mala_geometry,
-mala_bwd_workspace_size, mala_bwd_varlen_workspace_size, mala_decode_workspace_size);
-fwd / bwd / fwd_varlen /
-bwd_varlen / decode allocate their outputs and return them in a dict.
+mala_bwd_workspace_size, mala_bwd_varlen_workspace_size, mala_decode_workspace_size, and for
+a paged KV cache mala_paged_update, mala_paged_write, mala_paged_read, mala_paged_decode,
+mala_paged_decode_workspace_size); fwd / bwd / fwd_varlen / bwd_varlen / decode and
+paged_update / paged_read / paged_decode allocate their outputs and return them in a dict.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import os
 
@@ -32,7 +34,9 @@ NUM_COUNTERS = 8
 EXPORTS = ("mala_geometry", "mala_strerror", "mala_last_error", "mala_fwd",
            "mala_bwd_workspace_size", "mala_bwd", "mala_fwd_varlen", "mala_bwd_varlen",
            "mala_decode_workspace_size", "mala_decode", "mala_decode_noalloc",
-           "mala_bwd_varlen_workspace_size")
+           "mala_bwd_varlen_workspace_size", "mala_paged_update", "mala_paged_write",
+           "mala_paged_read", "mala_paged_decode_workspace_size", "mala_paged_decode")
+CACHE_BF16, CACHE_E4M3 = 0, 1
 DECODE_SCRATCH_BYTES = 16 << 20   # MALA_DECODE_SCRATCH_BYTES
 
 
@@ -44,6 +48,15 @@ class MalaError(RuntimeError):
 
 class _Geometry(ctypes.Structure):
     _fields_ = [("block_q", ctypes.c_int32), ("block_k", ctypes.c_int32)]
+
+
+class _PagedCacheStruct(ctypes.Structure):
+    _fields_ = [("k_pages", ctypes.c_void_p), ("v_pages", ctypes.c_void_p),
+                ("k_scale", ctypes.c_void_p), ("v_scale", ctypes.c_void_p),
+                ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
+                ("token_stride", ctypes.c_int64), ("num_pages", ctypes.c_int32),
+                ("page_size", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32),
+                ("dtype", ctypes.c_int32)]
 
 
 _lib = None
@@ -83,6 +96,17 @@ def load_library():
     lib.mala_decode.restype = i
     lib.mala_decode_noalloc.argtypes = [vp] * 8 + [i] * 6 + [f, f, i, vp]
     lib.mala_decode_noalloc.restype = i
+    cache, i64 = ctypes.POINTER(_PagedCacheStruct), ctypes.c_int64
+    lib.mala_paged_update.argtypes = [vp] * 10 + [i] * 6 + [vp]
+    lib.mala_paged_update.restype = i
+    lib.mala_paged_write.argtypes = [vp, vp, i64, i64, vp, cache, i, vp]
+    lib.mala_paged_write.restype = i
+    lib.mala_paged_read.argtypes = [cache] + [vp] * 4 + [i] * 4 + [vp]
+    lib.mala_paged_read.restype = i
+    lib.mala_paged_decode_workspace_size.argtypes = [i] * 6
+    lib.mala_paged_decode_workspace_size.restype = sz
+    lib.mala_paged_decode.argtypes = [vp, cache] + [vp] * 6 + [i, vp, sz] + [i] * 4 + [f, f, i, vp]
+    lib.mala_paged_decode.restype = i
     _lib = lib
     return lib
 
@@ -342,6 +366,159 @@ def mala_bwd_varlen(q, k, v, cu_seqlens, max_seqlen, o, lse, dout, dq, dk, dv, r
                                           _out_code(dq, dk, dv), _stream(stream)))
 
 
+# ---------------------------------------------------------------- paged KV cache
+class PagedCache:
+    """The pages of a KV cache: k_pages and v_pages [num_pages, Hkv, page_size, D], bf16 or
+    float8_e4m3fn, with the same strides, rows of D contiguous (views of other orders will
+    do, e.g. of [num_pages, page_size, Hkv, D], or of K and V in one tensor).  k_scale and
+    v_scale: fp32 [Hkv] of an e4m3 cache (an element stands for its value x scale; None: 1).
+
+    Kept by the caller for as long as the cache lives; it holds the tensors, and the calls
+    below take it.  page_size is a multiple of 16, D 64 or 128."""
+
+    def __init__(self, k_pages, v_pages, k_scale=None, v_scale=None):
+        N, Hkv, P, D = _dims(k_pages, "k_pages", 4)
+        if k_pages.dtype not in _CACHE:
+            raise TypeError("k_pages must have dtype %s, got %s" % (tuple(_CACHE), k_pages.dtype))
+        if not isinstance(v_pages, torch.Tensor) or v_pages.dtype != k_pages.dtype:
+            raise TypeError("v_pages must have the dtype of k_pages")
+        if v_pages.shape != k_pages.shape or v_pages.stride() != k_pages.stride():
+            raise ValueError("v_pages must have the shape and strides of k_pages")
+        if D > 1 and k_pages.stride(3) != 1:
+            raise ValueError("the rows of k_pages must be contiguous")
+        _spec(k_scale, "k_scale", torch.float32, (Hkv,), optional=True)
+        _spec(v_scale, "v_scale", torch.float32, (Hkv,), optional=True)
+        _on_device((("k_pages", k_pages), ("v_pages", v_pages), ("k_scale", k_scale),
+                    ("v_scale", v_scale)))
+        self.k_pages, self.v_pages, self.k_scale, self.v_scale = k_pages, v_pages, k_scale, v_scale
+        self.num_pages, self.Hkv, self.page_size, self.D = N, Hkv, P, D
+        self.device = k_pages.device
+        # (the stride of an axis of one entry is never used)
+        st = [k_pages.stride(i) if k_pages.shape[i] > 1 else max(D, 16) for i in range(3)]
+        self._struct = _PagedCacheStruct(
+            k_pages.data_ptr(), v_pages.data_ptr(), _addr(k_scale), _addr(v_scale), st[0], st[1],
+            st[2], N, P, Hkv, D, _CACHE[k_pages.dtype])
+        self._ref = ctypes.byref(self._struct)
+
+
+_CACHE = {torch.bfloat16: CACHE_BF16, torch.float8_e4m3fn: CACHE_E4M3}
+
+
+def _addr(t):
+    return None if t is None else t.data_ptr()
+
+
+def _cache(cache):
+    if not isinstance(cache, PagedCache):
+        raise TypeError("cache must be a PagedCache")
+    return cache
+
+
+def _launch(device, stream, call, *args):
+    """call(*args, stream) with the tensors' device current, on the given stream or on that
+    device's current one."""
+    if stream is None:
+        stream = torch.cuda.current_stream(device)
+    if device.index == torch.cuda.current_device():
+        _check(call(*args, stream.cuda_stream))
+    else:
+        with torch.cuda.device(device):
+            _check(call(*args, stream.cuda_stream))
+
+
+def mala_paged_update(lens, new_lens, block_table, free_ring, free_state, lens_out, cu_seqlens,
+                      slots, positions, free_state_out, page_size, num_pages, stream=None):
+    R, W = _dims(block_table, "block_table", 2)
+    _spec(block_table, "block_table", torch.int32, (R, W))
+    _spec(lens, "lens", torch.int32, (R,))
+    _spec(new_lens, "new_lens", torch.int32, (R,))
+    (C,) = _dims(free_ring, "free_ring", 1)
+    _spec(free_ring, "free_ring", torch.int32, (C,))
+    (fs,) = _dims(free_state, "free_state", 1)
+    _spec(free_state, "free_state", torch.int32, (fs,))
+    if fs < 2:
+        raise ValueError("free_state needs two entries (head, count)")
+    _spec(lens_out, "lens_out", torch.int32, (R,))
+    _spec(cu_seqlens, "cu_seqlens", torch.int32, (R + 1,))
+    (T,) = _dims(slots, "slots", 1)
+    _spec(slots, "slots", torch.int32, (T,))
+    _spec(positions, "positions", torch.int32, (T,), optional=True)
+    _spec(free_state_out, "free_state_out", torch.int32, (4,))
+    _on_device((("block_table", block_table), ("lens", lens), ("new_lens", new_lens),
+                ("free_ring", free_ring), ("free_state", free_state), ("lens_out", lens_out),
+                ("cu_seqlens", cu_seqlens), ("slots", slots), ("positions", positions),
+                ("free_state_out", free_state_out)))
+    _launch(block_table.device, stream, load_library().mala_paged_update, lens.data_ptr(),
+            new_lens.data_ptr(), block_table.data_ptr(), free_ring.data_ptr(),
+            free_state.data_ptr(), lens_out.data_ptr(), cu_seqlens.data_ptr(), slots.data_ptr(),
+            _addr(positions), free_state_out.data_ptr(), R, W, page_size, num_pages, C, T)
+
+
+def mala_paged_write(k_new, v_new, slots, cache, stream=None):
+    """k_new, v_new: bf16 [Hkv, T, D] with the same strides, rows of D contiguous (e.g. the
+    transposed slices of a [T, 2, Hkv, D] projection); slots: int32 [T]."""
+    c = _cache(cache)
+    Hkv, T, D = _dims(k_new, "k_new", 3)
+    if k_new.dtype != torch.bfloat16:
+        raise TypeError("k_new must have dtype %s, got %s" % (torch.bfloat16, k_new.dtype))
+    if not isinstance(v_new, torch.Tensor) or v_new.dtype != torch.bfloat16:
+        raise TypeError("v_new must be a torch tensor of the dtype of k_new")
+    if (Hkv, D) != (c.Hkv, c.D):
+        raise ValueError("k_new must have shape %s, got %s" % ((c.Hkv, T, c.D), (Hkv, T, D)))
+    if v_new.shape != k_new.shape or v_new.stride() != k_new.stride():
+        raise ValueError("v_new must have the shape and strides of k_new")
+    if k_new.stride(2) != 1:
+        raise ValueError("the rows of k_new must be contiguous")
+    _spec(slots, "slots", torch.int32, (T,))
+    _on_device((("k_pages", c.k_pages), ("k_new", k_new), ("v_new", v_new), ("slots", slots)))
+    _launch(c.device, stream, load_library().mala_paged_write, k_new.data_ptr(), v_new.data_ptr(),
+            k_new.stride(1) if T > 1 else D, k_new.stride(0) if Hkv > 1 else D, slots.data_ptr(),
+            c._ref, T)
+
+
+def mala_paged_read(cache, block_table, cu_seqlens, max_seqlen, k, v, stream=None):
+    c = _cache(cache)
+    S, W = _dims(block_table, "block_table", 2)
+    _spec(block_table, "block_table", torch.int32, (S, W))
+    _spec(cu_seqlens, "cu_seqlens", torch.int32, (S + 1,))
+    _, total, _ = _dims(k, "k", 3)
+    _spec(k, "k", torch.bfloat16, (c.Hkv, total, c.D))
+    _spec(v, "v", torch.bfloat16, (c.Hkv, total, c.D))
+    _on_device((("k_pages", c.k_pages), ("block_table", block_table),
+                ("cu_seqlens", cu_seqlens), ("k", k), ("v", v)))
+    _launch(c.device, stream, load_library().mala_paged_read, c._ref, block_table.data_ptr(),
+            cu_seqlens.data_ptr(), k.data_ptr(), v.data_ptr(), S, W, int(max_seqlen), total)
+
+
+def mala_paged_decode_workspace_size(B, Hq, Hkv, D, max_len, split_tokens):
+    return int(load_library().mala_paged_decode_workspace_size(B, Hq, Hkv, D, max_len,
+                                                               split_tokens))
+
+
+def mala_paged_decode(q, cache, block_table, cache_lens, max_len, o, lse, head_tiles, counters,
+                      split_tokens, workspace, scale, tau, stream=None):
+    c = _cache(cache)
+    B, Hq, D = _dims(q, "q", 3)
+    _spec(q, "q", torch.bfloat16, (B, Hq, c.D))
+    _, W = _dims(block_table, "block_table", 2)
+    _spec(block_table, "block_table", torch.int32, (B, W))
+    _spec(cache_lens, "cache_lens", torch.int32, (B,))
+    _spec(o, "o", _OUT, (B, Hq, D))
+    _spec(lse, "lse", torch.float32, (B, Hq))
+    _spec(head_tiles, "head_tiles", torch.int32, (B, Hq), optional=True)
+    _spec(counters, "counters", torch.int64, (NUM_COUNTERS,), optional=True)
+    if workspace is not None:
+        _workspace(workspace)
+    _on_device((("k_pages", c.k_pages), ("q", q), ("block_table", block_table),
+                ("cache_lens", cache_lens), ("o", o), ("lse", lse), ("head_tiles", head_tiles),
+                ("counters", counters), ("workspace", workspace)))
+    _launch(c.device, stream, load_library().mala_paged_decode, q.data_ptr(), c._ref,
+            block_table.data_ptr(), cache_lens.data_ptr(), o.data_ptr(), lse.data_ptr(),
+            _addr(head_tiles), _addr(counters), split_tokens, _addr(workspace),
+            0 if workspace is None else workspace.numel() * workspace.element_size(), B, Hq, W,
+            int(max_len), scale, tau, _out_code(o))
+
+
 # ---------------------------------------------------------------- allocating wrappers
 def fwd(q, k, v, scale, tau, stats=True, stream=None, out_dtype=torch.float32):
     """out_dtype: torch.float32 or torch.bfloat16 for O (LSE is always fp32)."""
@@ -430,3 +607,63 @@ def default_num_splits(B, Hkv, Nk, num_cus=256, waves_per_simd=2):
     tiles = -(-Nk // 32)
     want = max(1, (num_cus * 4 * waves_per_simd) // max(1, B * Hkv))
     return int(max(1, min(want, tiles // 16 if tiles >= 16 else 1)))
+
+
+# ---------------------------------------------------------------- paged KV cache, allocating
+def _on_stream(stream):
+    """Allocations inside belong to the stream the kernels run on, so that memory freed when
+    a call returns is not reused by another stream's work before they have run."""
+    return torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext()
+
+
+def paged_update(lens, new_lens, block_table, free_ring, free_state, max_tokens, page_size,
+                 num_pages, stream=None):
+    """One step's page tables (block_table and free_ring are updated in place): a dict of
+    lens, cu_seqlens, slots, positions ([max_tokens]) and free_state of the next step."""
+    R = lens.shape[0]
+    with _on_stream(stream):
+        i32 = dict(dtype=torch.int32, device=lens.device)
+        out = dict(lens=torch.empty(R, **i32), cu_seqlens=torch.empty(R + 1, **i32),
+                   slots=torch.empty(max_tokens, **i32), positions=torch.empty(max_tokens, **i32),
+                   free_state=torch.empty(4, **i32))
+    mala_paged_update(lens, new_lens, block_table, free_ring, free_state, out["lens"],
+                      out["cu_seqlens"], out["slots"], out["positions"], out["free_state"],
+                      page_size, num_pages, stream=stream)
+    return out
+
+
+def paged_read(cache, block_table, cu_seqlens, max_seqlen, total, stream=None):
+    """Cached rows of a packed batch as k, v [Hkv, total, D] for fwd_varlen (rows that no
+    sequence covers are zeros)."""
+    with _on_stream(stream):
+        k = torch.zeros((cache.Hkv, total, cache.D), dtype=torch.bfloat16, device=cache.device)
+        v = torch.zeros_like(k)
+    mala_paged_read(cache, block_table, cu_seqlens, max_seqlen, k, v, stream=stream)
+    return dict(k=k, v=v)
+
+
+def paged_decode(q, cache, block_table, cache_lens, max_len, scale, tau, split_tokens=None,
+                 stats=True, workspace=None, stream=None, out_dtype=torch.float32):
+    """decode over a PagedCache: block_table int32 [B, max_pages], cache_lens int32 [B] (at
+    most max_len); split_tokens: None for default_split_tokens."""
+    B, Hq, D = q.shape
+    if split_tokens is None:
+        split_tokens = default_split_tokens(B, cache.Hkv, max_len)
+    with _on_stream(stream):
+        o = torch.empty((B, Hq, D), dtype=out_dtype, device=q.device)
+        lse = torch.empty((B, Hq), dtype=torch.float32, device=q.device)
+        ht = torch.empty((B, Hq), dtype=torch.int32, device=q.device) if stats else None
+        cnt = torch.empty(NUM_COUNTERS, dtype=torch.int64, device=q.device) if stats else None
+        if workspace is None:
+            n = mala_paged_decode_workspace_size(B, Hq, cache.Hkv, D, max_len, split_tokens)
+            workspace = torch.empty(max(n, 16), dtype=torch.uint8, device=q.device)
+    mala_paged_decode(q, cache, block_table, cache_lens, max_len, o, lse, ht, cnt, split_tokens,
+                      workspace, scale, tau, stream=stream)
+    return dict(o=o, lse=lse, head_tiles=ht, counters=cnt)
+
+
+def default_split_tokens(B, Hkv, max_len, num_cus=256, waves_per_simd=2):
+    """Tokens per split (a multiple of 32) that give about num_cus * 4 * waves_per_simd splits
+    over batch and KV heads, between 64 and 512."""
+    tokens = -(-B * Hkv * max_len // (num_cus * 4 * waves_per_simd))
+    return int(max(64, min(512, -(-tokens // 32) * 32)))

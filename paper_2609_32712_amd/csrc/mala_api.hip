@@ -10,6 +10,7 @@
 #include "mala.h"
 #include "mala_device.h"
 #include "mala_kernels.h"
+#include "mala_paged.h"
 
 namespace {
 
@@ -451,6 +452,200 @@ int mala_decode_noalloc(const void* q, const void* k_cache, const void* v_cache,
   if ((st = scratch_address(s, &part)) != MALA_OK) return st;
   return run_decode(q, k_cache, v_cache, cache_lens, o, lse, head_tiles, counters, num_splits,
                     (float*)part, B, Hq, Hkv, Nk, D, scale, tau, out_dtype, s);
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------- paged KV cache
+namespace {
+
+// Checks a cache and fills its kernel form.
+int check_cache(const mala_paged_cache_t* c, mala::PagedCache* out) {
+  if (!c || !c->k_pages || !c->v_pages)
+    return fail(MALA_ERR_INVALID_ARG, "null cache, k_pages or v_pages");
+  if (c->num_pages <= 0 || c->page_size <= 0 || c->Hkv <= 0)
+    return fail(MALA_ERR_INVALID_ARG, "non-positive size (num_pages, page_size, Hkv)");
+  if (c->dtype != MALA_CACHE_BF16 && c->dtype != MALA_CACHE_E4M3)
+    return fail(MALA_ERR_INVALID_ARG, "cache dtype must be MALA_CACHE_BF16 or MALA_CACHE_E4M3, got %d", c->dtype);
+  if (c->dtype == MALA_CACHE_BF16 && (c->k_scale || c->v_scale))
+    return fail(MALA_ERR_INVALID_ARG, "a bf16 cache has no scales");
+  if (c->D != 64 && c->D != 128)
+    return fail(MALA_ERR_UNSUPPORTED, "head_dim %d not in {64, 128}", c->D);
+  if (c->page_size % mala::kPageRows)
+    return fail(MALA_ERR_UNSUPPORTED, "page_size %d is not a multiple of %d", c->page_size, mala::kPageRows);
+  if ((int64_t)c->num_pages * c->page_size > INT32_MAX)
+    return fail(MALA_ERR_UNSUPPORTED, "num_pages x page_size reaches 2^31");
+  const int64_t size = c->dtype == MALA_CACHE_E4M3 ? 1 : 2;
+  for (int64_t s : {c->page_stride, c->head_stride, c->token_stride}) {
+    if (s < c->D || (s * size) % 16)
+      return fail(MALA_ERR_INVALID_ARG, "cache strides must be at least D and multiples of 16 bytes");
+    if (s > INT64_MAX / 2 / c->num_pages)
+      return fail(MALA_ERR_UNSUPPORTED, "cache stride too large");
+  }
+  if (c->token_stride * size * mala::kPageRows > INT32_MAX)
+    return fail(MALA_ERR_UNSUPPORTED, "16 rows of the cache span 2^31 bytes");
+  if ((uintptr_t)c->k_pages % 16 || (uintptr_t)c->v_pages % 16)
+    return fail(MALA_ERR_INVALID_ARG, "k_pages or v_pages not 16-byte aligned");
+  if (out) {
+    out->k = (char*)c->k_pages;
+    out->v = (char*)c->v_pages;
+    out->ks = c->k_scale;
+    out->vs = c->v_scale;
+    out->page_stride = c->page_stride * size;
+    out->head_stride = c->head_stride * size;
+    out->token_stride = c->token_stride * size;
+    out->num_pages = c->num_pages;
+    out->page_size = c->page_size;
+    out->Hkv = c->Hkv;
+    out->e4m3 = c->dtype == MALA_CACHE_E4M3;
+  }
+  return MALA_OK;
+}
+
+int check_split_tokens(int split_tokens) {
+  if (split_tokens <= 0 || split_tokens % mala::kDecBk)
+    return fail(MALA_ERR_INVALID_ARG, "split_tokens %d is not a positive multiple of %d", split_tokens, mala::kDecBk);
+  return MALA_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int mala_paged_update(const int32_t* lens, const int32_t* new_lens, int32_t* block_table,
+                      int32_t* free_ring, const int32_t* free_state, int32_t* lens_out,
+                      int32_t* cu_seqlens, int32_t* slots, int32_t* positions,
+                      int32_t* free_state_out, int num_seqs, int max_pages, int page_size,
+                      int num_pages, int ring_size, int max_tokens, void* stream) {
+  g_err[0] = 0;
+  if (!lens || !new_lens || !block_table || !free_ring || !free_state || !lens_out || !cu_seqlens ||
+      !free_state_out || (!slots && max_tokens))
+    return fail(MALA_ERR_INVALID_ARG, "null argument");
+  if (num_seqs <= 0 || max_pages <= 0 || page_size <= 0 || num_pages <= 0 || ring_size <= 0 || max_tokens < 0)
+    return fail(MALA_ERR_INVALID_ARG, "non-positive size");
+  if (page_size % mala::kPageRows)
+    return fail(MALA_ERR_UNSUPPORTED, "page_size %d is not a multiple of %d", page_size, mala::kPageRows);
+  if ((double)num_seqs * max_pages * page_size > INT32_MAX || (int64_t)num_pages * page_size > INT32_MAX)
+    return fail(MALA_ERR_UNSUPPORTED, "num_seqs x max_pages x page_size or num_pages x page_size reaches 2^31");
+  const void* in[] = {lens, new_lens, block_table, free_ring, free_state};
+  const void* out[] = {lens_out, cu_seqlens, slots, positions, free_state_out};
+  for (int i = 0; i < 5; ++i)
+    for (int j = 0; j < 5; ++j)
+      if (out[j] && (in[i] == out[j] || (i < j && out[i] == out[j])))
+        return fail(MALA_ERR_INVALID_ARG, "an output shares its memory with another argument");
+  if (block_table == free_ring) return fail(MALA_ERR_INVALID_ARG, "block_table is free_ring");
+  const mala::PagedUpdateParams p = {lens, new_lens, block_table, free_ring, free_state, lens_out,
+                                     cu_seqlens, slots, positions, free_state_out, num_seqs,
+                                     max_pages, page_size, num_pages, ring_size, max_tokens};
+  const hipError_t e = mala::launch_paged_update(p, (hipStream_t)stream);
+  return e == hipSuccess ? MALA_OK : hip_fail(e, "mala_paged_update: kernel launch");
+}
+
+int mala_paged_write(const void* k_new, const void* v_new, int64_t new_token_stride,
+                     int64_t new_head_stride, const int32_t* slots,
+                     const mala_paged_cache_t* cache, int num_tokens, void* stream) {
+  g_err[0] = 0;
+  mala::PagedWriteParams p;
+  int st = check_cache(cache, &p.c);
+  if (st) return st;
+  if (num_tokens < 0) return fail(MALA_ERR_INVALID_ARG, "negative num_tokens");
+  if (!num_tokens) return MALA_OK;
+  if (!k_new || !v_new || !slots) return fail(MALA_ERR_INVALID_ARG, "null k_new, v_new or slots");
+  if ((uintptr_t)k_new % 16 || (uintptr_t)v_new % 16 || new_token_stride % 8 || new_head_stride % 8 ||
+      new_token_stride < 0 || new_head_stride < 0)
+    return fail(MALA_ERR_INVALID_ARG, "rows of k_new and v_new must be 16-byte aligned");
+  if (new_token_stride > INT64_MAX / 8 / num_tokens || new_head_stride > INT64_MAX / 8 / cache->Hkv)
+    return fail(MALA_ERR_UNSUPPORTED, "k_new stride too large");
+  p.k = (const char*)k_new;
+  p.v = (const char*)v_new;
+  p.token_stride = new_token_stride * 2;
+  p.head_stride = new_head_stride * 2;
+  p.slots = slots;
+  p.T = num_tokens;
+  const hipError_t e = mala::launch_paged_write(p, cache->D, (hipStream_t)stream);
+  return e == hipSuccess ? MALA_OK : hip_fail(e, "mala_paged_write: kernel launch");
+}
+
+int mala_paged_read(const mala_paged_cache_t* cache, const int32_t* block_table,
+                    const int32_t* cu_seqlens, void* k, void* v, int num_seqs, int max_pages,
+                    int max_seqlen, int total, void* stream) {
+  g_err[0] = 0;
+  mala::PagedReadParams p;
+  int st = check_cache(cache, &p.c);
+  if (st) return st;
+  if (!block_table || !cu_seqlens || !k || !v)
+    return fail(MALA_ERR_INVALID_ARG, "null block_table, cu_seqlens, k or v");
+  if (num_seqs <= 0 || max_pages <= 0 || max_seqlen <= 0 || total <= 0)
+    return fail(MALA_ERR_INVALID_ARG, "non-positive size (num_seqs, max_pages, max_seqlen, total)");
+  if (max_seqlen > (int64_t)max_pages * cache->page_size)
+    return fail(MALA_ERR_INVALID_ARG, "max_seqlen (%d) above max_pages x page_size", max_seqlen);
+  if ((uintptr_t)k % 16 || (uintptr_t)v % 16) return fail(MALA_ERR_INVALID_ARG, "k or v not 16-byte aligned");
+  if ((st = check_slice_range(total, cache->D))) return st;
+  p.table = block_table;
+  p.cu = cu_seqlens;
+  p.k = (char*)k;
+  p.v = (char*)v;
+  p.S = num_seqs; p.W = max_pages; p.max_len = max_seqlen; p.total = total;
+  const hipError_t e = mala::launch_paged_read(p, cache->D, (hipStream_t)stream);
+  return e == hipSuccess ? MALA_OK : hip_fail(e, "mala_paged_read: kernel launch");
+}
+
+size_t mala_paged_decode_workspace_size(int B, int Hq, int Hkv, int D, int max_len,
+                                        int split_tokens) {
+  if (B <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || (D != 64 && D != 128) || max_len <= 0 ||
+      split_tokens <= 0 || split_tokens % mala::kDecBk)
+    return 0;
+  const size_t n = mala::paged_decode_blocks(B, Hq, Hkv, max_len, split_tokens);
+  return n > 1 ? round_up((size_t)B * Hq * n * (D + mala::kDecStride) * sizeof(float), 256) : 0;
+}
+
+int mala_paged_decode(const void* q, const mala_paged_cache_t* cache, const int32_t* block_table,
+                      const int32_t* cache_lens, void* o, float* lse, int32_t* head_tiles,
+                      int64_t* counters, int split_tokens, void* workspace,
+                      size_t workspace_bytes, int B, int Hq, int max_pages, int max_len,
+                      float scale, float tau, int out_dtype, void* stream) {
+  g_err[0] = 0;
+  mala::PagedDecParams p;
+  int st = check_cache(cache, &p.c);
+  if (st) return st;
+  if (!q || !block_table || !cache_lens || !o || !lse)
+    return fail(MALA_ERR_INVALID_ARG, "null q, block_table, cache_lens, o or lse");
+  if (max_pages <= 0) return fail(MALA_ERR_INVALID_ARG, "non-positive max_pages");
+  st = check_common(B, Hq, cache->Hkv, 1, max_len, cache->D, 1, scale, tau);
+  if (!st) st = check_dtype(out_dtype, "out_dtype");
+  if (!st) st = check_split_tokens(split_tokens);
+  if (st) return st;
+  if (max_len > (int64_t)max_pages * cache->page_size)
+    return fail(MALA_ERR_INVALID_ARG, "max_len (%d) above max_pages x page_size", max_len);
+  if ((uintptr_t)q % 16 || (uintptr_t)o % 16) return fail(MALA_ERR_INVALID_ARG, "q or o not 16-byte aligned");
+  const size_t need =
+      mala_paged_decode_workspace_size(B, Hq, cache->Hkv, cache->D, max_len, split_tokens);
+  if (need && (!workspace || workspace_bytes < need))
+    return fail(MALA_ERR_WORKSPACE, "mala_paged_decode needs %zu workspace bytes, got %zu", need,
+                workspace_bytes);
+  if (((uintptr_t)workspace) % 16) return fail(MALA_ERR_WORKSPACE, "workspace not 16-byte aligned");
+  p.q = (const __bf16*)q;
+  p.table = block_table;
+  p.lens = cache_lens;
+  p.part = (float*)workspace;
+  p.o = o;
+  p.o_bf16 = out_dtype == MALA_OUT_BF16;
+  p.lse = lse;
+  p.head_tiles = head_tiles;
+  p.counters = (unsigned long long*)counters;
+  p.B = B; p.Hq = Hq; p.W = max_pages; p.max_len = max_len;
+  p.scale2 = scale * mala::kLog2e;
+  p.log2tau = log2_tau(tau);
+  const double groups = (double)B * Hq * mala::paged_decode_blocks(B, Hq, cache->Hkv, max_len, split_tokens);
+  if (groups > INT32_MAX) return fail(MALA_ERR_UNSUPPORTED, "more than 2^31 workgroups");
+  hipStream_t s = (hipStream_t)stream;
+  hipError_t e;
+  if (counters &&
+      (e = mala::launch_fill_zero(counters, mala::kNumCounters * sizeof(int64_t), s)) != hipSuccess)
+    return hip_fail(e, "mala_paged_decode: clearing counters");
+  if ((e = mala::launch_paged_decode(p, cache->D, split_tokens, s)) != hipSuccess)
+    return hip_fail(e, "mala_paged_decode: kernel launch");
+  return MALA_OK;
 }
 
 }  // extern "C"

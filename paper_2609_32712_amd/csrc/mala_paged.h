@@ -1,0 +1,81 @@
+// Parameter blocks and launchers of the paged KV cache kernels.
+#pragma once
+#include <hip/hip_runtime.h>
+#include <stdint.h>
+
+namespace mala {
+
+constexpr int kPageRows = 16;   // page sizes are multiples of this: 16 rows from a multiple of
+                                // 16 on lie in one page, so they share one base address
+
+// Pages of K and V: row r of page i, KV head h at byte i * page_stride + h * head_stride +
+// r * token_stride of k and v.  Strides in bytes (multiples of 16).
+struct PagedCache {
+  char* k;
+  char* v;
+  const float* ks;   // [Hkv] e4m3 scales, or null (1)
+  const float* vs;
+  int64_t page_stride, head_stride, token_stride;
+  int num_pages, page_size, Hkv;
+  int e4m3;
+};
+
+struct PagedUpdateParams {
+  const int32_t* lens;
+  const int32_t* new_lens;
+  int32_t* table;
+  int32_t* ring;
+  const int32_t* state;
+  int32_t* lens_out;
+  int32_t* cu;
+  int32_t* slots;
+  int32_t* positions;   // or null
+  int32_t* state_out;
+  int R, W, P, num_pages, C, max_tokens;
+};
+
+struct PagedWriteParams {
+  PagedCache c;
+  const char* k;        // bf16 rows: token t, head h at byte t * token_stride + h * head_stride
+  const char* v;
+  int64_t token_stride, head_stride;
+  const int32_t* slots;
+  int T;
+};
+
+struct PagedReadParams {
+  PagedCache c;
+  const int32_t* table;
+  const int32_t* cu;
+  char* k;              // bf16 [Hkv, total, D]
+  char* v;
+  int S, W, max_len, total;
+};
+
+struct PagedDecParams {
+  PagedCache c;
+  const __bf16* q;
+  const int32_t* table;
+  const int32_t* lens;
+  float* part;          // [B, Hq, nblk, D + kDecStride]
+  void* o;              // fp32, or bf16 when o_bf16
+  int o_bf16;
+  float* lse;
+  int32_t* head_tiles;  // or null
+  unsigned long long* counters;
+  int B, Hq, W, max_len;
+  int tps;              // tiles per wavefront (tau > 0: per split, from an empty state)
+  int nblk;             // workgroups along the longest cache
+  int nchunk;           // ceil((Hq / Hkv) / 16)
+  float scale2, log2tau;
+};
+
+// Partials of one query head at most (the caller's workspace is sized by it).
+int paged_decode_blocks(int B, int Hq, int Hkv, int max_len, int split_tokens);
+
+hipError_t launch_paged_update(const PagedUpdateParams& p, hipStream_t st);
+hipError_t launch_paged_write(const PagedWriteParams& p, int D, hipStream_t st);
+hipError_t launch_paged_read(const PagedReadParams& p, int D, hipStream_t st);
+hipError_t launch_paged_decode(PagedDecParams p, int D, int split_tokens, hipStream_t st);
+
+}  // namespace mala

@@ -1,0 +1,337 @@
+// The paged KV cache around the decode: page tables from lengths, rows into pages, pages
+// back to packed rows (gfx950).
+//
+// Position p of request r lives in slot table[r][p / P] P + p mod P, P rows per page.
+#include "mala_device.h"
+#include "mala_paged.h"
+
+namespace mala {
+
+namespace {
+
+// ------------------------------------------------------------------ page tables
+// One launch: every workgroup scans the lengths of all requests (they are few: R lengths are
+// 8 R bytes from the L2), so none waits for another, and then does its own share of the
+// tokens and of the pages given back.  What bounds a call is latency: the loads of the
+// lengths, the scan and one dependent load per token (its table entry or its page of the
+// ring).  Inputs and outputs never share an address: a request either takes pages or gives
+// some back, and the ring's popped and pushed places are disjoint while free and used pages
+// together fit it.
+constexpr int kUpdThreads = 1024;
+constexpr int kUpdChunk = 2048;   // tokens (or pages given back) a workgroup takes at a time
+
+struct Scan3 {
+  int grow, need, back;
+};
+
+// Inclusive scan over the workgroup's threads; `sum` is the total.
+__device__ Scan3 scan_block(Scan3 x, Scan3* wave_sums, Scan3* sum) {
+  const int lane = threadIdx.x & 63, w = threadIdx.x >> 6;
+#pragma unroll
+  for (int d = 1; d < 64; d *= 2) {
+    const int a = __shfl_up(x.grow, d), b = __shfl_up(x.need, d), c = __shfl_up(x.back, d);
+    if (lane >= d) {
+      x.grow += a;
+      x.need += b;
+      x.back += c;
+    }
+  }
+  __syncthreads();   // wave_sums of the block before have been read
+  if (lane == 63) wave_sums[w] = x;
+  __syncthreads();
+  Scan3 before = {0, 0, 0}, all = {0, 0, 0};
+  for (int u = 0; u < kUpdThreads / 64; ++u) {
+    const Scan3 y = wave_sums[u];
+    if (u < w) {
+      before.grow += y.grow;
+      before.need += y.need;
+      before.back += y.back;
+    }
+    all.grow += y.grow;
+    all.need += y.need;
+    all.back += y.back;
+  }
+  x.grow += before.grow;
+  x.need += before.need;
+  x.back += before.back;
+  *sum = all;
+  return x;
+}
+
+// The last of the first n entries of a (ascending) that is <= x; a[0] <= x.
+__device__ __forceinline__ int last_not_above(const int* a, int n, int x) {
+  int lo = 0, hi = n;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) / 2;
+    if (a[mid] <= x)
+      lo = mid;
+    else
+      hi = mid;
+  }
+  return lo;
+}
+
+__global__ __launch_bounds__(kUpdThreads) void mala_paged_update_kernel(PagedUpdateParams p) {
+  // the requests of the block being worked on
+  __shared__ int s_start[kUpdThreads], s_old[kUpdThreads], s_have[kUpdThreads];
+  __shared__ int s_page[kUpdThreads];    // its first page in the order of the ring, or -1: refused
+  __shared__ int s_back[kUpdThreads], s_want[kUpdThreads];
+  __shared__ Scan3 wave_sums[kUpdThreads / 64];
+  __shared__ int s_refused;
+
+  const int tid = threadIdx.x, G = gridDim.x, P = p.P;
+  const int most = p.W * P;              // tokens a table row can hold (below 2^31 in all)
+  const int head = min(max(p.state[0], 0), p.C - 1), count = min(max(p.state[1], 0), p.C);
+  if (tid == 0) s_refused = 0;
+
+  int tokens = 0, pages = 0, back = 0, taken = 0;   // of the requests before this block
+  for (int r0 = 0; r0 < p.R; r0 += kUpdThreads) {
+    const int r = r0 + tid, nr = min(kUpdThreads, p.R - r0);
+    int old = 0, now = 0;
+    if (r < p.R) {
+      old = min(max(p.lens[r], 0), most);
+      now = min(max(p.new_lens[r], 0), most);
+    }
+    const int have = (old + P - 1) / P, want = (now + P - 1) / P;
+    const Scan3 mine = {max(now - old, 0), max(want - have, 0), max(have - want, 0)};
+    Scan3 sum;
+    const Scan3 end = scan_block(mine, wave_sums, &sum);
+    const bool granted = mine.need == 0 || pages + end.need <= count;
+    const int start = tokens + end.grow - mine.grow;
+    s_start[tid] = start;
+    s_old[tid] = old;
+    s_have[tid] = have;
+    s_page[tid] = granted ? pages + end.need - mine.need : -1;
+    s_back[tid] = back + end.back - mine.back;
+    s_want[tid] = want;
+    if (blockIdx.x == 0 && r < p.R) {
+      p.cu[r] = start;
+      p.lens_out[r] = granted ? now : old;
+      if (!granted) atomicAdd(&s_refused, 1);
+    }
+    // pages taken: granted requests are those whose pages end within the free ones
+    const int lim = granted && mine.need ? pages + end.need : 0;
+    int mx = lim;
+#pragma unroll
+    for (int d = 32; d >= 1; d /= 2) mx = max(mx, __shfl_xor(mx, d));
+    taken = max(taken, mx);   // of this thread's wavefront; joined at the end
+    __syncthreads();
+
+    // tokens: chunks of kUpdChunk, every G-th of them this workgroup's
+    const int tok_end = tokens + sum.grow;
+    for (int c = tokens / kUpdChunk; (long)c * kUpdChunk < tok_end; ++c) {
+      if (c % G != (int)blockIdx.x) continue;
+      const int t1 = (int)min((long)tok_end, (long)(c + 1) * kUpdChunk);
+      for (int t = max(tokens, c * kUpdChunk) + tid; t < t1; t += kUpdThreads) {
+        const int i = last_not_above(s_start, nr, t);
+        const int pos = s_old[i] + t - s_start[i], page = pos / P, off = pos - page * P;
+        int32_t* entry = p.table + (long)(r0 + i) * p.W + page;
+        int number = -1;
+        if (s_page[i] >= 0) {
+          if (page >= s_have[i]) {
+            const unsigned at = (unsigned)head + s_page[i] + page - s_have[i];
+            number = p.ring[at >= (unsigned)p.C ? at - p.C : at];
+            if (off == 0) *entry = number;
+          } else {
+            number = *entry;
+          }
+        }
+        if (t < p.max_tokens) {
+          p.slots[t] = (unsigned)number < (unsigned)p.num_pages ? number * P + off : -1;
+          if (p.positions) p.positions[t] = pos;
+        }
+      }
+    }
+    // pages given back, to the end of the ring
+    const int back_end = back + sum.back;
+    for (int c = back / kUpdChunk; (long)c * kUpdChunk < back_end; ++c) {
+      if (c % G != (int)blockIdx.x) continue;
+      const int j1 = (int)min((long)back_end, (long)(c + 1) * kUpdChunk);
+      for (int j = max(back, c * kUpdChunk) + tid; j < j1; j += kUpdThreads) {
+        const int i = last_not_above(s_back, nr, j);
+        const int page = s_want[i] + j - s_back[i];
+        if (j < p.C - count) {           // (always, while free and used pages fit the ring)
+          const unsigned at = (unsigned)head + count + j;
+          p.ring[at >= (unsigned)p.C ? at - p.C : at] = p.table[(long)(r0 + i) * p.W + page];
+        }
+      }
+    }
+    tokens += sum.grow;
+    pages += sum.need;
+    back += sum.back;
+    __syncthreads();   // the block's requests have been read
+  }
+  // padding behind the last token
+  for (int c = tokens / kUpdChunk; (long)c * kUpdChunk < p.max_tokens; ++c) {
+    if (c % G != (int)blockIdx.x) continue;
+    const int t1 = (int)min((long)p.max_tokens, (long)(c + 1) * kUpdChunk);
+    for (int t = max(tokens, c * kUpdChunk) + tid; t < t1; t += kUpdThreads) {
+      p.slots[t] = -1;
+      if (p.positions) p.positions[t] = 0;
+    }
+  }
+  if (blockIdx.x == 0) {
+    if ((tid & 63) == 0) wave_sums[tid >> 6].need = taken;
+    __syncthreads();
+    if (tid == 0) {
+      int all = 0;
+      for (int u = 0; u < kUpdThreads / 64; ++u) all = max(all, wave_sums[u].need);
+      p.cu[p.R] = tokens;
+      const unsigned at = (unsigned)head + all;
+      p.state_out[0] = (int)(at >= (unsigned)p.C ? at - p.C : at);
+      p.state_out[1] = count - all + min(back, p.C - count);
+      p.state_out[2] = s_refused;
+      p.state_out[3] = tokens;
+    }
+  }
+}
+
+// ------------------------------------------------------------------ rows into pages
+// e4m3 bytes of 4 fp32 values (nearest even; beyond +-448 the largest finite value, NaN stays)
+__device__ __forceinline__ int to_e4m3x4(float a, float b, float c, float d) {
+  const auto lim = [](float x) { return x != x ? x : fminf(fmaxf(x, -448.f), 448.f); };
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(lim(a), lim(b), 0, false);
+  return __builtin_amdgcn_cvt_pk_fp8_f32(lim(c), lim(d), r, true);
+}
+
+// A thread moves 16 bytes of a row of the cache, of K and of V.  HBM-bound.
+template <int D, bool E4M3>
+__global__ __launch_bounds__(256) void mala_paged_write_kernel(PagedWriteParams p) {
+  constexpr int EPC = E4M3 ? 16 : 8;     // values per 16 bytes of the cache
+  constexpr int CPR = D / EPC;           // 16-byte chunks per row
+  const int Hkv = p.c.Hkv, P = p.c.page_size;
+  const long n = (long)p.T * Hkv * CPR, last = (long)p.c.num_pages * P;
+  for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256) {
+    const int c = (int)(i % CPR);
+    const long th = i / CPR;
+    const long t = th / Hkv;
+    const int h = (int)(th - t * Hkv);
+    const int slot = p.slots[t];
+    if (slot < 0 || slot >= last) continue;
+    const int page = slot / P, row = slot - page * P;
+    const long src = t * p.token_stride + h * p.head_stride + c * EPC * 2;
+    const long dst = page * p.c.page_stride + h * p.c.head_stride + row * p.c.token_stride + c * 16;
+    if constexpr (E4M3) {
+      const float ks = p.c.ks ? p.c.ks[h] : 1.f, vs = p.c.vs ? p.c.vs[h] : 1.f;
+      const auto put = [&](char* pool, const char* in, float s) {
+        i32x4 out;
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          const bf16x8 x = *reinterpret_cast<const bf16x8*>(in + src + 16 * e);
+          out[2 * e] = to_e4m3x4((float)x[0] / s, (float)x[1] / s, (float)x[2] / s, (float)x[3] / s);
+          out[2 * e + 1] = to_e4m3x4((float)x[4] / s, (float)x[5] / s, (float)x[6] / s, (float)x[7] / s);
+        }
+        *reinterpret_cast<i32x4*>(pool + dst) = out;
+      };
+      put(p.c.k, p.k, ks);
+      put(p.c.v, p.v, vs);
+    } else {
+      const i32x4 a = *reinterpret_cast<const i32x4*>(p.k + src);
+      const i32x4 b = *reinterpret_cast<const i32x4*>(p.v + src);
+      *reinterpret_cast<i32x4*>(p.c.k + dst) = a;
+      *reinterpret_cast<i32x4*>(p.c.v + dst) = b;
+    }
+  }
+}
+
+// ------------------------------------------------------------------ pages to packed rows
+// A workgroup takes kReadRows consecutive packed rows (of every head).  HBM-bound.
+constexpr int kReadRows = 16;
+template <int D, bool E4M3>
+__global__ __launch_bounds__(256) void mala_paged_read_kernel(PagedReadParams p) {
+  constexpr int EPC = E4M3 ? 16 : 8;
+  constexpr int CPR = D / EPC;
+  __shared__ int s_seq;
+  const int tid = threadIdx.x, row0 = blockIdx.x * kReadRows, Hkv = p.c.Hkv, P = p.c.page_size;
+  if (tid == 0) s_seq = 0;
+  __syncthreads();
+  int before = 0;                        // sequences that start at or before row0
+  for (int b = tid; b < p.S; b += 256) before += p.cu[b] <= row0;
+  if (before) atomicAdd(&s_seq, before);
+  __syncthreads();
+  const int seq0 = max(s_seq - 1, 0);
+  const int n = kReadRows * Hkv * CPR;
+  for (int i = tid; i < n; i += 256) {
+    const int c = i % CPR, rh = i / CPR, row = row0 + rh % kReadRows, h = rh / kReadRows;
+    if (row >= p.total) continue;
+    int b = seq0;
+    while (b < p.S && p.cu[b + 1] <= row) ++b;
+    if (b >= p.S) continue;
+    const int pos = row - p.cu[b];
+    if (pos < 0 || pos >= p.max_len) continue;
+    const int page = pos / P, off = pos - page * P;
+    const int number = p.table[(long)b * p.W + page];
+    const long src = (long)number * p.c.page_stride + h * p.c.head_stride + off * p.c.token_stride + c * 16;
+    const bool there = (unsigned)number < (unsigned)p.c.num_pages;
+    i32x4 a = {0, 0, 0, 0}, v = a;
+    if (there) {
+      a = *reinterpret_cast<const i32x4*>(p.c.k + src);
+      v = *reinterpret_cast<const i32x4*>(p.c.v + src);
+    }
+    const long dst = (((long)h * p.total + row) * D + c * EPC) * 2;
+    if constexpr (E4M3) {
+      const float ks = p.c.ks ? p.c.ks[h] : 1.f, vs = p.c.vs ? p.c.vs[h] : 1.f;
+      const auto put = [&](char* out, const i32x4& x, float s) {
+#pragma unroll
+        for (int e = 0; e < 2; ++e) {
+          bf16x8 y;
+#pragma unroll
+          for (int j = 0; j < 2; ++j) {
+            const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(x[2 * e + j], false);
+            const f32x2 hi = __builtin_amdgcn_cvt_pk_f32_fp8(x[2 * e + j], true);
+            y[4 * j] = (bf16)(lo[0] * s);
+            y[4 * j + 1] = (bf16)(lo[1] * s);
+            y[4 * j + 2] = (bf16)(hi[0] * s);
+            y[4 * j + 3] = (bf16)(hi[1] * s);
+          }
+          *reinterpret_cast<bf16x8*>(out + dst + 16 * e) = y;
+        }
+      };
+      put(p.k, a, ks);
+      put(p.v, v, vs);
+    } else {
+      *reinterpret_cast<i32x4*>(p.k + dst) = a;
+      *reinterpret_cast<i32x4*>(p.v + dst) = v;
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_paged_update(const PagedUpdateParams& p, hipStream_t st) {
+  const long chunks = ((long)p.max_tokens + kUpdChunk - 1) / kUpdChunk;
+  const unsigned grid = (unsigned)(chunks < 1 ? 1 : chunks > 256 ? 256 : chunks);
+  hipLaunchKernelGGL(mala_paged_update_kernel, dim3(grid), dim3(kUpdThreads), 0, st, p);
+  return hipGetLastError();
+}
+
+template <int D, bool E4M3>
+static void launch_write_t(const PagedWriteParams& p, hipStream_t st) {
+  const long n = (long)p.T * p.c.Hkv * (D / (E4M3 ? 16 : 8)), blocks = (n + 255) / 256;
+  const unsigned grid = (unsigned)(blocks < (1 << 20) ? blocks : (1 << 20));
+  hipLaunchKernelGGL((mala_paged_write_kernel<D, E4M3>), dim3(grid), dim3(256), 0, st, p);
+}
+
+hipError_t launch_paged_write(const PagedWriteParams& p, int D, hipStream_t st) {
+  if (D == 128)
+    p.c.e4m3 ? launch_write_t<128, true>(p, st) : launch_write_t<128, false>(p, st);
+  else
+    p.c.e4m3 ? launch_write_t<64, true>(p, st) : launch_write_t<64, false>(p, st);
+  return hipGetLastError();
+}
+
+template <int D, bool E4M3>
+static void launch_read_t(const PagedReadParams& p, hipStream_t st) {
+  const unsigned grid = (unsigned)(((long)p.total + kReadRows - 1) / kReadRows);
+  hipLaunchKernelGGL((mala_paged_read_kernel<D, E4M3>), dim3(grid), dim3(256), 0, st, p);
+}
+
+hipError_t launch_paged_read(const PagedReadParams& p, int D, hipStream_t st) {
+  if (D == 128)
+    p.c.e4m3 ? launch_read_t<128, true>(p, st) : launch_read_t<128, false>(p, st);
+  else
+    p.c.e4m3 ? launch_read_t<64, true>(p, st) : launch_read_t<64, false>(p, st);
+  return hipGetLastError();
+}
+
+}  // namespace mala
