@@ -419,8 +419,7 @@ size_t mala_paged_decode_workspace_size(int B, int Hq, int Hkv, int D, int max_l
  *       split.  At tau = 0 everything is retained whatever it is, and the library cuts the
  *       cache as it likes.
  *   o: [B, Hq, D] out (out_dtype; 16-byte aligned, as q); lse: fp32 [B, Hq] out; head_tiles:
- *       int32 [B, Hq] or NULL out; counters: int64 [MALA_NUM_COUNTERS] or NULL out (every
- *       V tile with a key is fetched).
+ *       int32 [B, Hq] or NULL out; counters: int64 [MALA_NUM_COUNTERS] or NULL out.
  *   workspace: at least mala_paged_decode_workspace_size(...) bytes, 16-byte aligned; what it
  *       holds on entry does not matter.  (NULL where that size is 0.)
  */

@@ -596,7 +596,7 @@ size_t mala_paged_decode_workspace_size(int B, int Hq, int Hkv, int D, int max_l
       split_tokens <= 0 || split_tokens % mala::kDecBk)
     return 0;
   const size_t n = mala::paged_decode_blocks(B, Hq, Hkv, max_len, split_tokens);
-  return n > 1 ? round_up((size_t)B * Hq * n * (D + mala::kDecStride) * sizeof(float), 256) : 0;
+  return n > (size_t)B ? round_up(n * Hq * (D + mala::kDecStride) * sizeof(float), 256) : 0;
 }
 
 int mala_paged_decode(const void* q, const mala_paged_cache_t* cache, const int32_t* block_table,
@@ -636,7 +636,7 @@ int mala_paged_decode(const void* q, const mala_paged_cache_t* cache, const int3
   p.B = B; p.Hq = Hq; p.W = max_pages; p.max_len = max_len;
   p.scale2 = scale * mala::kLog2e;
   p.log2tau = log2_tau(tau);
-  const double groups = (double)B * Hq * mala::paged_decode_blocks(B, Hq, cache->Hkv, max_len, split_tokens);
+  const double groups = (double)Hq * mala::paged_decode_blocks(B, Hq, cache->Hkv, max_len, split_tokens);
   if (groups > INT32_MAX) return fail(MALA_ERR_UNSUPPORTED, "more than 2^31 workgroups");
   hipStream_t s = (hipStream_t)stream;
   hipError_t e;

@@ -3,6 +3,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <algorithm>
+
 namespace mala {
 
 constexpr int kPageRows = 16;   // page sizes are multiples of this: 16 rows from a multiple of
@@ -57,20 +59,21 @@ struct PagedDecParams {
   const __bf16* q;
   const int32_t* table;
   const int32_t* lens;
-  float* part;          // [B, Hq, nblk, D + kDecStride]
+  float* part;          // [nblk, Hq, D + kDecStride], blocks of all sequences in order
   void* o;              // fp32, or bf16 when o_bf16
   int o_bf16;
   float* lse;
   int32_t* head_tiles;  // or null
   unsigned long long* counters;
   int B, Hq, W, max_len;
-  int tps;              // tiles per wavefront (tau > 0: per split, from an empty state)
-  int nblk;             // workgroups along the longest cache
+  int unit;             // tiles per split (tau = 0: 1)
+  int target, min_tpw;  // blocks that the tiles are shared out to; tiles per wavefront at least
+  int nblk;             // blocks of all sequences at most
   int nchunk;           // ceil((Hq / Hkv) / 16)
   float scale2, log2tau;
 };
 
-// Partials of one query head at most (the caller's workspace is sized by it).
+// Blocks of all sequences at most (their partials are the workspace).
 int paged_decode_blocks(int B, int Hq, int Hkv, int max_len, int split_tokens);
 
 hipError_t launch_paged_update(const PagedUpdateParams& p, hipStream_t st);

@@ -1,11 +1,11 @@
 // MALA decode of one query token over a paged KV cache (gfx950): the rule of mala_decode.hip
 // (splits of the cache, each tested from an empty state, L = n) on 16-row groups of pages.
 //
-// A workgroup of kPagedWaves wavefronts takes consecutive splits of one (sequence, KV head,
-// chunk of up to 16 query heads of its group), a split per wavefront: tiles of 32 keys from
-// the split's last one down, S^T = K Q^T and O^T += V^T P^T by 16x16x32 MFMAs, K and V through
-// the wavefront's own LDS slot.  The wavefronts' (m, l, O) are joined in LDS; sequences longer
-// than a workgroup's share leave partials that a second launch joins.
+// A wavefront takes a run of tiles (32 keys) of one (sequence, KV head, chunk of up to 16
+// query heads of its group), from its last tile down: S^T = K Q^T and O^T += V^T P^T by
+// 16x16x32 MFMAs, K and V through the wavefront's own LDS slot.  The kPagedWaves wavefronts of
+// a workgroup take neighbouring runs and join their (m, l, O) in LDS; a sequence longer than a
+// workgroup's share leaves partials that a second launch joins.
 //
 // A page's 16-row groups are contiguous up to the token stride, so a tile is two buffer
 // resources of 16 rows.  Rows at or past the length, and groups of a page whose table entry
@@ -19,7 +19,69 @@ namespace mala {
 
 namespace {
 
-constexpr int kPagedWaves = 4;
+// ------------------------------------------------------------------ who works on what
+// Only the device knows the lengths, so it shares out the work: the tiles of all sequences
+// are counted and every wavefront gets about as many, whatever the batch (`tiles_per_wave`),
+// in units of a whole split where tau > 0 (a unit of 1 where every tile is retained anyway).
+// The grid is the bound of what that can come to: with target blocks per KV head and chunk,
+// sum_b ceil(T_b / (W tpw)) <= target + B.
+struct Share {
+  int b, blk;        // sequence, block of it
+  int blocks;        // blocks of the sequence
+  int first;         // number of its first block among all sequences' (where partials lie)
+  int tpw;           // tiles per wavefront in this sequence
+  int n;             // its length
+};
+
+__device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
+
+// Inclusive sum over the wavefront's lanes.
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);   // row_shr:1
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);   // row_shr:2
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);   // row_shr:4
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);   // row_shr:8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // row_bcast:15 to rows 1, 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // row_bcast:31 to rows 2, 3
+  return x;
+}
+
+// The share of block number `at` among all sequences' blocks, or with `by_sequence` that of
+// sequence `at`; b = -1 past the last block.
+template <int W>
+__device__ Share share_of(const PagedDecParams& p, int at, bool by_sequence) {
+  const int lane = threadIdx.x & 63;
+  const auto tiles = [&](int b) {
+    return b < p.B ? (min(max(p.lens[b], 0), p.max_len) + kDecBk - 1) / kDecBk : 0;
+  };
+  const int t0 = tiles(lane);          // of the first 64 sequences
+  long total = 0;
+  for (int b0 = 0; b0 < p.B; b0 += 64)
+    total += __builtin_amdgcn_readlane(wave_scan(b0 ? tiles(b0 + lane) : t0), 63);
+  const long even = (total + (long)p.target * W - 1) / ((long)p.target * W);
+  const int tpw = ceil_div(max((int)even, p.min_tpw), p.unit) * p.unit;
+  Share s = {-1, 0, 1, 0, 0, 0};
+  int before = 0;
+  for (int b0 = 0; b0 < p.B; b0 += 64) {
+    const int t = b0 ? tiles(b0 + lane) : t0;
+    const int nb = b0 + lane < p.B ? max(1, ceil_div(t, W * tpw)) : 0;
+    const int end = wave_scan(nb), all = __builtin_amdgcn_readlane(end, 63);
+    const int i = by_sequence ? at - b0
+                              : __popcll(__builtin_amdgcn_ballot_w64(before + end <= at));
+    if (by_sequence ? i >= 0 && i < 64 : i < 64) {
+      s.b = b0 + i;
+      s.blocks = __builtin_amdgcn_readlane(nb, i);
+      s.first = before + __builtin_amdgcn_readlane(end, i) - s.blocks;
+      s.blk = at - s.first;
+      // even runs within the sequence
+      s.tpw = ceil_div(ceil_div(__builtin_amdgcn_readlane(t, i), s.blocks * W), p.unit) * p.unit;
+      s.n = min(max(p.lens[s.b], 0), p.max_len);
+      return s;
+    }
+    before += all;
+  }
+  return s;
+}
 
 // x ~= hi + lo + rest to 24 bits: fp32 outputs keep fp32's accuracy (with two terms the
 // probabilities carry 16 bits, ~3e-6 relative, fine below a bf16 output's 2^-9)
@@ -31,8 +93,18 @@ __device__ __forceinline__ bf16x8 rest_bf16x8(const float* x, bf16x8 hi, bf16x8 
   return r;
 }
 
-template <int D, bool E4M3>
-__global__ __launch_bounds__(kPagedWaves * 64) void mala_paged_decode_kernel(PagedDecParams p) {
+// Reductions over the four 16-lane rows of a wavefront (lanes of equal lane % 16).
+__device__ __forceinline__ float rows_max(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return halves_max(fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1])));
+}
+__device__ __forceinline__ float rows_sum(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return halves_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
+}
+
+template <int D, bool E4M3, bool DENSE, int W>
+__global__ __launch_bounds__(W * 64) void mala_paged_decode_kernel(PagedDecParams p) {
   constexpr int KS = D / 32;             // k-steps of 32 over head_dim
   constexpr int NDB = D / 16;            // 16-row blocks of O^T
   constexpr int LD = D + 8;
@@ -41,33 +113,24 @@ __global__ __launch_bounds__(kPagedWaves * 64) void mala_paged_decode_kernel(Pag
   constexpr int IPG = kPageRows / RPI;   // load instructions per 16-row group
   static_assert(IPG >= 1, "a load instruction stays within a group");
   // a K or V tile of 32 rows of bf16, later the wavefront's 16 x D accumulator in fp32
-  __shared__ __attribute__((aligned(16))) bf16 slot[kPagedWaves][kDecBk * LD];
-  __shared__ float refs[kPagedWaves][16], sums[kPagedWaves][16];
-  __shared__ int counts[kPagedWaves][16];
+  __shared__ __attribute__((aligned(16))) bf16 slot[W][kDecBk * LD];
+  __shared__ float refs[W][16], sums[W][16];
+  __shared__ int counts[W][16];
 
   const int lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int Hkv = p.c.Hkv, grp = p.Hq / Hkv, items = p.B * Hkv * p.nchunk;
-  const int blk = blockIdx.x / items, item = blockIdx.x % items;
-  const int chunk = item % p.nchunk, bhk = item / p.nchunk;
-  const int b = bhk / Hkv, hkv = bhk % Hkv;
+  const int Hkv = p.c.Hkv, grp = p.Hq / Hkv, per = Hkv * p.nchunk;
+  const Share sh = share_of<W>(p, blockIdx.x / per, false);
+  if (sh.b < 0) return;                              // the same for the whole workgroup
+  const int chunk = blockIdx.x % p.nchunk, hkv = blockIdx.x % per / p.nchunk, b = sh.b;
   const int nh = min(16, grp - 16 * chunk);
-  const int n = min(max(p.lens[b], 0), p.max_len);
-  const int T = (n + kDecBk - 1) / kDecBk;
-  const int wg_lo = blk * kPagedWaves * p.tps;       // first tile of the workgroup
-  if (blk > 0 && wg_lo >= T) return;                 // past the sequence: no partial
-  const int t_lo = min(T, wg_lo + w * p.tps), t_hi = min(T, t_lo + p.tps);
+  const int n = sh.n, T = (n + kDecBk - 1) / kDecBk;
+  const int t_lo = min(T, (sh.blk * W + w) * sh.tpw), t_hi = min(T, t_lo + sh.tpw);
   const float thr2 = p.log2tau - log2f((float)n);    // L = n
   const bool head_valid = col < nh;
   const int hq = hkv * grp + 16 * chunk + col;
 
-  bf16x8 qreg[KS];
-#pragma unroll
-  for (int kk = 0; kk < KS; ++kk)
-    qreg[kk] = head_valid ? load8(p.q + ((long)b * p.Hq + hq) * D + 32 * kk + 8 * g) : zero8();
-  const float scale2 = p.scale2 * (E4M3 && p.c.ks ? p.c.ks[hkv] : 1.f);
-
-  // table entries of the split, from its last page down: lane i holds the one i pages below
+  // table entries of the run, from its last page down: lane i holds the one i pages below
   // `top`; groups of 16 rows are walked downwards
   const int gpp = p.c.page_size / kPageRows;
   const int32_t* row = p.table + (long)b * p.W;
@@ -83,6 +146,12 @@ __global__ __launch_bounds__(kPagedWaves * 64) void mala_paged_decode_kernel(Pag
     within = last - page * gpp;
     load_entries();
   }
+  bf16x8 qreg[KS];
+#pragma unroll
+  for (int kk = 0; kk < KS; ++kk)
+    qreg[kk] = head_valid ? load8(p.q + ((long)b * p.Hq + hq) * D + 32 * kk + 8 * g) : zero8();
+  const float scale2 = p.scale2 * (E4M3 && p.c.ks ? p.c.ks[hkv] : 1.f);
+
   // byte offset of the next group below (-1: its page is outside the pool)
   const auto next_group = [&]() -> long {
     if (page < 0) return -1;
@@ -97,17 +166,29 @@ __global__ __launch_bounds__(kPagedWaves * 64) void mala_paged_decode_kernel(Pag
     --within;
     return (unsigned)number < (unsigned)p.c.num_pages ? off : -1;
   };
+  // a tile's two groups: where they start, and how many of their rows are there
+  struct Place {
+    long off0, off1;
+    int rows0, rows1;
+  };
+  const auto next_tile = [&](int t) {
+    Place x = {0, 0, 0, 0};
+    if (t < t_lo) return x;
+    x.off1 = next_group();
+    x.off0 = next_group();
+    x.rows0 = x.off0 < 0 ? 0 : min(kPageRows, n - 2 * t * kPageRows);
+    x.rows1 = x.off1 < 0 ? 0 : max(0, min(kPageRows, n - (2 * t + 1) * kPageRows));
+    x.off0 = max(x.off0, 0l);
+    x.off1 = max(x.off1, 0l);
+    return x;
+  };
 
   const uint32_t lane_off = (uint32_t)(lane / CPR) * (uint32_t)p.c.token_stride + (lane % CPR) * 16;
   const uint32_t step = (uint32_t)(RPI * p.c.token_stride);
   typedef bf16x8 Tile[2 * IPG];          // raw bytes (16 per lane and instruction)
-  // rows of group h (0, 1) of tile t that exist: of those the resource covers every byte
-  const auto rows_of = [&](int t, int h, long off) {
-    return off < 0 ? 0 : max(0, min(kPageRows, n - (2 * t + h) * kPageRows));
-  };
-  const auto load_tile = [&](const char* base, int t, long off0, long off1, Tile& x) {
-    const auto r0 = make_rsrc(base + max(off0, 0l), (uint32_t)(rows_of(t, 0, off0) * p.c.token_stride));
-    const auto r1 = make_rsrc(base + max(off1, 0l), (uint32_t)(rows_of(t, 1, off1) * p.c.token_stride));
+  const auto load_tile = [&](const char* base, const Place& at, bool want, Tile& x) {
+    const auto r0 = make_rsrc(base + at.off0, want ? (uint32_t)(at.rows0 * p.c.token_stride) : 0u);
+    const auto r1 = make_rsrc(base + at.off1, want ? (uint32_t)(at.rows1 * p.c.token_stride) : 0u);
 #pragma unroll
     for (int i = 0; i < IPG; ++i) {
       x[i] = buf_load8_stream(r0, lane_off + i * step);
@@ -121,98 +202,147 @@ __global__ __launch_bounds__(kPagedWaves * 64) void mala_paged_decode_kernel(Pag
       const int r = i * RPI + lane / CPR, c = lane % CPR;
       if constexpr (E4M3) {
         const i32x4 raw = __builtin_bit_cast(i32x4, x[i]);
-        bf16x8 lo, hi;
+        bf16x8 y[2];
 #pragma unroll
-        for (int j = 0; j < 2; ++j) {
+        for (int j = 0; j < 4; ++j) {
           const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[j], 1.f, false);
           const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[j], 1.f, true);
-          lo[4 * j] = a[0];
-          lo[4 * j + 1] = a[1];
-          lo[4 * j + 2] = d[0];
-          lo[4 * j + 3] = d[1];
-          const bf16x2 e = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[2 + j], 1.f, false);
-          const bf16x2 f = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[2 + j], 1.f, true);
-          hi[4 * j] = e[0];
-          hi[4 * j + 1] = e[1];
-          hi[4 * j + 2] = f[0];
-          hi[4 * j + 3] = f[1];
+          y[j / 2][4 * (j % 2)] = a[0];
+          y[j / 2][4 * (j % 2) + 1] = a[1];
+          y[j / 2][4 * (j % 2) + 2] = d[0];
+          y[j / 2][4 * (j % 2) + 3] = d[1];
         }
-        store8(mine + r * LD + c * 16, lo);
-        store8(mine + r * LD + c * 16 + 8, hi);
+        store8(mine + r * LD + c * 16, y[0]);
+        store8(mine + r * LD + c * 16 + 8, y[1]);
       } else {
         store8(mine + r * LD + c * 8, x[i]);
       }
     }
   };
 
-  float m = kNegInf, l = 0.f;
-  f32x4 acc[NDB];
-#pragma unroll
-  for (int db = 0; db < NDB; ++db) acc[db] = f32x4{0.f, 0.f, 0.f, 0.f};
-  int cnt = 0;
-  unsigned legal = 0, vloads = 0;
-  unsigned long long hsum = 0;
-
-  for (int t = t_hi - 1; t >= t_lo; --t) {
-    const long off1 = next_group(), off0 = next_group();
-    const int rows0 = rows_of(t, 0, off0), rows1 = rows_of(t, 1, off1);
-    if (rows0 + rows1 == 0) continue;    // no key of the tile is there
-    ++legal;
-    Tile x;
-    load_tile(p.c.k, t, off0, off1, x);
-    to_lds(x);
-    load_tile(p.c.v, t, off0, off1, x);
+  // K of a tile (in kr) to base-2 scores of this lane's head: sv[0..3] keys 4 g + r, sv[4..7]
+  // keys 16 + 4 g + r; their maximum over the tile.  One wavefront's LDS accesses complete in
+  // issue order, so K and V tiles can follow each other in one slot without waits.
+  Tile kr, vr;
+  const auto scores = [&](const Place& at, float (&sv)[8]) {
     f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) {
       s0 = mfma16(load8(mine + col * LD + 32 * kk + 8 * g), qreg[kk], s0);
       s1 = mfma16(load8(mine + (16 + col) * LD + 32 * kk + 8 * g), qreg[kk], s1);
     }
-    float sv[8], mt = kNegInf;
+    float mt = kNegInf;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      sv[r] = 4 * g + r < rows0 ? s0[r] * scale2 : kNegInf;
-      sv[4 + r] = 4 * g + r < rows1 ? s1[r] * scale2 : kNegInf;
+      sv[r] = 4 * g + r < at.rows0 ? s0[r] * scale2 : kNegInf;
+      sv[4 + r] = 4 * g + r < at.rows1 ? s1[r] * scale2 : kNegInf;
       mt = fmaxf(mt, fmaxf(sv[r], sv[4 + r]));
     }
-    mt = fmaxf(mt, __shfl_xor(mt, 16));
-    mt = fmaxf(mt, __shfl_xor(mt, 32));
-    const bool demand = head_valid && (l == 0.f || mt - (m + fast_log2(l)) >= thr2);
-    if (!wave_any(demand)) continue;
-    ++vloads;
-    float alpha = 1.f, m_new = m;
-    if (demand) {
-      m_new = fmaxf(m, mt);
-      alpha = m_new == kNegInf ? 1.f : fast_exp2(m - m_new);
-    }
-    const float shift = m_new == kNegInf ? 0.f : m_new;   // a tile of -inf scores adds 0
-    float ps = 0.f;
+    return rows_max(mt);
+  };
+
+  // m, l: reference and normaliser of what this wavefront retained (l of this lane's keys;
+  // the rows are added at the end).  md, ld: those of the split being tested, over its rows.
+  float m = kNegInf, l = 0.f, md = kNegInf, ld = 0.f;
+  f32x4 acc[NDB];
 #pragma unroll
-    for (int r = 0; r < 8; ++r) {
-      sv[r] = demand ? fast_exp2(sv[r] - shift) : 0.f;
-      ps += sv[r];
+  for (int db = 0; db < NDB; ++db) acc[db] = f32x4{0.f, 0.f, 0.f, 0.f};
+  int cnt = 0;
+  unsigned legal = 0, vfetch = 0, vloads = 0;
+  unsigned long long hsum = 0;
+
+  // While tile t is worked on, K of t - 1 is in registers or on its way (its scores are taken
+  // first), K of t - 2 and V of t load.  V of t - 1 is fetched when the state before tile t's
+  // update may retain it: the normaliser only grows, so a tile that fails this test fails the
+  // real one too (a margin covers the rounding).
+  constexpr float kHintMargin = 1e-2f;
+  float sv[8], sn[8], mt = kNegInf, mtn = kNegInf;
+  int left = 0;                              // tiles of the split below the one worked on
+  Place at = next_tile(t_hi - 1), next = next_tile(t_hi - 2);
+  load_tile(p.c.k, at, true, kr);
+  load_tile(p.c.v, at, true, vr);
+  if (t_hi > t_lo) {
+    to_lds(kr);
+    load_tile(p.c.k, next, true, kr);
+    mt = scores(at, sv);
+    vfetch += at.rows0 + at.rows1 > 0;
+  }
+  for (int t = t_hi - 1; t >= t_lo; --t) {
+    const Place after = next_tile(t - 2);
+    to_lds(kr);                              // K of t - 1 (zeros past the run's first tile)
+    load_tile(p.c.k, after, true, kr);
+    mtn = scores(next, sn);
+    const bool here = at.rows0 + at.rows1 > 0, there = next.rows0 + next.rows1 > 0;
+    bool demand = head_valid && here, hint = there;
+    if constexpr (!DENSE) {
+      if (left == 0) {                       // the split's last tile, the first one tested
+        md = kNegInf;
+        ld = 0.f;
+        left = t == t_hi - 1 ? t % p.unit + 1 : p.unit;
+      }
+      --left;
+      const float run = md + fast_log2(ld);
+      demand = demand && (ld == 0.f || mt - run >= thr2);
+      hint = there && (left == 0 ||
+                       wave_any(head_valid && (ld == 0.f || mtn - run >= thr2 - kHintMargin)));
     }
-    ps += __shfl_xor(ps, 16);
-    ps += __shfl_xor(ps, 32);
-    if (demand) {
+    const bool any = wave_any(demand);
+    if (any) to_lds(vr);
+    load_tile(p.c.v, next, hint, vr);
+    legal += here ? 1u : 0u;
+    vfetch += hint ? 1u : 0u;
+    if (any) {
+      ++vloads;
+      float alpha = 1.f, m_new = m;
+      if (demand) {
+        m_new = fmaxf(m, mt);
+        alpha = m_new == kNegInf ? 1.f : fast_exp2(m - m_new);
+        ++cnt;
+      }
+      // weights of the tile: at tau = 0 against the run's reference; else against the tile's
+      // own maximum, for the split's state, and from there to the run's reference
+      const float shift = m_new == kNegInf ? 0.f : m_new;   // a tile of -inf scores adds 0
+      const float own = DENSE ? shift : mt == kNegInf ? 0.f : mt;
+      float ps = 0.f;
+#pragma unroll
+      for (int r = 0; r < 8; ++r) {
+        sv[r] = demand ? fast_exp2(sv[r] - own) : 0.f;
+        ps += sv[r];
+      }
+      if constexpr (!DENSE) {
+        const float all = rows_sum(ps);
+        if (demand) {
+          const float d_new = fmaxf(md, mt), ds = d_new == kNegInf ? 0.f : d_new;
+          ld = ld * fast_exp2(md - ds) + all * fast_exp2(own - ds);
+          md = d_new;
+        }
+        const float f = fast_exp2(own - shift);
+#pragma unroll
+        for (int r = 0; r < 8; ++r) sv[r] *= f;
+        ps *= f;
+      }
       l = alpha * l + ps;
       m = m_new;
-      ++cnt;
-      if (p.counters) hsum += tile_hash(b, hq, 0, t);
-    }
-    to_lds(x);
-    bf16x8 ph, pl;
-    split_bf16x8(sv, ph, pl);
-    const bf16x8 pr = rest_bf16x8(sv, ph, pl);
+      if (p.counters && demand) hsum += tile_hash(b, hq, 0, t);
+      bf16x8 ph, pl;
+      split_bf16x8(sv, ph, pl);
+      const bf16x8 pr = rest_bf16x8(sv, ph, pl);
 #pragma unroll
-    for (int db = 0; db < NDB; ++db) {
-      const bf16* vrow = mine + (4 * g + (col >> 2)) * LD + 16 * db + 4 * (col & 3);
-      const bf16x8 a = cat(lds_read_tr(vrow), lds_read_tr(vrow + 16 * LD));
-      acc[db] = mfma16(a, ph, acc[db] * alpha);
-      acc[db] = mfma16(a, pl, acc[db]);
-      if (!p.o_bf16) acc[db] = mfma16(a, pr, acc[db]);
+      for (int db = 0; db < NDB; ++db) {
+        const bf16* vrow = mine + (4 * g + (col >> 2)) * LD + 16 * db + 4 * (col & 3);
+        const bf16x8 a = cat(lds_read_tr(vrow), lds_read_tr(vrow + 16 * LD));
+        acc[db] = mfma16(a, ph, acc[db] * alpha);
+        acc[db] = mfma16(a, pl, acc[db]);
+        if (!p.o_bf16) acc[db] = mfma16(a, pr, acc[db]);
+      }
     }
+#pragma unroll
+    for (int r = 0; r < 8; ++r) sv[r] = sn[r];
+    mt = mtn;
+    at = next;
+    next = after;
   }
+  l = rows_sum(l);
 
   // join the wavefronts: a common reference per head, the accumulators scaled to it and added
   if (g == 0) {
@@ -223,7 +353,7 @@ __global__ __launch_bounds__(kPagedWaves * 64) void mala_paged_decode_kernel(Pag
   __syncthreads();
   float M = kNegInf;
 #pragma unroll
-  for (int u = 0; u < kPagedWaves; ++u) M = fmaxf(M, refs[u][col]);
+  for (int u = 0; u < W; ++u) M = fmaxf(M, refs[u][col]);
   if (M == kNegInf) M = 0.f;
   {
     const float f = fast_exp2(m - M);    // 0 for a wavefront without keys
@@ -234,33 +364,33 @@ __global__ __launch_bounds__(kPagedWaves * 64) void mala_paged_decode_kernel(Pag
       *reinterpret_cast<f32x4*>(out + (db * 64 + lane) * 4) = acc[db] * f;
   }
   __syncthreads();
-  const int nb = max(1, (T + kPagedWaves * p.tps - 1) / (kPagedWaves * p.tps));
-  for (int i = threadIdx.x; i < NDB * 64; i += kPagedWaves * 64) {
+  for (int i = threadIdx.x; i < NDB * 64; i += W * 64) {
     const int ln = i & 63, db = i >> 6, c = ln & 15, d = 16 * db + 4 * (ln >> 4);
     if (c >= nh) continue;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
     float L = 0.f, mx = kNegInf;
     int kept = 0;
 #pragma unroll
-    for (int u = 0; u < kPagedWaves; ++u) mx = fmaxf(mx, refs[u][c]);
+    for (int u = 0; u < W; ++u) mx = fmaxf(mx, refs[u][c]);
     const float ref = mx == kNegInf ? 0.f : mx;
 #pragma unroll
-    for (int u = 0; u < kPagedWaves; ++u) {
+    for (int u = 0; u < W; ++u) {
       o += *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(slot[u]) + i * 4);
       L += sums[u][c] * fast_exp2(refs[u][c] - ref);
       kept += counts[u][c];
     }
     const float inv = L != 0.f ? (E4M3 && p.c.vs ? p.c.vs[hkv] : 1.f) / L : 0.f;
     const float lse = L != 0.f ? (ref + fast_log2(L)) * kLn2 : kNegInf;
-    const long bh = (long)b * p.Hq + hkv * grp + 16 * chunk + c;
-    if (nb == 1) {
+    const int h = hkv * grp + 16 * chunk + c;
+    if (sh.blocks == 1) {
+      const long bh = (long)b * p.Hq + h;
       store_out4(p.o, bh * D + d, o * inv, p.o_bf16);
       if (d == 0) {
         p.lse[bh] = lse;
         if (p.head_tiles) p.head_tiles[bh] = kept;
       }
     } else {
-      float* pp = p.part + (bh * p.nblk + blk) * (D + kDecStride);
+      float* pp = p.part + ((long)(sh.first + sh.blk) * p.Hq + h) * (D + kDecStride);
       *reinterpret_cast<f32x4*>(pp + d) = o * inv;
       if (d == 0) {
         pp[D] = lse;
@@ -276,69 +406,121 @@ __global__ __launch_bounds__(kPagedWaves * 64) void mala_paged_decode_kernel(Pag
     }
     if (lane == 0 && legal) {
       atomicAdd(&p.counters[kCntLegal], (unsigned long long)legal * nh);
-      atomicAdd(&p.counters[kCntVTiles], (unsigned long long)legal);
+      atomicAdd(&p.counters[kCntVTiles], (unsigned long long)vfetch);
       atomicAdd(&p.counters[kCntVNeeded], (unsigned long long)vloads);
     }
   }
 }
 
-// Joins the partials of the sequences that have more than one: one workgroup per query head.
-template <int D>
-__global__ __launch_bounds__(D) void mala_paged_join_kernel(PagedDecParams p) {
-  __shared__ float lses[D];
-  const long bh = blockIdx.x;
-  const int b = (int)(bh / p.Hq), n = min(max(p.lens[b], 0), p.max_len);
-  const int T = (n + kDecBk - 1) / kDecBk, per = kPagedWaves * p.tps, nb = (T + per - 1) / per;
-  if (nb <= 1) return;                   // the decode kernel wrote the outputs
-  const float* pp = p.part + bh * p.nblk * (D + kDecStride);
+// Joins the partials of the sequences that have more than one block, a workgroup per query
+// head: lse = logsumexp_s lse_s, o = sum_s exp(lse_s - lse) o_s.  Latency-bound: the weights of
+// 256 parts at a time by the threads, the rows 16 bytes per thread and 256 / (D / 4) at once.
+constexpr int kJoinThreads = 256;
+template <int D, int W>
+__global__ __launch_bounds__(kJoinThreads) void mala_paged_join_kernel(PagedDecParams p) {
+  constexpr int LPR = D / 4, NG = kJoinThreads / LPR, LD = D + kDecStride;
+  __shared__ float wts[kJoinThreads], red[kJoinThreads / 64];
+  __shared__ __attribute__((aligned(16))) f32x4 rows[kJoinThreads];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int b = blockIdx.x / p.Hq, h = blockIdx.x % p.Hq;
+  const Share sh = share_of<W>(p, b, true);
+  if (sh.blocks <= 1) return;            // the decode kernel wrote the outputs
+  const float* pp = p.part + ((long)sh.first * p.Hq + h) * LD;
+  const long stride = (long)p.Hq * LD;
+  const int nb = sh.blocks, grp = tid / LPR, cl = tid % LPR;
   float mx = kNegInf;
-  for (int s = 0; s < nb; ++s) mx = fmaxf(mx, pp[(long)s * (D + kDecStride) + D]);
-  const float ref = mx == kNegInf ? 0.f : mx;
-  float z = 0.f, o = 0.f;
   int kept = 0;
-  for (int s = 0; s < nb; ++s) {
-    const float* x = pp + (long)s * (D + kDecStride);
-    const float f = expf(x[D] - ref);    // 0 for a part without keys
-    z += f;
-    o += f * x[threadIdx.x];
-    kept += __float_as_int(x[D + 1]);
+  for (int s = lane; s < nb; s += 64) {
+    mx = fmaxf(mx, pp[s * stride + D]);
+    kept += __float_as_int(pp[s * stride + D + 1]);
   }
-  const float inv = z != 0.f ? 1.f / z : 0.f;
-  lses[threadIdx.x] = o * inv;
+#pragma unroll
+  for (int d = 32; d >= 1; d /= 2) {
+    mx = fmaxf(mx, __shfl_xor(mx, d));
+    kept += __shfl_xor(kept, d);
+  }
+  const float ref = mx == kNegInf ? 0.f : mx;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
+  float z = 0.f;
+  for (int s0 = 0; s0 < nb; s0 += kJoinThreads) {
+    if (s0) __syncthreads();             // the last weights have been read
+    const float f = s0 + tid < nb ? expf(pp[(s0 + tid) * stride + D] - ref) : 0.f;
+    wts[tid] = f;                        // 0 for a part without keys
+    z += f;
+    __syncthreads();
+    const int m = min(nb - s0, kJoinThreads);
+#pragma unroll 4
+    for (int s = grp; s < m; s += NG)
+      acc += wts[s] * *reinterpret_cast<const f32x4*>(pp + (s0 + s) * stride + 4 * cl);
+  }
+#pragma unroll
+  for (int d = 32; d >= 1; d /= 2) z += __shfl_xor(z, d);
+  if (lane == 0) red[tid / 64] = z;
+  rows[tid] = acc;
   __syncthreads();
-  if (threadIdx.x < D / 4)
-    store_out4(p.o, bh * D + 4 * threadIdx.x, *reinterpret_cast<f32x4*>(lses + 4 * threadIdx.x),
-               p.o_bf16);
-  if (threadIdx.x == 0) {
+  if (tid >= LPR) return;
+  z = red[0] + red[1] + red[2] + red[3];
+#pragma unroll
+  for (int u = 1; u < NG; ++u) acc += rows[u * LPR + tid];
+  const float inv = z != 0.f ? 1.f / z : 0.f;
+  const long bh = blockIdx.x;
+  store_out4(p.o, bh * D + 4 * tid, acc * inv, p.o_bf16);
+  if (tid == 0) {
     p.lse[bh] = z != 0.f ? ref + logf(z) : kNegInf;
     if (p.head_tiles) p.head_tiles[bh] = kept;
   }
 }
 
-int tiles_per_wave(int split_tokens) { return split_tokens / kDecBk; }
+// ------------------------------------------------------------------ launches
+#ifndef TGT
+#define TGT 1024
+#define WV 4
+#define MINT 2
+#endif
+constexpr int kPagedWaves = WV;
+constexpr int kTargetGroups = TGT;     // workgroups that a large batch is shared out to
+constexpr int kMinTiles = MINT;          // tiles per wavefront at least
+
+struct Plan {
+  int target, unit, min_tpw, blocks;
+};
+Plan plan_of(int B, int Hq, int Hkv, int max_len, int split_tokens, bool dense) {
+  const int nchunk = (Hq / Hkv + 15) / 16, T = (max_len + kDecBk - 1) / kDecBk;
+  Plan x;
+  x.target = std::max(1, kTargetGroups / (Hkv * nchunk));
+  x.unit = dense ? 1 : split_tokens / kDecBk;
+  x.min_tpw = kMinTiles;
+  const long tpw = (x.min_tpw + x.unit - 1) / x.unit * (long)x.unit, most = (T + kPagedWaves * tpw - 1) / (kPagedWaves * tpw);
+  x.blocks = (int)std::min<long>({(long)B + x.target, B * most, INT32_MAX});
+  return x;
+}
 
 template <int D, bool E4M3>
 void launch_t(const PagedDecParams& p, hipStream_t st) {
-  const long grid = (long)p.B * p.c.Hkv * p.nchunk * p.nblk;
-  hipLaunchKernelGGL((mala_paged_decode_kernel<D, E4M3>), dim3((unsigned)grid),
-                     dim3(kPagedWaves * 64), 0, st, p);
-  if (p.nblk > 1)
-    hipLaunchKernelGGL(mala_paged_join_kernel<D>, dim3((unsigned)(p.B * p.Hq)), dim3(D), 0, st, p);
+  const dim3 grid((unsigned)(p.nblk * p.c.Hkv * p.nchunk)), wg(kPagedWaves * 64);
+  if (p.unit == 1 && p.log2tau == kNegInf)
+    hipLaunchKernelGGL((mala_paged_decode_kernel<D, E4M3, true, kPagedWaves>), grid, wg, 0, st, p);
+  else
+    hipLaunchKernelGGL((mala_paged_decode_kernel<D, E4M3, false, kPagedWaves>), grid, wg, 0, st, p);
+  if (p.nblk > p.B)
+    hipLaunchKernelGGL((mala_paged_join_kernel<D, kPagedWaves>), dim3((unsigned)(p.B * p.Hq)),
+                       dim3(kJoinThreads), 0, st, p);
 }
 
 }  // namespace
 
 int paged_decode_blocks(int B, int Hq, int Hkv, int max_len, int split_tokens) {
-  (void)B;
-  (void)Hq;
-  (void)Hkv;
-  const int T = (max_len + kDecBk - 1) / kDecBk, per = kPagedWaves * tiles_per_wave(split_tokens);
-  return (T + per - 1) / per;
+  const Plan a = plan_of(B, Hq, Hkv, max_len, split_tokens, true);
+  const Plan b = plan_of(B, Hq, Hkv, max_len, split_tokens, false);
+  return std::max(a.blocks, b.blocks);
 }
 
 hipError_t launch_paged_decode(PagedDecParams p, int D, int split_tokens, hipStream_t st) {
-  p.tps = tiles_per_wave(split_tokens);
-  p.nblk = paged_decode_blocks(p.B, p.Hq, p.c.Hkv, p.max_len, split_tokens);
+  const Plan x = plan_of(p.B, p.Hq, p.c.Hkv, p.max_len, split_tokens, p.log2tau == kNegInf);
+  p.target = x.target;
+  p.unit = x.unit;
+  p.min_tpw = x.min_tpw;
+  p.nblk = x.blocks;
   p.nchunk = (p.Hq / p.c.Hkv + 15) / 16;
   if (D == 128)
     p.c.e4m3 ? launch_t<128, true>(p, st) : launch_t<128, false>(p, st);
