@@ -392,7 +392,7 @@ class PagedCache:
                     ("v_scale", v_scale)))
         self.k_pages, self.v_pages, self.k_scale, self.v_scale = k_pages, v_pages, k_scale, v_scale
         self.num_pages, self.Hkv, self.page_size, self.D = N, Hkv, P, D
-        self.device = k_pages.device
+        self.device = k_pages.get_device()
         # (the stride of an axis of one entry is never used)
         st = [k_pages.stride(i) if k_pages.shape[i] > 1 else max(D, 16) for i in range(3)]
         self._struct = _PagedCacheStruct(
@@ -414,41 +414,64 @@ def _cache(cache):
     return cache
 
 
+def _args(device, *specs):
+    """(tensor, name, dtype, shape) of each argument (None: left out): the checks of _spec and
+    _on_device, in one quick look where everything is right.  A call of a few microseconds on
+    the GPU must not take longer here."""
+    for t, name, dtype, shape in specs:
+        if (type(t) is torch.Tensor and t.dtype is dtype and t.shape == shape
+                and t.get_device() == device and t.is_contiguous()):
+            continue
+        if t is not None:
+            _spec(t, name, dtype, shape)
+            if not t.is_cuda:
+                raise TypeError("%s must be a CUDA (HIP) tensor" % name)
+            if t.get_device() != device:
+                raise TypeError("%s is on %s, the other tensors on cuda:%d" % (name, t.device, device))
+
+
+def _device(t, name):
+    if not t.is_cuda:
+        raise TypeError("%s must be a CUDA (HIP) tensor" % name)
+    return t.get_device()
+
+
+def _required(**named):
+    for name, t in named.items():
+        if t is None:
+            raise TypeError("%s is required" % name)
+
+
 def _launch(device, stream, call, *args):
     """call(*args, stream) with the tensors' device current, on the given stream or on that
     device's current one."""
-    if stream is None:
-        stream = torch.cuda.current_stream(device)
-    if device.index == torch.cuda.current_device():
-        _check(call(*args, stream.cuda_stream))
+    s = torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
+    if device == torch.cuda.current_device():
+        status = call(*args, s)
     else:
         with torch.cuda.device(device):
-            _check(call(*args, stream.cuda_stream))
+            status = call(*args, s)
+    if status != MALA_OK:
+        _check(status)
 
 
 def mala_paged_update(lens, new_lens, block_table, free_ring, free_state, lens_out, cu_seqlens,
                       slots, positions, free_state_out, page_size, num_pages, stream=None):
     R, W = _dims(block_table, "block_table", 2)
-    _spec(block_table, "block_table", torch.int32, (R, W))
-    _spec(lens, "lens", torch.int32, (R,))
-    _spec(new_lens, "new_lens", torch.int32, (R,))
     (C,) = _dims(free_ring, "free_ring", 1)
-    _spec(free_ring, "free_ring", torch.int32, (C,))
     (fs,) = _dims(free_state, "free_state", 1)
-    _spec(free_state, "free_state", torch.int32, (fs,))
+    (T,) = _dims(slots, "slots", 1)
     if fs < 2:
         raise ValueError("free_state needs two entries (head, count)")
-    _spec(lens_out, "lens_out", torch.int32, (R,))
-    _spec(cu_seqlens, "cu_seqlens", torch.int32, (R + 1,))
-    (T,) = _dims(slots, "slots", 1)
-    _spec(slots, "slots", torch.int32, (T,))
-    _spec(positions, "positions", torch.int32, (T,), optional=True)
-    _spec(free_state_out, "free_state_out", torch.int32, (4,))
-    _on_device((("block_table", block_table), ("lens", lens), ("new_lens", new_lens),
-                ("free_ring", free_ring), ("free_state", free_state), ("lens_out", lens_out),
-                ("cu_seqlens", cu_seqlens), ("slots", slots), ("positions", positions),
-                ("free_state_out", free_state_out)))
-    _launch(block_table.device, stream, load_library().mala_paged_update, lens.data_ptr(),
+    _required(lens=lens, new_lens=new_lens, lens_out=lens_out, cu_seqlens=cu_seqlens,
+              free_state_out=free_state_out)
+    dev, i32 = _device(block_table, "block_table"), torch.int32
+    _args(dev, (block_table, "block_table", i32, (R, W)), (lens, "lens", i32, (R,)),
+          (new_lens, "new_lens", i32, (R,)), (free_ring, "free_ring", i32, (C,)),
+          (free_state, "free_state", i32, (fs,)), (lens_out, "lens_out", i32, (R,)),
+          (cu_seqlens, "cu_seqlens", i32, (R + 1,)), (slots, "slots", i32, (T,)),
+          (positions, "positions", i32, (T,)), (free_state_out, "free_state_out", i32, (4,)))
+    _launch(dev, stream, (_lib or load_library()).mala_paged_update, lens.data_ptr(),
             new_lens.data_ptr(), block_table.data_ptr(), free_ring.data_ptr(),
             free_state.data_ptr(), lens_out.data_ptr(), cu_seqlens.data_ptr(), slots.data_ptr(),
             _addr(positions), free_state_out.data_ptr(), R, W, page_size, num_pages, C, T)
@@ -459,35 +482,38 @@ def mala_paged_write(k_new, v_new, slots, cache, stream=None):
     transposed slices of a [T, 2, Hkv, D] projection); slots: int32 [T]."""
     c = _cache(cache)
     Hkv, T, D = _dims(k_new, "k_new", 3)
-    if k_new.dtype != torch.bfloat16:
-        raise TypeError("k_new must have dtype %s, got %s" % (torch.bfloat16, k_new.dtype))
-    if not isinstance(v_new, torch.Tensor) or v_new.dtype != torch.bfloat16:
-        raise TypeError("v_new must be a torch tensor of the dtype of k_new")
-    if (Hkv, D) != (c.Hkv, c.D):
+    _dims(v_new, "v_new", 3)
+    if k_new.dtype != torch.bfloat16 or v_new.dtype != torch.bfloat16:
+        raise TypeError("k_new and v_new must have dtype %s, got %s and %s"
+                        % (torch.bfloat16, k_new.dtype, v_new.dtype))
+    if Hkv != c.Hkv or D != c.D:
         raise ValueError("k_new must have shape %s, got %s" % ((c.Hkv, T, c.D), (Hkv, T, D)))
-    if v_new.shape != k_new.shape or v_new.stride() != k_new.stride():
+    st = k_new.stride()
+    if v_new.shape != k_new.shape or v_new.stride() != st:
         raise ValueError("v_new must have the shape and strides of k_new")
-    if k_new.stride(2) != 1:
+    if st[2] != 1:
         raise ValueError("the rows of k_new must be contiguous")
-    _spec(slots, "slots", torch.int32, (T,))
-    _on_device((("k_pages", c.k_pages), ("k_new", k_new), ("v_new", v_new), ("slots", slots)))
-    _launch(c.device, stream, load_library().mala_paged_write, k_new.data_ptr(), v_new.data_ptr(),
-            k_new.stride(1) if T > 1 else D, k_new.stride(0) if Hkv > 1 else D, slots.data_ptr(),
+    if k_new.get_device() != c.device or v_new.get_device() != c.device:
+        raise TypeError("k_new and v_new must be CUDA (HIP) tensors on the device of the cache")
+    _required(slots=slots)
+    _args(c.device, (slots, "slots", torch.int32, (T,)))
+    _launch(c.device, stream, (_lib or load_library()).mala_paged_write, k_new.data_ptr(),
+            v_new.data_ptr(), st[1] if T > 1 else D, st[0] if Hkv > 1 else D, slots.data_ptr(),
             c._ref, T)
 
 
 def mala_paged_read(cache, block_table, cu_seqlens, max_seqlen, k, v, stream=None):
     c = _cache(cache)
     S, W = _dims(block_table, "block_table", 2)
-    _spec(block_table, "block_table", torch.int32, (S, W))
-    _spec(cu_seqlens, "cu_seqlens", torch.int32, (S + 1,))
-    _, total, _ = _dims(k, "k", 3)
-    _spec(k, "k", torch.bfloat16, (c.Hkv, total, c.D))
-    _spec(v, "v", torch.bfloat16, (c.Hkv, total, c.D))
-    _on_device((("k_pages", c.k_pages), ("block_table", block_table),
-                ("cu_seqlens", cu_seqlens), ("k", k), ("v", v)))
-    _launch(c.device, stream, load_library().mala_paged_read, c._ref, block_table.data_ptr(),
-            cu_seqlens.data_ptr(), k.data_ptr(), v.data_ptr(), S, W, int(max_seqlen), total)
+    total = _dims(k, "k", 3)[1]
+    _required(cu_seqlens=cu_seqlens, v=v)
+    shape = (c.Hkv, total, c.D)
+    _args(c.device, (block_table, "block_table", torch.int32, (S, W)),
+          (cu_seqlens, "cu_seqlens", torch.int32, (S + 1,)), (k, "k", torch.bfloat16, shape),
+          (v, "v", torch.bfloat16, shape))
+    _launch(c.device, stream, (_lib or load_library()).mala_paged_read, c._ref,
+            block_table.data_ptr(), cu_seqlens.data_ptr(), k.data_ptr(), v.data_ptr(), S, W,
+            int(max_seqlen), total)
 
 
 def mala_paged_decode_workspace_size(B, Hq, Hkv, D, max_len, split_tokens):
@@ -499,24 +525,24 @@ def mala_paged_decode(q, cache, block_table, cache_lens, max_len, o, lse, head_t
                       split_tokens, workspace, scale, tau, stream=None):
     c = _cache(cache)
     B, Hq, D = _dims(q, "q", 3)
-    _spec(q, "q", torch.bfloat16, (B, Hq, c.D))
-    _, W = _dims(block_table, "block_table", 2)
-    _spec(block_table, "block_table", torch.int32, (B, W))
-    _spec(cache_lens, "cache_lens", torch.int32, (B,))
-    _spec(o, "o", _OUT, (B, Hq, D))
-    _spec(lse, "lse", torch.float32, (B, Hq))
-    _spec(head_tiles, "head_tiles", torch.int32, (B, Hq), optional=True)
-    _spec(counters, "counters", torch.int64, (NUM_COUNTERS,), optional=True)
+    W = _dims(block_table, "block_table", 2)[1]
+    _required(cache_lens=cache_lens, o=o, lse=lse)
+    bf16 = o.dtype is torch.bfloat16
+    _args(c.device, (q, "q", torch.bfloat16, (B, Hq, c.D)),
+          (block_table, "block_table", torch.int32, (B, W)),
+          (cache_lens, "cache_lens", torch.int32, (B,)),
+          (o, "o", torch.bfloat16 if bf16 else torch.float32, (B, Hq, D)),
+          (lse, "lse", torch.float32, (B, Hq)), (head_tiles, "head_tiles", torch.int32, (B, Hq)),
+          (counters, "counters", torch.int64, (NUM_COUNTERS,)))
+    nbytes = 0
     if workspace is not None:
-        _workspace(workspace)
-    _on_device((("k_pages", c.k_pages), ("q", q), ("block_table", block_table),
-                ("cache_lens", cache_lens), ("o", o), ("lse", lse), ("head_tiles", head_tiles),
-                ("counters", counters), ("workspace", workspace)))
-    _launch(c.device, stream, load_library().mala_paged_decode, q.data_ptr(), c._ref,
+        nbytes = _workspace(workspace).numel() * workspace.element_size()
+        if workspace.get_device() != c.device:
+            raise TypeError("workspace must be on the device of the cache")
+    _launch(c.device, stream, (_lib or load_library()).mala_paged_decode, q.data_ptr(), c._ref,
             block_table.data_ptr(), cache_lens.data_ptr(), o.data_ptr(), lse.data_ptr(),
-            _addr(head_tiles), _addr(counters), split_tokens, _addr(workspace),
-            0 if workspace is None else workspace.numel() * workspace.element_size(), B, Hq, W,
-            int(max_len), scale, tau, _out_code(o))
+            _addr(head_tiles), _addr(counters), split_tokens, _addr(workspace), nbytes, B, Hq, W,
+            int(max_len), scale, tau, OUT_BF16 if bf16 else OUT_F32)
 
 
 # ---------------------------------------------------------------- allocating wrappers
@@ -636,7 +662,7 @@ def paged_read(cache, block_table, cu_seqlens, max_seqlen, total, stream=None):
     """Cached rows of a packed batch as k, v [Hkv, total, D] for fwd_varlen (rows that no
     sequence covers are zeros)."""
     with _on_stream(stream):
-        k = torch.zeros((cache.Hkv, total, cache.D), dtype=torch.bfloat16, device=cache.device)
+        k = torch.zeros((cache.Hkv, total, cache.D), dtype=torch.bfloat16, device=cache.k_pages.device)
         v = torch.zeros_like(k)
     mala_paged_read(cache, block_table, cu_seqlens, max_seqlen, k, v, stream=stream)
     return dict(k=k, v=v)

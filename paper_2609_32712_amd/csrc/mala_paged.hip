@@ -83,6 +83,11 @@ __global__ __launch_bounds__(kUpdThreads) void mala_paged_update_kernel(PagedUpd
   const int most = p.W * P;              // tokens a table row can hold (below 2^31 in all)
   const int head = min(max(p.state[0], 0), p.C - 1), count = min(max(p.state[1], 0), p.C);
   if (tid == 0) s_refused = 0;
+  // the first of this workgroup's chunks (every G-th) that ends behind item x
+  const auto my_chunk = [&](int x) {
+    const int c = x / kUpdChunk, over = c % G;
+    return c - over + (int)blockIdx.x + ((int)blockIdx.x < over ? G : 0);
+  };
 
   int tokens = 0, pages = 0, back = 0, taken = 0;   // of the requests before this block
   for (int r0 = 0; r0 < p.R; r0 += kUpdThreads) {
@@ -119,8 +124,7 @@ __global__ __launch_bounds__(kUpdThreads) void mala_paged_update_kernel(PagedUpd
 
     // tokens: chunks of kUpdChunk, every G-th of them this workgroup's
     const int tok_end = tokens + sum.grow;
-    for (int c = tokens / kUpdChunk; (long)c * kUpdChunk < tok_end; ++c) {
-      if (c % G != (int)blockIdx.x) continue;
+    for (int c = my_chunk(tokens); (long)c * kUpdChunk < tok_end; c += G) {
       const int t1 = (int)min((long)tok_end, (long)(c + 1) * kUpdChunk);
       for (int t = max(tokens, c * kUpdChunk) + tid; t < t1; t += kUpdThreads) {
         const int i = last_not_above(s_start, nr, t);
@@ -144,8 +148,7 @@ __global__ __launch_bounds__(kUpdThreads) void mala_paged_update_kernel(PagedUpd
     }
     // pages given back, to the end of the ring
     const int back_end = back + sum.back;
-    for (int c = back / kUpdChunk; (long)c * kUpdChunk < back_end; ++c) {
-      if (c % G != (int)blockIdx.x) continue;
+    for (int c = my_chunk(back); (long)c * kUpdChunk < back_end; c += G) {
       const int j1 = (int)min((long)back_end, (long)(c + 1) * kUpdChunk);
       for (int j = max(back, c * kUpdChunk) + tid; j < j1; j += kUpdThreads) {
         const int i = last_not_above(s_back, nr, j);
@@ -162,8 +165,7 @@ __global__ __launch_bounds__(kUpdThreads) void mala_paged_update_kernel(PagedUpd
     __syncthreads();   // the block's requests have been read
   }
   // padding behind the last token
-  for (int c = tokens / kUpdChunk; (long)c * kUpdChunk < p.max_tokens; ++c) {
-    if (c % G != (int)blockIdx.x) continue;
+  for (int c = my_chunk(tokens); (long)c * kUpdChunk < p.max_tokens; c += G) {
     const int t1 = (int)min((long)p.max_tokens, (long)(c + 1) * kUpdChunk);
     for (int t = max(tokens, c * kUpdChunk) + tid; t < t1; t += kUpdThreads) {
       p.slots[t] = -1;
