@@ -19,12 +19,19 @@ namespace mala {
 
 namespace {
 
+#ifndef TGT
+#define TGT 1024
+#define WV 4
+#define MINT 2
+#define WPE 2
+#endif
 // ------------------------------------------------------------------ who works on what
 // Only the device knows the lengths, so it shares out the work: the tiles of all sequences
 // are counted and every wavefront gets about as many, whatever the batch (`tiles_per_wave`),
 // in units of a whole split where tau > 0 (a unit of 1 where every tile is retained anyway).
 // The grid is the bound of what that can come to: with target blocks per KV head and chunk,
 // sum_b ceil(T_b / (W tpw)) <= target + B.
+constexpr int kPagedWaves = WV;        // wavefronts of a workgroup (W)
 struct Share {
   int b, blk;        // sequence, block of it
   int blocks;        // blocks of the sequence
@@ -46,39 +53,42 @@ __device__ __forceinline__ int wave_scan(int x) {
   return x;
 }
 
-// The share of block number `at` among all sequences' blocks, or with `by_sequence` that of
-// sequence `at`; b = -1 past the last block.
-template <int W>
-__device__ Share share_of(const PagedDecParams& p, int at, bool by_sequence) {
+// The share of block number `at` among all sequences' blocks, or with SEQ that of sequence
+// `at`; b = -1 past the last block.  UNIT1: units of one tile (tau = 0).
+template <bool SEQ, bool UNIT1>
+__device__ __forceinline__ Share share_of(const PagedDecParams& p, int at) {
+  constexpr int W = kPagedWaves;
   const int lane = threadIdx.x & 63;
   const auto tiles = [&](int b) {
     return b < p.B ? (min(max(p.lens[b], 0), p.max_len) + kDecBk - 1) / kDecBk : 0;
   };
+  const auto in_units = [&](unsigned x) { return UNIT1 ? x : (x + p.unit - 1) / p.unit * p.unit; };
   const int t0 = tiles(lane);          // of the first 64 sequences
-  long total = 0;
+  unsigned total = 0;
   for (int b0 = 0; b0 < p.B; b0 += 64)
     total += __builtin_amdgcn_readlane(wave_scan(b0 ? tiles(b0 + lane) : t0), 63);
-  const long even = (total + (long)p.target * W - 1) / ((long)p.target * W);
-  const int tpw = ceil_div(max((int)even, p.min_tpw), p.unit) * p.unit;
+  // (a floor plus one: at least the even share)
+  const unsigned even = total / (unsigned)(p.target * W) + 1;
+  const unsigned per_block = W * in_units(max(even, (unsigned)p.min_tpw));
   Share s = {-1, 0, 1, 0, 0, 0};
   int before = 0;
   for (int b0 = 0; b0 < p.B; b0 += 64) {
     const int t = b0 ? tiles(b0 + lane) : t0;
-    const int nb = b0 + lane < p.B ? max(1, ceil_div(t, W * tpw)) : 0;
-    const int end = wave_scan(nb), all = __builtin_amdgcn_readlane(end, 63);
-    const int i = by_sequence ? at - b0
-                              : __popcll(__builtin_amdgcn_ballot_w64(before + end <= at));
-    if (by_sequence ? i >= 0 && i < 64 : i < 64) {
+    const int nb = b0 + lane < p.B ? max(1u, (t + per_block - 1) / per_block) : 0;
+    const int end = wave_scan(nb);
+    const int i = SEQ ? at - b0 : __popcll(__builtin_amdgcn_ballot_w64(before + end <= at));
+    if (SEQ ? i < 64 : i < min(64, p.B - b0)) {
       s.b = b0 + i;
       s.blocks = __builtin_amdgcn_readlane(nb, i);
       s.first = before + __builtin_amdgcn_readlane(end, i) - s.blocks;
       s.blk = at - s.first;
-      // even runs within the sequence
-      s.tpw = ceil_div(ceil_div(__builtin_amdgcn_readlane(t, i), s.blocks * W), p.unit) * p.unit;
       s.n = min(max(p.lens[s.b], 0), p.max_len);
+      // even runs within the sequence
+      const unsigned runs = s.blocks * W;
+      s.tpw = in_units((__builtin_amdgcn_readlane(t, i) + runs - 1) / runs);
       return s;
     }
-    before += all;
+    before += __builtin_amdgcn_readlane(end, 63);
   }
   return s;
 }
@@ -103,8 +113,9 @@ __device__ __forceinline__ float rows_sum(float x) {
   return halves_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
 
-template <int D, bool E4M3, bool DENSE, int W>
-__global__ __launch_bounds__(W * 64) void mala_paged_decode_kernel(PagedDecParams p) {
+template <int D, bool E4M3, bool DENSE, bool F32>
+__global__ __launch_bounds__(kPagedWaves * 64, WPE) void mala_paged_decode_kernel(PagedDecParams p) {
+  constexpr int W = kPagedWaves;
   constexpr int KS = D / 32;             // k-steps of 32 over head_dim
   constexpr int NDB = D / 16;            // 16-row blocks of O^T
   constexpr int LD = D + 8;
@@ -120,79 +131,81 @@ __global__ __launch_bounds__(W * 64) void mala_paged_decode_kernel(PagedDecParam
   const int lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int Hkv = p.c.Hkv, grp = p.Hq / Hkv, per = Hkv * p.nchunk;
-  const Share sh = share_of<W>(p, blockIdx.x / per, false);
+  const Share sh = share_of<false, DENSE>(p, blockIdx.x / per);
   if (sh.b < 0) return;                              // the same for the whole workgroup
   const int chunk = blockIdx.x % p.nchunk, hkv = blockIdx.x % per / p.nchunk, b = sh.b;
-  const int nh = min(16, grp - 16 * chunk);
+  const int nh = min(16, grp - 16 * chunk), h0 = hkv * grp + 16 * chunk;
   const int n = sh.n, T = (n + kDecBk - 1) / kDecBk;
   const int t_lo = min(T, (sh.blk * W + w) * sh.tpw), t_hi = min(T, t_lo + sh.tpw);
-  const float thr2 = p.log2tau - log2f((float)n);    // L = n
   const bool head_valid = col < nh;
-  const int hq = hkv * grp + 16 * chunk + col;
+  const uint32_t ts = (uint32_t)p.c.token_stride;
 
-  // table entries of the run, from its last page down: lane i holds the one i pages below
-  // `top`; groups of 16 rows are walked downwards
-  const int gpp = p.c.page_size / kPageRows;
-  const int32_t* row = p.table + (long)b * p.W;
-  int page = 0, within = 0, top = 0, entries = -1;
-  const auto load_entries = [&]() {
-    top = page;
-    const int at = page - lane;
-    entries = at >= 0 && at < p.W ? row[at] : -1;
+  // Where the 64 16-row groups below group `g_top` are (32 tiles): lane i holds, of group g_top - i,
+  // the byte offset from the pool's start and how many of its rows are there (0: past the
+  // length, or of a page whose entry is outside the pool).
+  uint32_t off_lo = 0, off_hi = 0;
+  int rows = 0;
+  const int32_t* entry = p.table + (long)b * p.W;
+  const unsigned gpp = p.c.page_size / kPageRows;
+  const auto find_groups = [&](int g_top) {
+    const int gr = g_top - lane;
+    rows = gr >= 0 ? max(0, min(kPageRows, n - gr * kPageRows)) : 0;
+    const unsigned page = (unsigned)max(gr, 0) / gpp, within = (unsigned)max(gr, 0) - page * gpp;
+    const int number = rows > 0 ? entry[page] : -1;
+    rows = (unsigned)number < (unsigned)p.c.num_pages ? rows : 0;
+    const uint64_t off = rows ? (uint64_t)number * (uint64_t)p.c.page_stride +
+                                    (uint64_t)hkv * (uint64_t)p.c.head_stride +
+                                    (uint64_t)(within * kPageRows) * ts
+                              : 0;
+    off_lo = (uint32_t)off;
+    off_hi = (uint32_t)(off >> 32);
   };
-  if (t_hi > t_lo) {
-    const int last = 2 * t_hi - 1;
-    page = last / gpp;
-    within = last - page * gpp;
-    load_entries();
-  }
+  find_groups(2 * t_hi - 1);
+
+  // q rows of the heads (zeros for the columns that have none)
   bf16x8 qreg[KS];
+  {
+    const auto r = make_rsrc(p.q + ((long)b * p.Hq + h0) * D, (uint32_t)(nh * D * 2));
 #pragma unroll
-  for (int kk = 0; kk < KS; ++kk)
-    qreg[kk] = head_valid ? load8(p.q + ((long)b * p.Hq + hq) * D + 32 * kk + 8 * g) : zero8();
+    for (int kk = 0; kk < KS; ++kk)
+      qreg[kk] = __builtin_bit_cast(
+          bf16x8, __builtin_amdgcn_raw_buffer_load_b128(r, (col * D + 32 * kk + 8 * g) * 2, 0, 0));
+  }
   const float scale2 = p.scale2 * (E4M3 && p.c.ks ? p.c.ks[hkv] : 1.f);
+  const float thr2 = DENSE ? 0.f : p.log2tau - log2f((float)n);    // L = n
 
-  // byte offset of the next group below (-1: its page is outside the pool)
-  const auto next_group = [&]() -> long {
-    if (page < 0) return -1;
-    if (top - page >= 64) load_entries();
-    const int number = __builtin_amdgcn_readlane(entries, top - page);
-    const long off = number * p.c.page_stride + hkv * p.c.head_stride +
-                     (long)(within * kPageRows) * p.c.token_stride;
-    if (within == 0) {
-      within = gpp;
-      --page;
-    }
-    --within;
-    return (unsigned)number < (unsigned)p.c.num_pages ? off : -1;
-  };
   // a tile's two groups: where they start, and how many of their rows are there
   struct Place {
-    long off0, off1;
+    uint64_t off0, off1;
     int rows0, rows1;
   };
+  int in = 0;                            // lane of the next tile's upper group
   const auto next_tile = [&](int t) {
     Place x = {0, 0, 0, 0};
     if (t < t_lo) return x;
-    x.off1 = next_group();
-    x.off0 = next_group();
-    x.rows0 = x.off0 < 0 ? 0 : min(kPageRows, n - 2 * t * kPageRows);
-    x.rows1 = x.off1 < 0 ? 0 : max(0, min(kPageRows, n - (2 * t + 1) * kPageRows));
-    x.off0 = max(x.off0, 0l);
-    x.off1 = max(x.off1, 0l);
+    if (in == 64) {
+      find_groups(2 * t + 1);
+      in = 0;
+    }
+    x.off1 = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(off_hi, in) << 32 |
+             (uint32_t)__builtin_amdgcn_readlane(off_lo, in);
+    x.rows1 = __builtin_amdgcn_readlane(rows, in);
+    x.off0 = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(off_hi, in + 1) << 32 |
+             (uint32_t)__builtin_amdgcn_readlane(off_lo, in + 1);
+    x.rows0 = __builtin_amdgcn_readlane(rows, in + 1);
+    in += 2;
     return x;
   };
 
-  const uint32_t lane_off = (uint32_t)(lane / CPR) * (uint32_t)p.c.token_stride + (lane % CPR) * 16;
-  const uint32_t step = (uint32_t)(RPI * p.c.token_stride);
+  const uint32_t lane_off = (uint32_t)(lane / CPR) * ts + (lane % CPR) * 16;
   typedef bf16x8 Tile[2 * IPG];          // raw bytes (16 per lane and instruction)
   const auto load_tile = [&](const char* base, const Place& at, bool want, Tile& x) {
-    const auto r0 = make_rsrc(base + at.off0, want ? (uint32_t)(at.rows0 * p.c.token_stride) : 0u);
-    const auto r1 = make_rsrc(base + at.off1, want ? (uint32_t)(at.rows1 * p.c.token_stride) : 0u);
+    const auto r0 = make_rsrc(base + at.off0, want ? at.rows0 * ts : 0u);
+    const auto r1 = make_rsrc(base + at.off1, want ? at.rows1 * ts : 0u);
 #pragma unroll
     for (int i = 0; i < IPG; ++i) {
-      x[i] = buf_load8_stream(r0, lane_off + i * step);
-      x[IPG + i] = buf_load8_stream(r1, lane_off + i * step);
+      x[i] = buf_load8_stream(r0, lane_off + i * (RPI * ts));
+      x[IPG + i] = buf_load8_stream(r1, lane_off + i * (RPI * ts));
     }
   };
   bf16* mine = slot[w];
@@ -323,17 +336,18 @@ __global__ __launch_bounds__(W * 64) void mala_paged_decode_kernel(PagedDecParam
       }
       l = alpha * l + ps;
       m = m_new;
-      if (p.counters && demand) hsum += tile_hash(b, hq, 0, t);
+      if (p.counters && demand) hsum += tile_hash(b, h0 + col, 0, t);
       bf16x8 ph, pl;
       split_bf16x8(sv, ph, pl);
-      const bf16x8 pr = rest_bf16x8(sv, ph, pl);
+      bf16x8 pr;
+      if constexpr (F32) pr = rest_bf16x8(sv, ph, pl);
 #pragma unroll
       for (int db = 0; db < NDB; ++db) {
         const bf16* vrow = mine + (4 * g + (col >> 2)) * LD + 16 * db + 4 * (col & 3);
         const bf16x8 a = cat(lds_read_tr(vrow), lds_read_tr(vrow + 16 * LD));
         acc[db] = mfma16(a, ph, acc[db] * alpha);
         acc[db] = mfma16(a, pl, acc[db]);
-        if (!p.o_bf16) acc[db] = mfma16(a, pr, acc[db]);
+        if constexpr (F32) acc[db] = mfma16(a, pr, acc[db]);
       }
     }
 #pragma unroll
@@ -381,10 +395,10 @@ __global__ __launch_bounds__(W * 64) void mala_paged_decode_kernel(PagedDecParam
     }
     const float inv = L != 0.f ? (E4M3 && p.c.vs ? p.c.vs[hkv] : 1.f) / L : 0.f;
     const float lse = L != 0.f ? (ref + fast_log2(L)) * kLn2 : kNegInf;
-    const int h = hkv * grp + 16 * chunk + c;
+    const int h = h0 + c;
     if (sh.blocks == 1) {
       const long bh = (long)b * p.Hq + h;
-      store_out4(p.o, bh * D + d, o * inv, p.o_bf16);
+      store_out4(p.o, bh * D + d, o * inv, !F32);
       if (d == 0) {
         p.lse[bh] = lse;
         if (p.head_tiles) p.head_tiles[bh] = kept;
@@ -416,14 +430,14 @@ __global__ __launch_bounds__(W * 64) void mala_paged_decode_kernel(PagedDecParam
 // head: lse = logsumexp_s lse_s, o = sum_s exp(lse_s - lse) o_s.  Latency-bound: the weights of
 // 256 parts at a time by the threads, the rows 16 bytes per thread and 256 / (D / 4) at once.
 constexpr int kJoinThreads = 256;
-template <int D, int W>
+template <int D, bool DENSE>
 __global__ __launch_bounds__(kJoinThreads) void mala_paged_join_kernel(PagedDecParams p) {
   constexpr int LPR = D / 4, NG = kJoinThreads / LPR, LD = D + kDecStride;
   __shared__ float wts[kJoinThreads], red[kJoinThreads / 64];
   __shared__ __attribute__((aligned(16))) f32x4 rows[kJoinThreads];
   const int tid = threadIdx.x, lane = tid & 63;
   const int b = blockIdx.x / p.Hq, h = blockIdx.x % p.Hq;
-  const Share sh = share_of<W>(p, b, true);
+  const Share sh = share_of<true, DENSE>(p, b);
   if (sh.blocks <= 1) return;            // the decode kernel wrote the outputs
   const float* pp = p.part + ((long)sh.first * p.Hq + h) * LD;
   const long stride = (long)p.Hq * LD;
@@ -472,12 +486,6 @@ __global__ __launch_bounds__(kJoinThreads) void mala_paged_join_kernel(PagedDecP
 }
 
 // ------------------------------------------------------------------ launches
-#ifndef TGT
-#define TGT 1024
-#define WV 4
-#define MINT 2
-#endif
-constexpr int kPagedWaves = WV;
 constexpr int kTargetGroups = TGT;     // workgroups that a large batch is shared out to
 constexpr int kMinTiles = MINT;          // tiles per wavefront at least
 
@@ -495,16 +503,24 @@ Plan plan_of(int B, int Hq, int Hkv, int max_len, int split_tokens, bool dense) 
   return x;
 }
 
-template <int D, bool E4M3>
+template <int D, bool E4M3, bool DENSE>
 void launch_t(const PagedDecParams& p, hipStream_t st) {
   const dim3 grid((unsigned)(p.nblk * p.c.Hkv * p.nchunk)), wg(kPagedWaves * 64);
-  if (p.unit == 1 && p.log2tau == kNegInf)
-    hipLaunchKernelGGL((mala_paged_decode_kernel<D, E4M3, true, kPagedWaves>), grid, wg, 0, st, p);
+  if (p.o_bf16)
+    hipLaunchKernelGGL((mala_paged_decode_kernel<D, E4M3, DENSE, false>), grid, wg, 0, st, p);
   else
-    hipLaunchKernelGGL((mala_paged_decode_kernel<D, E4M3, false, kPagedWaves>), grid, wg, 0, st, p);
+    hipLaunchKernelGGL((mala_paged_decode_kernel<D, E4M3, DENSE, true>), grid, wg, 0, st, p);
   if (p.nblk > p.B)
-    hipLaunchKernelGGL((mala_paged_join_kernel<D, kPagedWaves>), dim3((unsigned)(p.B * p.Hq)),
+    hipLaunchKernelGGL((mala_paged_join_kernel<D, DENSE>), dim3((unsigned)(p.B * p.Hq)),
                        dim3(kJoinThreads), 0, st, p);
+}
+template <int D>
+void launch_d(const PagedDecParams& p, hipStream_t st) {
+  const bool dense = p.log2tau == kNegInf;
+  if (p.c.e4m3)
+    dense ? launch_t<D, true, true>(p, st) : launch_t<D, true, false>(p, st);
+  else
+    dense ? launch_t<D, false, true>(p, st) : launch_t<D, false, false>(p, st);
 }
 
 }  // namespace
@@ -522,10 +538,7 @@ hipError_t launch_paged_decode(PagedDecParams p, int D, int split_tokens, hipStr
   p.min_tpw = x.min_tpw;
   p.nblk = x.blocks;
   p.nchunk = (p.Hq / p.c.Hkv + 15) / 16;
-  if (D == 128)
-    p.c.e4m3 ? launch_t<128, true>(p, st) : launch_t<128, false>(p, st);
-  else
-    p.c.e4m3 ? launch_t<64, true>(p, st) : launch_t<64, false>(p, st);
+  D == 128 ? launch_d<128>(p, st) : launch_d<64>(p, st);
   return hipGetLastError();
 }
 
