@@ -93,14 +93,21 @@ __device__ __forceinline__ Share share_of(const PagedDecParams& p, int at) {
   return s;
 }
 
-// x ~= hi + lo + rest to 24 bits: fp32 outputs keep fp32's accuracy (with two terms the
-// probabilities carry 16 bits, ~3e-6 relative, fine below a bf16 output's 2^-9)
-__device__ __forceinline__ bf16x8 rest_bf16x8(const float* x, bf16x8 hi, bf16x8 lo) {
+// Eight probabilities as bf16 terms whose sum is x: hi + lo to 16 bits (~3e-6 relative, fine
+// below a bf16 output's 2^-9), and with the third term to 24 bits, so that fp32 outputs keep
+// fp32's accuracy.  x becomes what is left.
+__device__ __forceinline__ bf16x8 take_bf16x8(float (&x)[8]) {
 #pragma clang fp contract(off)
-  bf16x8 r;
+  i32x4 u;
 #pragma unroll
-  for (int i = 0; i < 8; ++i) r[i] = (bf16)((x[i] - (float)hi[i]) - (float)lo[i]);
-  return r;
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t h = __builtin_bit_cast(
+        uint32_t, __builtin_convertvector((f32x2{x[2 * i], x[2 * i + 1]}), bf16x2));
+    x[2 * i] -= __uint_as_float(h << 16);          // exact: a bf16 is the upper half of an fp32
+    x[2 * i + 1] -= __uint_as_float(h & 0xffff0000u);
+    u[i] = (int)h;
+  }
+  return __builtin_bit_cast(bf16x8, u);
 }
 
 // Reductions over the four 16-lane rows of a wavefront (lanes of equal lane % 16).
@@ -171,7 +178,18 @@ __global__ __launch_bounds__(kPagedWaves * 64, WPE) void mala_paged_decode_kerne
       qreg[kk] = __builtin_bit_cast(
           bf16x8, __builtin_amdgcn_raw_buffer_load_b128(r, (col * D + 32 * kk + 8 * g) * 2, 0, 0));
   }
-  const float scale2 = p.scale2 * (E4M3 && p.c.ks ? p.c.ks[hkv] : 1.f);
+  // scores are scale2 x (K row . q), scale2 > 0: a negative scale goes into q, and one of 0 stays
+  // large enough to keep a masked score at -inf
+  float scale2 = p.scale2;
+  if (E4M3 && p.c.ks) {
+    scale2 *= p.c.ks[hkv];
+    if (scale2 < 0.f) {
+#pragma unroll
+      for (int kk = 0; kk < KS; ++kk) qreg[kk] = -qreg[kk];
+      scale2 = -scale2;
+    }
+    if (scale2 == 0.f) scale2 = 1e-37f;
+  }
   const float thr2 = DENSE ? 0.f : p.log2tau - log2f((float)n);    // L = n
 
   // a tile's two groups: where they start, and how many of their rows are there
@@ -197,17 +215,24 @@ __global__ __launch_bounds__(kPagedWaves * 64, WPE) void mala_paged_decode_kerne
     return x;
   };
 
-  const uint32_t lane_off = (uint32_t)(lane / CPR) * ts + (lane % CPR) * 16;
+  uint32_t lane_off[IPG];
+#pragma unroll
+  for (int i = 0; i < IPG; ++i) {
+    lane_off[i] = (lane / CPR + i * RPI) * ts + (lane % CPR) * 16;
+    asm("" : "+v"(lane_off[i]));         // kept, not computed again at every load
+  }
   typedef bf16x8 Tile[2 * IPG];          // raw bytes (16 per lane and instruction)
   const auto load_tile = [&](const char* base, const Place& at, bool want, Tile& x) {
     const auto r0 = make_rsrc(base + at.off0, want ? at.rows0 * ts : 0u);
     const auto r1 = make_rsrc(base + at.off1, want ? at.rows1 * ts : 0u);
 #pragma unroll
     for (int i = 0; i < IPG; ++i) {
-      x[i] = buf_load8_stream(r0, lane_off + i * (RPI * ts));
-      x[IPG + i] = buf_load8_stream(r1, lane_off + i * (RPI * ts));
+      x[i] = buf_load8_stream(r0, lane_off[i]);
+      x[IPG + i] = buf_load8_stream(r1, lane_off[i]);
     }
   };
+  // A tile's rows to LDS.  One wavefront's LDS accesses complete in issue order, so K and V
+  // tiles can follow each other in one slot without waits.
   bf16* mine = slot[w];
   const auto to_lds = [&](const Tile& x) {
 #pragma unroll
@@ -215,202 +240,229 @@ __global__ __launch_bounds__(kPagedWaves * 64, WPE) void mala_paged_decode_kerne
       const int r = i * RPI + lane / CPR, c = lane % CPR;
       if constexpr (E4M3) {
         const i32x4 raw = __builtin_bit_cast(i32x4, x[i]);
-        bf16x8 y[2];
+        i32x4 y[2];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[j], 1.f, false);
-          const bf16x2 d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[j], 1.f, true);
-          y[j / 2][4 * (j % 2)] = a[0];
-          y[j / 2][4 * (j % 2) + 1] = a[1];
-          y[j / 2][4 * (j % 2) + 2] = d[0];
-          y[j / 2][4 * (j % 2) + 3] = d[1];
+        for (int k = 0; k < 4; ++k) {
+          y[k / 2][2 * (k % 2)] = __builtin_bit_cast(
+              int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[k], 1.f, false));
+          y[k / 2][2 * (k % 2) + 1] = __builtin_bit_cast(
+              int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[k], 1.f, true));
         }
-        store8(mine + r * LD + c * 16, y[0]);
-        store8(mine + r * LD + c * 16 + 8, y[1]);
+        store8(mine + r * LD + c * 16, __builtin_bit_cast(bf16x8, y[0]));
+        store8(mine + r * LD + c * 16 + 8, __builtin_bit_cast(bf16x8, y[1]));
       } else {
         store8(mine + r * LD + c * 8, x[i]);
       }
     }
   };
 
-  // K of a tile (in kr) to base-2 scores of this lane's head: sv[0..3] keys 4 g + r, sv[4..7]
-  // keys 16 + 4 g + r; their maximum over the tile.  One wavefront's LDS accesses complete in
-  // issue order, so K and V tiles can follow each other in one slot without waits.
-  Tile kr, vr;
-  const auto scores = [&](const Place& at, float (&sv)[8]) {
+  // Products of the K tile in LDS with this lane's head (before scale2): s[0..3] keys 4 g + r,
+  // s[4..7] keys 16 + 4 g + r; keys that are not there -inf.  Returns the scaled maximum.
+  const auto scores = [&](const Place& at, float (&s)[8]) {
     f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) {
       s0 = mfma16(load8(mine + col * LD + 32 * kk + 8 * g), qreg[kk], s0);
       s1 = mfma16(load8(mine + (16 + col) * LD + 32 * kk + 8 * g), qreg[kk], s1);
     }
-    float mt = kNegInf;
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
-      sv[r] = 4 * g + r < at.rows0 ? s0[r] * scale2 : kNegInf;
-      sv[4 + r] = 4 * g + r < at.rows1 ? s1[r] * scale2 : kNegInf;
-      mt = fmaxf(mt, fmaxf(sv[r], sv[4 + r]));
+      s[r] = s0[r];
+      s[4 + r] = s1[r];
     }
-    return rows_max(mt);
+    if (at.rows0 + at.rows1 < kDecBk) {
+#pragma unroll
+      for (int r = 0; r < 4; ++r) {
+        if (4 * g + r >= at.rows0) s[r] = kNegInf;
+        if (4 * g + r >= at.rows1) s[4 + r] = kNegInf;
+      }
+    }
+    float x = fmaxf(s[0], s[4]);
+#pragma unroll
+    for (int r = 1; r < 4; ++r) x = fmaxf(x, fmaxf(s[r], s[4 + r]));
+    return rows_max(x) * scale2;
   };
 
   // m, l: reference and normaliser of what this wavefront retained (l of this lane's keys;
-  // the rows are added at the end).  md, ld: those of the split being tested, over its rows.
-  float m = kNegInf, l = 0.f, md = kNegInf, ld = 0.f;
+  // the rows are added at the end).
+  float m = kNegInf, l = 0.f;
   f32x4 acc[NDB];
 #pragma unroll
   for (int db = 0; db < NDB; ++db) acc[db] = f32x4{0.f, 0.f, 0.f, 0.f};
+  // moves the reference up to m_new (most tiles leave every head's where it is)
+  const auto raise = [&](float m_new) {
+    if (!wave_any(m_new > m)) return;
+    const float alpha = m_new > m ? fast_exp2(m - m_new) : 1.f;
+    l *= alpha;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) acc[db] *= alpha;
+    m = m_new;
+  };
+  // adds the V tile in LDS, weighted
+  const auto add_values = [&](float (&x)[8]) {
+    const bf16x8 ph = take_bf16x8(x), pl = take_bf16x8(x);
+    bf16x8 pr;
+    if constexpr (F32) pr = take_bf16x8(x);
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) {
+      const bf16* vrow = mine + (4 * g + (col >> 2)) * LD + 16 * db + 4 * (col & 3);
+      const bf16x8 a = cat(lds_read_tr(vrow), lds_read_tr(vrow + 16 * LD));
+      acc[db] = mfma16(a, ph, acc[db]);
+      acc[db] = mfma16(a, pl, acc[db]);
+      if constexpr (F32) acc[db] = mfma16(a, pr, acc[db]);
+    }
+  };
   int cnt = 0;
   unsigned legal = 0, vfetch = 0, vloads = 0;
   unsigned long long hsum = 0;
-
-  // While tile t is worked on, K of t - 1 is in registers or on its way (its scores are taken
-  // first), K of t - 2 and V of t load.  V of t - 1 is fetched when the state before tile t's
-  // update may retain it: the normaliser only grows, so a tile that fails this test fails the
-  // real one too (a margin covers the rounding).
-  constexpr float kHintMargin = 1e-2f;
-  float sv[8], sn[8], mt = kNegInf, mtn = kNegInf;
-  int left = 0;                              // tiles of the split below the one worked on
-  Place at = next_tile(t_hi - 1), next = next_tile(t_hi - 2);
+  Tile kr, vr;
+  Place at = next_tile(t_hi - 1);
   load_tile(p.c.k, at, true, kr);
   load_tile(p.c.v, at, true, vr);
-  if (t_hi > t_lo) {
+
+  if constexpr (DENSE) {
+    // every tile counts: K and V of the next one load while a tile is worked on.  (Columns
+    // without a head have zero queries; what they hold is never stored.)
+    for (int t = t_hi - 1; t >= t_lo; --t) {
+      const Place next = next_tile(t - 1);
+      to_lds(kr);
+      load_tile(p.c.k, next, true, kr);
+      float s[8];
+      const float mt = scores(at, s);
+      raise(fmaxf(m, mt));
+      const float shift = m == kNegInf ? 0.f : m;       // scores of -inf alone add 0
+      to_lds(vr);
+      load_tile(p.c.v, next, true, vr);
+#pragma unroll
+      for (int r = 0; r < 8; ++r) s[r] = fast_exp2(__builtin_fmaf(s[r], scale2, -shift));
+      l += ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
+      add_values(s);
+      const bool here = at.rows0 + at.rows1 > 0;
+      legal += here ? 1u : 0u;
+      if (p.counters && here) hsum += tile_hash(b, h0 + col, 0, t);
+      at = next;
+    }
+    cnt = legal;
+    vfetch = vloads = legal;
+  } else if (t_hi > t_lo) {
+    // md, ld: reference and normaliser of the split being tested, over all its retained keys.
+    // While tile t is worked on, K of t - 1 is in registers or on its way (its scores are taken
+    // first), K of t - 2 and V of t load.  V of t - 1 is fetched when the state before tile t's
+    // update may retain it: the normaliser only grows, so a tile that fails this test fails the
+    // real one too (a margin covers the rounding).
+    constexpr float kHintMargin = 1e-2f;
+    float md = kNegInf, ld = 0.f, s[8], sn[8];
+    int left = (t_hi - 1) % p.unit + 1;      // tiles of the split from t down
+    Place next = next_tile(t_hi - 2);
     to_lds(kr);
     load_tile(p.c.k, next, true, kr);
-    mt = scores(at, sv);
-    vfetch += at.rows0 + at.rows1 > 0;
-  }
-  for (int t = t_hi - 1; t >= t_lo; --t) {
-    const Place after = next_tile(t - 2);
-    to_lds(kr);                              // K of t - 1 (zeros past the run's first tile)
-    load_tile(p.c.k, after, true, kr);
-    mtn = scores(next, sn);
-    const bool here = at.rows0 + at.rows1 > 0, there = next.rows0 + next.rows1 > 0;
-    bool demand = head_valid && here, hint = there;
-    if constexpr (!DENSE) {
-      if (left == 0) {                       // the split's last tile, the first one tested
-        md = kNegInf;
-        ld = 0.f;
-        left = t == t_hi - 1 ? t % p.unit + 1 : p.unit;
-      }
-      --left;
+    float mt = scores(at, s);
+    vfetch = at.rows0 + at.rows1 > 0;
+    for (int t = t_hi - 1; t >= t_lo; --t) {
+      const Place after = next_tile(t - 2);
+      to_lds(kr);                            // K of t - 1 (zeros past the run's first tile)
+      load_tile(p.c.k, after, true, kr);
+      const float mtn = scores(next, sn);
+      const bool here = at.rows0 + at.rows1 > 0, there = next.rows0 + next.rows1 > 0;
       const float run = md + fast_log2(ld);
-      demand = demand && (ld == 0.f || mt - run >= thr2);
-      hint = there && (left == 0 ||
-                       wave_any(head_valid && (ld == 0.f || mtn - run >= thr2 - kHintMargin)));
-    }
-    const bool any = wave_any(demand);
-    if (any) to_lds(vr);
-    load_tile(p.c.v, next, hint, vr);
-    legal += here ? 1u : 0u;
-    vfetch += hint ? 1u : 0u;
-    if (any) {
-      ++vloads;
-      float alpha = 1.f, m_new = m;
-      if (demand) {
-        m_new = fmaxf(m, mt);
-        alpha = m_new == kNegInf ? 1.f : fast_exp2(m - m_new);
-        ++cnt;
-      }
-      // weights of the tile: at tau = 0 against the run's reference; else against the tile's
-      // own maximum, for the split's state, and from there to the run's reference
-      const float shift = m_new == kNegInf ? 0.f : m_new;   // a tile of -inf scores adds 0
-      const float own = DENSE ? shift : mt == kNegInf ? 0.f : mt;
-      float ps = 0.f;
+      const bool demand = head_valid && here && (ld == 0.f || mt - run >= thr2);
+      const bool last = --left == 0;         // the next tile starts a split: always retained
+      const bool hint =
+          there && (last || wave_any(head_valid && (ld == 0.f || mtn - run >= thr2 - kHintMargin)));
+      const bool any = wave_any(demand);
+      if (any) to_lds(vr);
+      load_tile(p.c.v, next, hint, vr);
+      legal += here ? 1u : 0u;
+      vfetch += hint ? 1u : 0u;
+      if (any) {
+        ++vloads;
+        raise(demand ? fmaxf(m, mt) : m);
+        // weights against the tile's own maximum, for the split's state, and from there to the
+        // run's reference
+        const float shift = m == kNegInf ? 0.f : m;     // a tile of -inf scores adds 0
+        const float own = mt == kNegInf ? 0.f : mt, f = demand ? fast_exp2(own - shift) : 0.f;
 #pragma unroll
-      for (int r = 0; r < 8; ++r) {
-        sv[r] = demand ? fast_exp2(sv[r] - own) : 0.f;
-        ps += sv[r];
-      }
-      if constexpr (!DENSE) {
+        for (int r = 0; r < 8; ++r)
+          s[r] = demand ? fast_exp2(__builtin_fmaf(s[r], scale2, -own)) : 0.f;
+        const float ps = ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
         const float all = rows_sum(ps);
         if (demand) {
           const float d_new = fmaxf(md, mt), ds = d_new == kNegInf ? 0.f : d_new;
           ld = ld * fast_exp2(md - ds) + all * fast_exp2(own - ds);
           md = d_new;
+          ++cnt;
+          if (p.counters) hsum += tile_hash(b, h0 + col, 0, t);
         }
-        const float f = fast_exp2(own - shift);
+        l += ps * f;
 #pragma unroll
-        for (int r = 0; r < 8; ++r) sv[r] *= f;
-        ps *= f;
+        for (int r = 0; r < 8; ++r) s[r] *= f;
+        add_values(s);
       }
-      l = alpha * l + ps;
-      m = m_new;
-      if (p.counters && demand) hsum += tile_hash(b, h0 + col, 0, t);
-      bf16x8 ph, pl;
-      split_bf16x8(sv, ph, pl);
-      bf16x8 pr;
-      if constexpr (F32) pr = rest_bf16x8(sv, ph, pl);
+      if (last) {
+        md = kNegInf;
+        ld = 0.f;
+        left = p.unit;
+      }
 #pragma unroll
-      for (int db = 0; db < NDB; ++db) {
-        const bf16* vrow = mine + (4 * g + (col >> 2)) * LD + 16 * db + 4 * (col & 3);
-        const bf16x8 a = cat(lds_read_tr(vrow), lds_read_tr(vrow + 16 * LD));
-        acc[db] = mfma16(a, ph, acc[db] * alpha);
-        acc[db] = mfma16(a, pl, acc[db]);
-        if constexpr (F32) acc[db] = mfma16(a, pr, acc[db]);
-      }
+      for (int r = 0; r < 8; ++r) s[r] = sn[r];
+      mt = mtn;
+      at = next;
+      next = after;
     }
-#pragma unroll
-    for (int r = 0; r < 8; ++r) sv[r] = sn[r];
-    mt = mtn;
-    at = next;
-    next = after;
   }
   l = rows_sum(l);
 
-  // join the wavefronts: a common reference per head, the accumulators scaled to it and added
+  // join the wavefronts: per head a common reference and normaliser, then every accumulator's
+  // share of the output, added up
   if (g == 0) {
     refs[w][col] = m;
     sums[w][col] = l;
     counts[w][col] = cnt;
   }
   __syncthreads();
-  float M = kNegInf;
+  float M = kNegInf, L = 0.f;
 #pragma unroll
   for (int u = 0; u < W; ++u) M = fmaxf(M, refs[u][col]);
   if (M == kNegInf) M = 0.f;
+#pragma unroll
+  for (int u = 0; u < W; ++u) L += sums[u][col] * fast_exp2(refs[u][col] - M);
+  const long part = (long)(sh.first + sh.blk) * p.Hq + h0;   // of the block's first head
   {
-    const float f = fast_exp2(m - M);    // 0 for a wavefront without keys
+    // (0 for a wavefront without keys)
+    const float f = L != 0.f ? fast_exp2(m - M) * (E4M3 && p.c.vs ? p.c.vs[hkv] : 1.f) / L : 0.f;
     float* out = reinterpret_cast<float*>(mine);
     static_assert(sizeof(slot[0]) >= 16 * D * sizeof(float), "an accumulator fits a tile");
 #pragma unroll
     for (int db = 0; db < NDB; ++db)
       *reinterpret_cast<f32x4*>(out + (db * 64 + lane) * 4) = acc[db] * f;
   }
-  __syncthreads();
-  for (int i = threadIdx.x; i < NDB * 64; i += W * 64) {
-    const int ln = i & 63, db = i >> 6, c = ln & 15, d = 16 * db + 4 * (ln >> 4);
-    if (c >= nh) continue;
-    f32x4 o = {0.f, 0.f, 0.f, 0.f};
-    float L = 0.f, mx = kNegInf;
+  if (threadIdx.x < nh) {
+    const float lse = L != 0.f ? (M + fast_log2(L)) * kLn2 : kNegInf;
     int kept = 0;
 #pragma unroll
-    for (int u = 0; u < W; ++u) mx = fmaxf(mx, refs[u][c]);
-    const float ref = mx == kNegInf ? 0.f : mx;
-#pragma unroll
-    for (int u = 0; u < W; ++u) {
-      o += *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(slot[u]) + i * 4);
-      L += sums[u][c] * fast_exp2(refs[u][c] - ref);
-      kept += counts[u][c];
-    }
-    const float inv = L != 0.f ? (E4M3 && p.c.vs ? p.c.vs[hkv] : 1.f) / L : 0.f;
-    const float lse = L != 0.f ? (ref + fast_log2(L)) * kLn2 : kNegInf;
-    const int h = h0 + c;
+    for (int u = 0; u < W; ++u) kept += counts[u][col];
     if (sh.blocks == 1) {
-      const long bh = (long)b * p.Hq + h;
-      store_out4(p.o, bh * D + d, o * inv, !F32);
-      if (d == 0) {
-        p.lse[bh] = lse;
-        if (p.head_tiles) p.head_tiles[bh] = kept;
-      }
+      const long bh = (long)b * p.Hq + h0 + col;
+      p.lse[bh] = lse;
+      if (p.head_tiles) p.head_tiles[bh] = kept;
     } else {
-      float* pp = p.part + ((long)(sh.first + sh.blk) * p.Hq + h) * (D + kDecStride);
-      *reinterpret_cast<f32x4*>(pp + d) = o * inv;
-      if (d == 0) {
-        pp[D] = lse;
-        pp[D + 1] = __int_as_float(kept);
-      }
+      *reinterpret_cast<f32x2*>(p.part + (part + col) * (D + kDecStride) + D) =
+          f32x2{lse, __int_as_float(kept)};
     }
+  }
+  __syncthreads();
+#pragma unroll
+  for (int i0 = 0; i0 < NDB * 64; i0 += W * 64) {
+    const int i = i0 + threadIdx.x, c = i & 15, d = 16 * (i >> 6) + 4 * ((i & 63) >> 4);
+    f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int u = 0; u < W; ++u)
+      o += *reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(slot[u]) + i * 4);
+    if (c >= nh) continue;
+    if (sh.blocks == 1)
+      store_out4(p.o, ((long)b * p.Hq + h0 + c) * D + d, o, !F32);
+    else
+      *reinterpret_cast<f32x4*>(p.part + (part + c) * (D + kDecStride) + d) = o;
   }
   if (p.counters) {
     if (head_valid && g == 0 && cnt) {
