@@ -502,6 +502,9 @@ int check_cache(const mala_paged_cache_t* c, mala::PagedCache* out) {
   return MALA_OK;
 }
 
+// Decode workspace: where every sequence's partials lie, then the partials.
+size_t paged_plan_bytes(int B) { return round_up((size_t)B * sizeof(int2), 256); }
+
 int check_split_tokens(int split_tokens) {
   if (split_tokens <= 0 || split_tokens % mala::kDecBk)
     return fail(MALA_ERR_INVALID_ARG, "split_tokens %d is not a positive multiple of %d", split_tokens, mala::kDecBk);
@@ -595,8 +598,9 @@ size_t mala_paged_decode_workspace_size(int B, int Hq, int Hkv, int D, int max_l
   if (B <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || (D != 64 && D != 128) || max_len <= 0 ||
       split_tokens <= 0 || split_tokens % mala::kDecBk)
     return 0;
-  const size_t n = mala::paged_decode_blocks(B, Hq, Hkv, max_len, split_tokens);
-  return n > (size_t)B ? round_up(n * Hq * (D + mala::kDecStride) * sizeof(float), 256) : 0;
+  const size_t n = mala::paged_decode_blocks(B, Hq, Hkv, D, max_len, split_tokens);
+  if (n <= (size_t)B) return 0;
+  return paged_plan_bytes(B) + round_up(n * Hq * (D + mala::kDecStride) * sizeof(float), 256);
 }
 
 int mala_paged_decode(const void* q, const mala_paged_cache_t* cache, const int32_t* block_table,
@@ -627,7 +631,8 @@ int mala_paged_decode(const void* q, const mala_paged_cache_t* cache, const int3
   p.q = (const __bf16*)q;
   p.table = block_table;
   p.lens = cache_lens;
-  p.part = (float*)workspace;
+  p.plan = (int2*)workspace;
+  p.part = workspace ? (float*)((char*)workspace + paged_plan_bytes(B)) : nullptr;
   p.o = o;
   p.o_bf16 = out_dtype == MALA_OUT_BF16;
   p.lse = lse;
@@ -636,8 +641,10 @@ int mala_paged_decode(const void* q, const mala_paged_cache_t* cache, const int3
   p.B = B; p.Hq = Hq; p.W = max_pages; p.max_len = max_len;
   p.scale2 = scale * mala::kLog2e;
   p.log2tau = log2_tau(tau);
-  const double groups = (double)Hq * mala::paged_decode_blocks(B, Hq, cache->Hkv, max_len, split_tokens);
-  if (groups > INT32_MAX) return fail(MALA_ERR_UNSUPPORTED, "more than 2^31 workgroups");
+  const double groups =
+      (double)Hq * mala::paged_decode_blocks(B, Hq, cache->Hkv, cache->D, max_len, split_tokens);
+  if (groups > INT32_MAX || (double)B * max_len / mala::kDecBk > INT32_MAX / 2)
+    return fail(MALA_ERR_UNSUPPORTED, "2^31 workgroups or 2^30 tiles, or more");
   hipStream_t s = (hipStream_t)stream;
   hipError_t e;
   if (counters &&

@@ -59,6 +59,7 @@ struct PagedDecParams {
   const __bf16* q;
   const int32_t* table;
   const int32_t* lens;
+  int2* plan;           // [B]: number of a sequence's first block, its blocks
   float* part;          // [nblk, Hq, D + kDecStride], blocks of all sequences in order
   void* o;              // fp32, or bf16 when o_bf16
   int o_bf16;
@@ -74,7 +75,7 @@ struct PagedDecParams {
 };
 
 // Blocks of all sequences at most (their partials are the workspace).
-int paged_decode_blocks(int B, int Hq, int Hkv, int max_len, int split_tokens);
+int paged_decode_blocks(int B, int Hq, int Hkv, int D, int max_len, int split_tokens);
 
 hipError_t launch_paged_update(const PagedUpdateParams& p, hipStream_t st);
 hipError_t launch_paged_write(const PagedWriteParams& p, int D, hipStream_t st);

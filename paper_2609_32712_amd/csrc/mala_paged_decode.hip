@@ -19,19 +19,13 @@ namespace mala {
 
 namespace {
 
-#ifndef TGT
-#define TGT 1024
-#define WV 4
-#define MINT 2
-#define WPE 2
-#endif
 // ------------------------------------------------------------------ who works on what
 // Only the device knows the lengths, so it shares out the work: the tiles of all sequences
 // are counted and every wavefront gets about as many, whatever the batch (`tiles_per_wave`),
 // in units of a whole split where tau > 0 (a unit of 1 where every tile is retained anyway).
 // The grid is the bound of what that can come to: with target blocks per KV head and chunk,
 // sum_b ceil(T_b / (W tpw)) <= target + B.
-constexpr int kPagedWaves = WV;        // wavefronts of a workgroup (W)
+constexpr int kPagedWaves = 4;         // wavefronts of a workgroup (W)
 struct Share {
   int b, blk;        // sequence, block of it
   int blocks;        // blocks of the sequence
@@ -53,9 +47,9 @@ __device__ __forceinline__ int wave_scan(int x) {
   return x;
 }
 
-// The share of block number `at` among all sequences' blocks, or with SEQ that of sequence
-// `at`; b = -1 past the last block.  UNIT1: units of one tile (tau = 0).
-template <bool SEQ, bool UNIT1>
+// The share of block number `at` among all sequences' blocks; b = -1 past the last one.
+// UNIT1: units of one tile (tau = 0).
+template <bool UNIT1>
 __device__ __forceinline__ Share share_of(const PagedDecParams& p, int at) {
   constexpr int W = kPagedWaves;
   const int lane = threadIdx.x & 63;
@@ -76,8 +70,8 @@ __device__ __forceinline__ Share share_of(const PagedDecParams& p, int at) {
     const int t = b0 ? tiles(b0 + lane) : t0;
     const int nb = b0 + lane < p.B ? max(1u, (t + per_block - 1) / per_block) : 0;
     const int end = wave_scan(nb);
-    const int i = SEQ ? at - b0 : __popcll(__builtin_amdgcn_ballot_w64(before + end <= at));
-    if (SEQ ? i < 64 : i < min(64, p.B - b0)) {
+    const int i = __popcll(__builtin_amdgcn_ballot_w64(before + end <= at));
+    if (i < min(64, p.B - b0)) {
       s.b = b0 + i;
       s.blocks = __builtin_amdgcn_readlane(nb, i);
       s.first = before + __builtin_amdgcn_readlane(end, i) - s.blocks;
@@ -121,7 +115,7 @@ __device__ __forceinline__ float rows_sum(float x) {
 }
 
 template <int D, bool E4M3, bool DENSE, bool F32>
-__global__ __launch_bounds__(kPagedWaves * 64, WPE) void mala_paged_decode_kernel(PagedDecParams p) {
+__global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(PagedDecParams p) {
   constexpr int W = kPagedWaves;
   constexpr int KS = D / 32;             // k-steps of 32 over head_dim
   constexpr int NDB = D / 16;            // 16-row blocks of O^T
@@ -138,7 +132,7 @@ __global__ __launch_bounds__(kPagedWaves * 64, WPE) void mala_paged_decode_kerne
   const int lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int Hkv = p.c.Hkv, grp = p.Hq / Hkv, per = Hkv * p.nchunk;
-  const Share sh = share_of<false, DENSE>(p, blockIdx.x / per);
+  const Share sh = share_of<DENSE>(p, blockIdx.x / per);
   if (sh.b < 0) return;                              // the same for the whole workgroup
   const int chunk = blockIdx.x % p.nchunk, hkv = blockIdx.x % per / p.nchunk, b = sh.b;
   const int nh = min(16, grp - 16 * chunk), h0 = hkv * grp + 16 * chunk;
@@ -190,6 +184,9 @@ __global__ __launch_bounds__(kPagedWaves * 64, WPE) void mala_paged_decode_kerne
     }
     if (scale2 == 0.f) scale2 = 1e-37f;
   }
+  // for the join: where the sequence's partials lie
+  if (sh.blk == 0 && blockIdx.x % per == 0 && threadIdx.x == 0 && p.nblk > p.B)
+    p.plan[b] = make_int2(sh.first, sh.blocks);
   const float thr2 = DENSE ? 0.f : p.log2tau - log2f((float)n);    // L = n
 
   // a tile's two groups: where they start, and how many of their rows are there
@@ -454,6 +451,7 @@ __global__ __launch_bounds__(kPagedWaves * 64, WPE) void mala_paged_decode_kerne
 #pragma unroll
   for (int i0 = 0; i0 < NDB * 64; i0 += W * 64) {
     const int i = i0 + threadIdx.x, c = i & 15, d = 16 * (i >> 6) + 4 * ((i & 63) >> 4);
+    if (i >= NDB * 64) break;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int u = 0; u < W; ++u)
@@ -478,79 +476,103 @@ __global__ __launch_bounds__(kPagedWaves * 64, WPE) void mala_paged_decode_kerne
   }
 }
 
-// Joins the partials of the sequences that have more than one block, a workgroup per query
-// head: lse = logsumexp_s lse_s, o = sum_s exp(lse_s - lse) o_s.  Latency-bound: the weights of
-// 256 parts at a time by the threads, the rows 16 bytes per thread and 256 / (D / 4) at once.
+// Joins the partials of the sequences that have more than one block: lse = logsumexp_s lse_s,
+// o = sum_s exp(lse_s - lse) o_s, a workgroup per query head.  LPR lanes read a partial row 16
+// bytes each, the workgroup's NG groups of LPR lanes take the parts in turn.  Latency-bound.
 constexpr int kJoinThreads = 256;
-template <int D, bool DENSE>
+template <int D>
 __global__ __launch_bounds__(kJoinThreads) void mala_paged_join_kernel(PagedDecParams p) {
-  constexpr int LPR = D / 4, NG = kJoinThreads / LPR, LD = D + kDecStride;
-  __shared__ float wts[kJoinThreads], red[kJoinThreads / 64];
+  constexpr int LPR = D / 4, NG = kJoinThreads / LPR, REC = D + kDecStride;
   __shared__ __attribute__((aligned(16))) f32x4 rows[kJoinThreads];
-  const int tid = threadIdx.x, lane = tid & 63;
+  __shared__ f32x2 state[NG];
+  __shared__ int counts[NG];
+  const int tid = threadIdx.x, grp = tid / LPR, cl = tid % LPR;
   const int b = blockIdx.x / p.Hq, h = blockIdx.x % p.Hq;
-  const Share sh = share_of<true, DENSE>(p, b);
-  if (sh.blocks <= 1) return;            // the decode kernel wrote the outputs
-  const float* pp = p.part + ((long)sh.first * p.Hq + h) * LD;
-  const long stride = (long)p.Hq * LD;
-  const int nb = sh.blocks, grp = tid / LPR, cl = tid % LPR;
-  float mx = kNegInf;
+  const int2 plan = p.plan[b];
+  const int nb = plan.y;
+  if (nb <= 1) return;                   // the decode kernel wrote the outputs
+  const long step = (long)p.Hq * REC;
+  const float* pp = p.part + (long)plan.x * step + (long)h * REC;
+  float m = kNegInf, z = 0.f;
+  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   int kept = 0;
-  for (int s = lane; s < nb; s += 64) {
-    mx = fmaxf(mx, pp[s * stride + D]);
-    kept += __float_as_int(pp[s * stride + D + 1]);
+  // LPR of the group's parts at a time: their lse by the lanes, their rows by all of them
+  for (int c0 = grp; c0 < nb; c0 += LPR * NG) {
+    const int s = c0 + cl * NG;
+    const f32x2 x = s < nb ? *reinterpret_cast<const f32x2*>(pp + s * step + D) : f32x2{kNegInf, 0.f};
+    kept += __float_as_int(x[1]);
+    float mx = x[0];
+#pragma unroll
+    for (int d = LPR / 2; d >= 1; d /= 2) mx = fmaxf(mx, __shfl_xor(mx, d));
+    const float m_new = fmaxf(m, mx), ref = m_new == kNegInf ? 0.f : m_new;
+    const float alpha = __expf(m - ref), f = __expf(x[0] - ref);   // 0 for a part without keys
+    m = m_new;
+    acc *= alpha;
+    z = z * alpha + f;                   // of this lane's parts
+    const int n = min(LPR, (nb - c0 + NG - 1) / NG);
+#pragma unroll 8
+    for (int j = 0; j < n; ++j)
+      acc += __shfl(f, j, LPR) * *reinterpret_cast<const f32x4*>(pp + (c0 + j * NG) * step + 4 * cl);
   }
 #pragma unroll
-  for (int d = 32; d >= 1; d /= 2) {
-    mx = fmaxf(mx, __shfl_xor(mx, d));
+  for (int d = LPR / 2; d >= 1; d /= 2) {
+    z += __shfl_xor(z, d);
     kept += __shfl_xor(kept, d);
   }
-  const float ref = mx == kNegInf ? 0.f : mx;
-  f32x4 acc = {0.f, 0.f, 0.f, 0.f};
-  float z = 0.f;
-  for (int s0 = 0; s0 < nb; s0 += kJoinThreads) {
-    if (s0) __syncthreads();             // the last weights have been read
-    const float f = s0 + tid < nb ? expf(pp[(s0 + tid) * stride + D] - ref) : 0.f;
-    wts[tid] = f;                        // 0 for a part without keys
-    z += f;
-    __syncthreads();
-    const int m = min(nb - s0, kJoinThreads);
-#pragma unroll 4
-    for (int s = grp; s < m; s += NG)
-      acc += wts[s] * *reinterpret_cast<const f32x4*>(pp + (s0 + s) * stride + 4 * cl);
+  rows[tid] = acc;                       // the groups' sums
+  if (cl == 0) {
+    state[grp] = f32x2{m, z};
+    counts[grp] = kept;
   }
-#pragma unroll
-  for (int d = 32; d >= 1; d /= 2) z += __shfl_xor(z, d);
-  if (lane == 0) red[tid / 64] = z;
-  rows[tid] = acc;
   __syncthreads();
-  if (tid >= LPR) return;
-  z = red[0] + red[1] + red[2] + red[3];
+  if (grp) return;
+  m = kNegInf;
 #pragma unroll
-  for (int u = 1; u < NG; ++u) acc += rows[u * LPR + tid];
-  const float inv = z != 0.f ? 1.f / z : 0.f;
+  for (int u = 0; u < NG; ++u) m = fmaxf(m, state[u][0]);
+  const float ref = m == kNegInf ? 0.f : m;
+  acc = f32x4{0.f, 0.f, 0.f, 0.f};
+  z = 0.f;
+  kept = 0;
+#pragma unroll
+  for (int u = 0; u < NG; ++u) {
+    const float f = __expf(state[u][0] - ref);
+    z += state[u][1] * f;
+    acc += rows[u * LPR + cl] * f;
+    kept += counts[u];
+  }
   const long bh = blockIdx.x;
-  store_out4(p.o, bh * D + 4 * tid, acc * inv, p.o_bf16);
-  if (tid == 0) {
-    p.lse[bh] = z != 0.f ? ref + logf(z) : kNegInf;
+  store_out4(p.o, bh * D + 4 * cl, acc * (z != 0.f ? 1.f / z : 0.f), p.o_bf16);
+  if (cl == 0) {
+    p.lse[bh] = z != 0.f ? ref + __logf(z) : kNegInf;
     if (p.head_tiles) p.head_tiles[bh] = kept;
   }
 }
 
 // ------------------------------------------------------------------ launches
-constexpr int kTargetGroups = TGT;     // workgroups that a large batch is shared out to
-constexpr int kMinTiles = MINT;          // tiles per wavefront at least
+// Workgroups that a large call is shared out to.  A CU gets its own share of HBM's rate, so it is
+// the CU with the most tiles that sets the time: equal workgroups should be as many as there are
+// CUs, or a multiple.  With tiles of 16 KB (K and V of 32 bf16 rows of 128) the four wavefronts
+// of one workgroup keep 64 KB on their way, which is enough; smaller tiles need more of them.
+// us per call with 256 / 336-512 / 608-1024 workgroups: 16 ragged 8192-token caches 52.6 / 63.5 /
+// 58.4, 32 x 2048 tokens 47.0 / 50.4 / 50.4, one of 32768 28.9 / 31 / 32; of 8 KB tiles, 64
+// ragged e4m3 caches 49.4 / 45.6 / 45.2; of 4 KB, 32 ragged ones (D = 64) 25.6 / 20.6 / 20.7.
+int target_groups(int D, bool e4m3) { return kNumCus * (128 / D) * (e4m3 ? 2 : 1); }
+
+// Sequences of up to 16 tiles stay in one workgroup, each wavefront taking up to 4: three more
+// tiles take a wavefront as long as the join of two blocks (3.5 us).
+constexpr int kSingleTiles = 4 * kPagedWaves;
 
 struct Plan {
   int target, unit, min_tpw, blocks;
 };
-Plan plan_of(int B, int Hq, int Hkv, int max_len, int split_tokens, bool dense) {
+Plan plan_of(int B, int Hq, int Hkv, int D, bool e4m3, int max_len, int split_tokens, bool dense) {
   const int nchunk = (Hq / Hkv + 15) / 16, T = (max_len + kDecBk - 1) / kDecBk;
   Plan x;
-  x.target = std::max(1, kTargetGroups / (Hkv * nchunk));
+  x.target = std::max(1, target_groups(D, e4m3) / (Hkv * nchunk));
   x.unit = dense ? 1 : split_tokens / kDecBk;
-  x.min_tpw = kMinTiles;
-  const long tpw = (x.min_tpw + x.unit - 1) / x.unit * (long)x.unit, most = (T + kPagedWaves * tpw - 1) / (kPagedWaves * tpw);
+  x.min_tpw = T <= kSingleTiles ? (T + kPagedWaves - 1) / kPagedWaves : 1;
+  const long tpw = (x.min_tpw + x.unit - 1) / x.unit * (long)x.unit;
+  const long most = (T + kPagedWaves * tpw - 1) / (kPagedWaves * tpw);
   x.blocks = (int)std::min<long>({(long)B + x.target, B * most, INT32_MAX});
   return x;
 }
@@ -562,9 +584,9 @@ void launch_t(const PagedDecParams& p, hipStream_t st) {
     hipLaunchKernelGGL((mala_paged_decode_kernel<D, E4M3, DENSE, false>), grid, wg, 0, st, p);
   else
     hipLaunchKernelGGL((mala_paged_decode_kernel<D, E4M3, DENSE, true>), grid, wg, 0, st, p);
-  if (p.nblk > p.B)
-    hipLaunchKernelGGL((mala_paged_join_kernel<D, DENSE>), dim3((unsigned)(p.B * p.Hq)),
-                       dim3(kJoinThreads), 0, st, p);
+  if (p.nblk <= p.B) return;
+  hipLaunchKernelGGL(mala_paged_join_kernel<D>, dim3((unsigned)(p.B * p.Hq)), dim3(kJoinThreads), 0,
+                     st, p);
 }
 template <int D>
 void launch_d(const PagedDecParams& p, hipStream_t st) {
@@ -577,14 +599,16 @@ void launch_d(const PagedDecParams& p, hipStream_t st) {
 
 }  // namespace
 
-int paged_decode_blocks(int B, int Hq, int Hkv, int max_len, int split_tokens) {
-  const Plan a = plan_of(B, Hq, Hkv, max_len, split_tokens, true);
-  const Plan b = plan_of(B, Hq, Hkv, max_len, split_tokens, false);
-  return std::max(a.blocks, b.blocks);
+int paged_decode_blocks(int B, int Hq, int Hkv, int D, int max_len, int split_tokens) {
+  int n = 0;
+  for (int i = 0; i < 4; ++i)
+    n = std::max(n, plan_of(B, Hq, Hkv, D, i & 1, max_len, split_tokens, i & 2).blocks);
+  return n;
 }
 
 hipError_t launch_paged_decode(PagedDecParams p, int D, int split_tokens, hipStream_t st) {
-  const Plan x = plan_of(p.B, p.Hq, p.c.Hkv, p.max_len, split_tokens, p.log2tau == kNegInf);
+  const Plan x = plan_of(p.B, p.Hq, p.c.Hkv, D, p.c.e4m3, p.max_len, split_tokens,
+                         p.log2tau == kNegInf);
   p.target = x.target;
   p.unit = x.unit;
   p.min_tpw = x.min_tpw;
