@@ -414,16 +414,18 @@ def _cache(cache):
     return cache
 
 
+_OPTIONAL = frozenset(("positions", "head_tiles", "counters"))
+
+
 def _args(device, *specs):
-    """(tensor, name, dtype, shape) of each argument (None: left out): the checks of _spec and
-    _on_device, in one quick look where everything is right.  A call of a few microseconds on
-    the GPU must not take longer here."""
+    """(tensor, name, dtype, shape) of each argument: the checks of _spec and _on_device, in one
+    quick look where everything is right.  A call of a few microseconds on the GPU must not
+    take longer here."""
     for t, name, dtype, shape in specs:
         if (type(t) is torch.Tensor and t.dtype is dtype and t.shape == shape
                 and t.get_device() == device and t.is_contiguous()):
             continue
-        if t is not None:
-            _spec(t, name, dtype, shape)
+        if _spec(t, name, dtype, shape, name in _OPTIONAL) is not None:
             if not t.is_cuda:
                 raise TypeError("%s must be a CUDA (HIP) tensor" % name)
             if t.get_device() != device:
@@ -436,10 +438,10 @@ def _device(t, name):
     return t.get_device()
 
 
-def _required(**named):
-    for name, t in named.items():
-        if t is None:
-            raise TypeError("%s is required" % name)
+def _shape(t, name, ndim):
+    """_dims for a tensor that is most likely right."""
+    shape = t.shape if type(t) is torch.Tensor else ()
+    return shape if len(shape) == ndim else _dims(t, name, ndim)
 
 
 def _launch(device, stream, call, *args):
@@ -457,14 +459,12 @@ def _launch(device, stream, call, *args):
 
 def mala_paged_update(lens, new_lens, block_table, free_ring, free_state, lens_out, cu_seqlens,
                       slots, positions, free_state_out, page_size, num_pages, stream=None):
-    R, W = _dims(block_table, "block_table", 2)
-    (C,) = _dims(free_ring, "free_ring", 1)
-    (fs,) = _dims(free_state, "free_state", 1)
-    (T,) = _dims(slots, "slots", 1)
+    R, W = _shape(block_table, "block_table", 2)
+    (C,) = _shape(free_ring, "free_ring", 1)
+    (fs,) = _shape(free_state, "free_state", 1)
+    (T,) = _shape(slots, "slots", 1)
     if fs < 2:
         raise ValueError("free_state needs two entries (head, count)")
-    _required(lens=lens, new_lens=new_lens, lens_out=lens_out, cu_seqlens=cu_seqlens,
-              free_state_out=free_state_out)
     dev, i32 = _device(block_table, "block_table"), torch.int32
     _args(dev, (block_table, "block_table", i32, (R, W)), (lens, "lens", i32, (R,)),
           (new_lens, "new_lens", i32, (R,)), (free_ring, "free_ring", i32, (C,)),
@@ -481,8 +481,8 @@ def mala_paged_write(k_new, v_new, slots, cache, stream=None):
     """k_new, v_new: bf16 [Hkv, T, D] with the same strides, rows of D contiguous (e.g. the
     transposed slices of a [T, 2, Hkv, D] projection); slots: int32 [T]."""
     c = _cache(cache)
-    Hkv, T, D = _dims(k_new, "k_new", 3)
-    _dims(v_new, "v_new", 3)
+    Hkv, T, D = _shape(k_new, "k_new", 3)
+    _shape(v_new, "v_new", 3)
     if k_new.dtype != torch.bfloat16 or v_new.dtype != torch.bfloat16:
         raise TypeError("k_new and v_new must have dtype %s, got %s and %s"
                         % (torch.bfloat16, k_new.dtype, v_new.dtype))
@@ -495,7 +495,6 @@ def mala_paged_write(k_new, v_new, slots, cache, stream=None):
         raise ValueError("the rows of k_new must be contiguous")
     if k_new.get_device() != c.device or v_new.get_device() != c.device:
         raise TypeError("k_new and v_new must be CUDA (HIP) tensors on the device of the cache")
-    _required(slots=slots)
     _args(c.device, (slots, "slots", torch.int32, (T,)))
     _launch(c.device, stream, (_lib or load_library()).mala_paged_write, k_new.data_ptr(),
             v_new.data_ptr(), st[1] if T > 1 else D, st[0] if Hkv > 1 else D, slots.data_ptr(),
@@ -504,9 +503,8 @@ def mala_paged_write(k_new, v_new, slots, cache, stream=None):
 
 def mala_paged_read(cache, block_table, cu_seqlens, max_seqlen, k, v, stream=None):
     c = _cache(cache)
-    S, W = _dims(block_table, "block_table", 2)
-    total = _dims(k, "k", 3)[1]
-    _required(cu_seqlens=cu_seqlens, v=v)
+    S, W = _shape(block_table, "block_table", 2)
+    total = _shape(k, "k", 3)[1]
     shape = (c.Hkv, total, c.D)
     _args(c.device, (block_table, "block_table", torch.int32, (S, W)),
           (cu_seqlens, "cu_seqlens", torch.int32, (S + 1,)), (k, "k", torch.bfloat16, shape),
@@ -524,10 +522,9 @@ def mala_paged_decode_workspace_size(B, Hq, Hkv, D, max_len, split_tokens):
 def mala_paged_decode(q, cache, block_table, cache_lens, max_len, o, lse, head_tiles, counters,
                       split_tokens, workspace, scale, tau, stream=None):
     c = _cache(cache)
-    B, Hq, D = _dims(q, "q", 3)
-    W = _dims(block_table, "block_table", 2)[1]
-    _required(cache_lens=cache_lens, o=o, lse=lse)
-    bf16 = o.dtype is torch.bfloat16
+    B, Hq, D = _shape(q, "q", 3)
+    W = _shape(block_table, "block_table", 2)[1]
+    bf16 = isinstance(o, torch.Tensor) and o.dtype is torch.bfloat16
     _args(c.device, (q, "q", torch.bfloat16, (B, Hq, c.D)),
           (block_table, "block_table", torch.int32, (B, W)),
           (cache_lens, "cache_lens", torch.int32, (B,)),

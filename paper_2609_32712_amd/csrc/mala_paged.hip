@@ -9,6 +9,19 @@ namespace mala {
 
 namespace {
 
+typedef int i32x2 __attribute__((ext_vector_type(2)));
+
+// Data that a call moves once: past the caches' retention.  (e4m3 rows are read by the write
+// as two halves of 32 bytes per lane, which an ordinary load keeps close for the second.)
+template <class T>
+__device__ __forceinline__ T load_once(const void* p) {
+  return __builtin_nontemporal_load(reinterpret_cast<const T*>(p));
+}
+template <class T>
+__device__ __forceinline__ void store_once(void* p, T v) {
+  __builtin_nontemporal_store(v, reinterpret_cast<T*>(p));
+}
+
 // ------------------------------------------------------------------ page tables
 // One launch: every workgroup scans the lengths of all requests (they are few: R lengths are
 // 8 R bytes from the L2), so none waits for another, and then does its own share of the
@@ -18,7 +31,7 @@ namespace {
 // some back, and the ring's popped and pushed places are disjoint while free and used pages
 // together fit it.
 constexpr int kUpdThreads = 1024;
-constexpr int kUpdChunk = 2048;   // tokens (or pages given back) a workgroup takes at a time
+constexpr int kUpdChunk = 1024;   // tokens (or pages given back) a workgroup takes at a time
 
 struct Scan3 {
   int grow, need, back;
@@ -196,25 +209,23 @@ __device__ __forceinline__ int to_e4m3x4(float a, float b, float c, float d) {
   return __builtin_amdgcn_cvt_pk_fp8_f32(lim(c), lim(d), r, true);
 }
 
-// A thread moves 16 bytes of a row of the cache, of K and of V.  HBM-bound.
+// A thread moves 16 bytes of a row of the cache, of K and of V; a workgroup stays with a head.
+// HBM-bound.
 template <int D, bool E4M3>
 __global__ __launch_bounds__(256) void mala_paged_write_kernel(PagedWriteParams p) {
   constexpr int EPC = E4M3 ? 16 : 8;     // values per 16 bytes of the cache
-  constexpr int CPR = D / EPC;           // 16-byte chunks per row
-  const int Hkv = p.c.Hkv, P = p.c.page_size;
-  const long n = (long)p.T * Hkv * CPR, last = (long)p.c.num_pages * P;
-  for (long i = (long)blockIdx.x * 256 + threadIdx.x; i < n; i += (long)gridDim.x * 256) {
-    const int c = (int)(i % CPR);
-    const long th = i / CPR;
-    const long t = th / Hkv;
-    const int h = (int)(th - t * Hkv);
-    const int slot = p.slots[t];
-    if (slot < 0 || slot >= last) continue;
-    const int page = slot / P, row = slot - page * P;
+  constexpr int CPR = D / EPC;
+  const long i = (long)blockIdx.x * 256 + threadIdx.x, t = i / CPR;
+  const int c = (int)(i % CPR);
+  if (t >= p.T) return;
+  const int slot = p.slots[t];
+  const unsigned P = p.c.page_size;
+  if (slot < 0 || (unsigned)slot >= p.c.num_pages * P) return;
+  const unsigned page = slot / P, row = slot - page * P;
+  for (int h = blockIdx.y; h < p.c.Hkv; h += gridDim.y) {
     const long src = t * p.token_stride + h * p.head_stride + c * EPC * 2;
     const long dst = page * p.c.page_stride + h * p.c.head_stride + row * p.c.token_stride + c * 16;
     if constexpr (E4M3) {
-      const float ks = p.c.ks ? p.c.ks[h] : 1.f, vs = p.c.vs ? p.c.vs[h] : 1.f;
       const auto put = [&](char* pool, const char* in, float s) {
         i32x4 out;
 #pragma unroll
@@ -223,28 +234,27 @@ __global__ __launch_bounds__(256) void mala_paged_write_kernel(PagedWriteParams 
           out[2 * e] = to_e4m3x4((float)x[0] / s, (float)x[1] / s, (float)x[2] / s, (float)x[3] / s);
           out[2 * e + 1] = to_e4m3x4((float)x[4] / s, (float)x[5] / s, (float)x[6] / s, (float)x[7] / s);
         }
-        *reinterpret_cast<i32x4*>(pool + dst) = out;
+        store_once(pool + dst, out);
       };
-      put(p.c.k, p.k, ks);
-      put(p.c.v, p.v, vs);
+      put(p.c.k, p.k, p.c.ks ? p.c.ks[h] : 1.f);
+      put(p.c.v, p.v, p.c.vs ? p.c.vs[h] : 1.f);
     } else {
-      const i32x4 a = *reinterpret_cast<const i32x4*>(p.k + src);
-      const i32x4 b = *reinterpret_cast<const i32x4*>(p.v + src);
-      *reinterpret_cast<i32x4*>(p.c.k + dst) = a;
-      *reinterpret_cast<i32x4*>(p.c.v + dst) = b;
+      const i32x4 a = load_once<i32x4>(p.k + src), b = load_once<i32x4>(p.v + src);
+      store_once(p.c.k + dst, a);
+      store_once(p.c.v + dst, b);
     }
   }
 }
 
 // ------------------------------------------------------------------ pages to packed rows
 // A workgroup takes kReadRows consecutive packed rows (of every head).  HBM-bound.
-constexpr int kReadRows = 16;
+constexpr int kReadRows = 4;
 template <int D, bool E4M3>
 __global__ __launch_bounds__(256) void mala_paged_read_kernel(PagedReadParams p) {
-  constexpr int EPC = E4M3 ? 16 : 8;
-  constexpr int CPR = D / EPC;
+  constexpr int CPR = D / 8;             // pieces of 8 values per row
   __shared__ int s_seq;
-  const int tid = threadIdx.x, row0 = blockIdx.x * kReadRows, Hkv = p.c.Hkv, P = p.c.page_size;
+  const int tid = threadIdx.x, row0 = blockIdx.x * kReadRows, Hkv = p.c.Hkv;
+  const unsigned P = p.c.page_size;
   if (tid == 0) s_seq = 0;
   __syncthreads();
   int before = 0;                        // sequences that start at or before row0
@@ -252,48 +262,52 @@ __global__ __launch_bounds__(256) void mala_paged_read_kernel(PagedReadParams p)
   if (before) atomicAdd(&s_seq, before);
   __syncthreads();
   const int seq0 = max(s_seq - 1, 0);
-  const int n = kReadRows * Hkv * CPR;
-  for (int i = tid; i < n; i += 256) {
-    const int c = i % CPR, rh = i / CPR, row = row0 + rh % kReadRows, h = rh / kReadRows;
-    if (row >= p.total) continue;
-    int b = seq0;
-    while (b < p.S && p.cu[b + 1] <= row) ++b;
-    if (b >= p.S) continue;
-    const int pos = row - p.cu[b];
-    if (pos < 0 || pos >= p.max_len) continue;
-    const int page = pos / P, off = pos - page * P;
-    const int number = p.table[(long)b * p.W + page];
-    const long src = (long)number * p.c.page_stride + h * p.c.head_stride + off * p.c.token_stride + c * 16;
-    const bool there = (unsigned)number < (unsigned)p.c.num_pages;
-    i32x4 a = {0, 0, 0, 0}, v = a;
-    if (there) {
-      a = *reinterpret_cast<const i32x4*>(p.c.k + src);
-      v = *reinterpret_cast<const i32x4*>(p.c.v + src);
-    }
-    const long dst = (((long)h * p.total + row) * D + c * EPC) * 2;
+  // a thread keeps its piece of the row and its row, and goes on by heads
+  constexpr int HEADS = 256 / (CPR * kReadRows);   // heads at a time
+  const int c = tid % CPR, row = row0 + tid / CPR % kReadRows;
+  int b = seq0;
+  while (b < p.S && p.cu[b + 1] <= row) ++b;
+  if (b >= p.S || row >= p.total) return;
+  const int pos = row - p.cu[b];
+  if (pos < 0 || pos >= p.max_len) return;
+  const unsigned page = pos / P, off = pos - page * P;
+  const int number = p.table[(long)b * p.W + page];
+  const bool there = (unsigned)number < (unsigned)p.c.num_pages;
+  const long at = there ? (long)number * p.c.page_stride + off * p.c.token_stride : 0;
+#pragma unroll 4
+  for (int h = tid / (CPR * kReadRows); h < Hkv; h += HEADS) {
+    const long dst = (((long)h * p.total + row) * D + c * 8) * 2;
     if constexpr (E4M3) {
-      const float ks = p.c.ks ? p.c.ks[h] : 1.f, vs = p.c.vs ? p.c.vs[h] : 1.f;
-      const auto put = [&](char* out, const i32x4& x, float s) {
+      const long src = at + h * p.c.head_stride + c * 8;
+      i32x2 a = {0, 0}, v = a;
+      if (there) {
+        a = load_once<i32x2>(p.c.k + src);
+        v = load_once<i32x2>(p.c.v + src);
+      }
+      const auto put = [&](char* out, const i32x2& x, float s) {
+        bf16x8 y;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-          bf16x8 y;
-#pragma unroll
-          for (int j = 0; j < 2; ++j) {
-            const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(x[2 * e + j], false);
-            const f32x2 hi = __builtin_amdgcn_cvt_pk_f32_fp8(x[2 * e + j], true);
-            y[4 * j] = (bf16)(lo[0] * s);
-            y[4 * j + 1] = (bf16)(lo[1] * s);
-            y[4 * j + 2] = (bf16)(hi[0] * s);
-            y[4 * j + 3] = (bf16)(hi[1] * s);
-          }
-          *reinterpret_cast<bf16x8*>(out + dst + 16 * e) = y;
+        for (int j = 0; j < 2; ++j) {
+          const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(x[j], false);
+          const f32x2 hi = __builtin_amdgcn_cvt_pk_f32_fp8(x[j], true);
+          y[4 * j] = (bf16)(lo[0] * s);
+          y[4 * j + 1] = (bf16)(lo[1] * s);
+          y[4 * j + 2] = (bf16)(hi[0] * s);
+          y[4 * j + 3] = (bf16)(hi[1] * s);
         }
+        store_once(out + dst, __builtin_bit_cast(i32x4, y));
       };
-      put(p.k, a, ks);
-      put(p.v, v, vs);
+      put(p.k, a, p.c.ks ? p.c.ks[h] : 1.f);
+      put(p.v, v, p.c.vs ? p.c.vs[h] : 1.f);
     } else {
-      *reinterpret_cast<i32x4*>(p.k + dst) = a;
-      *reinterpret_cast<i32x4*>(p.v + dst) = v;
+      const long src = at + h * p.c.head_stride + c * 16;
+      i32x4 a = {0, 0, 0, 0}, v = a;
+      if (there) {
+        a = load_once<i32x4>(p.c.k + src);
+        v = load_once<i32x4>(p.c.v + src);
+      }
+      store_once(p.k + dst, a);
+      store_once(p.v + dst, v);
     }
   }
 }
@@ -309,9 +323,9 @@ hipError_t launch_paged_update(const PagedUpdateParams& p, hipStream_t st) {
 
 template <int D, bool E4M3>
 static void launch_write_t(const PagedWriteParams& p, hipStream_t st) {
-  const long n = (long)p.T * p.c.Hkv * (D / (E4M3 ? 16 : 8)), blocks = (n + 255) / 256;
-  const unsigned grid = (unsigned)(blocks < (1 << 20) ? blocks : (1 << 20));
-  hipLaunchKernelGGL((mala_paged_write_kernel<D, E4M3>), dim3(grid), dim3(256), 0, st, p);
+  const long n = (long)p.T * (D / (E4M3 ? 16 : 8));
+  const dim3 grid((unsigned)((n + 255) / 256), (unsigned)std::min(p.c.Hkv, 65535));
+  hipLaunchKernelGGL((mala_paged_write_kernel<D, E4M3>), grid, dim3(256), 0, st, p);
 }
 
 hipError_t launch_paged_write(const PagedWriteParams& p, int D, hipStream_t st) {
