@@ -448,7 +448,7 @@ def _launch(device, stream, call, *args):
     """call(*args, stream) with the tensors' device current, on the given stream or on that
     device's current one."""
     s = torch._C._cuda_getCurrentRawStream(device) if stream is None else stream.cuda_stream
-    if device == torch.cuda.current_device():
+    if device == torch._C._cuda_getDevice():
         status = call(*args, s)
     else:
         with torch.cuda.device(device):

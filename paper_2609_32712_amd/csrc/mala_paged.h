@@ -77,6 +77,17 @@ struct PagedDecParams {
 // Blocks of all sequences at most (their partials are the workspace).
 int paged_decode_blocks(int B, int Hq, int Hkv, int D, int max_len, int split_tokens);
 
+// Inclusive sum over the wavefront's lanes.
+__device__ __forceinline__ int wave_scan(int x) {
+  x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);   // row_shr:1
+  x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);   // row_shr:2
+  x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);   // row_shr:4
+  x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);   // row_shr:8
+  x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // row_bcast:15 to rows 1, 3
+  x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // row_bcast:31 to rows 2, 3
+  return x;
+}
+
 hipError_t launch_paged_update(const PagedUpdateParams& p, hipStream_t st);
 hipError_t launch_paged_write(const PagedWriteParams& p, int D, hipStream_t st);
 hipError_t launch_paged_read(const PagedReadParams& p, int D, hipStream_t st);
