@@ -3,7 +3,7 @@
 //
 // A wavefront takes a run of tiles (32 keys) of one (sequence, KV head, chunk of up to 16
 // query heads of its group), from its last tile down: S^T = K Q^T and O^T += V^T P^T by
-// 16x16x32 MFMAs, K and V through the wavefront's own LDS slot.  The kPagedWaves wavefronts of
+// 16x16x32 MFMAs, K and V through the wavefront's own LDS slot.  The W wavefronts of
 // a workgroup take neighbouring runs and join their (m, l, O) in LDS; a sequence longer than a
 // workgroup's share leaves partials that a second launch joins.
 //
@@ -25,27 +25,31 @@ namespace {
 // in units of a whole split where tau > 0 (a unit of 1 where every tile is retained anyway).
 // The grid is the bound of what that can come to: with target blocks per KV head and chunk,
 // sum_b ceil(T_b / (W tpw)) <= target + B.
-constexpr int kPagedWaves = 4;         // wavefronts of a workgroup (W)
+// How a block of tiles is worked on: kDense (tau = 0) and kChain, a run of tiles per wavefront
+// (kChain: of whole splits, tested one after the other); kTeam, whole splits by all
+// wavefronts, a tile each at a time.
+enum { kDense = 0, kChain = 1, kTeam = 2 };
+constexpr int kPagedWaves = 4;           // wavefronts of a workgroup
+
 struct Share {
   int b, blk;        // sequence, block of it
   int blocks;        // blocks of the sequence
   int first;         // number of its first block among all sequences' (where partials lie)
-  int tpw;           // tiles per wavefront in this sequence
+  int tpw;           // tiles per wavefront (kTeam: per block) in this sequence
   int n;             // its length
 };
 
 __device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
 // The share of block number `at` among all sequences' blocks; b = -1 past the last one.
-// UNIT1: units of one tile (tau = 0).
-template <bool UNIT1>
+template <int MODE>
 __device__ __forceinline__ Share share_of(const PagedDecParams& p, int at) {
-  constexpr int W = kPagedWaves;
+  constexpr int W = MODE == kTeam ? 1 : kPagedWaves;   // runs per block
   const int lane = threadIdx.x & 63;
   const auto tiles = [&](int b) {
     return b < p.B ? (min(max(p.lens[b], 0), p.max_len) + kDecBk - 1) / kDecBk : 0;
   };
-  const auto in_units = [&](unsigned x) { return UNIT1 ? x : (x + p.unit - 1) / p.unit * p.unit; };
+  const auto in_units = [&](unsigned x) { return MODE == kDense ? x : (x + p.unit - 1) / p.unit * p.unit; };
   const int t0 = tiles(lane);          // of the first 64 sequences
   unsigned total = 0;
   for (int b0 = 0; b0 < p.B; b0 += 64)
@@ -103,9 +107,10 @@ __device__ __forceinline__ float rows_sum(float x) {
   return halves_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
 
-template <int D, bool E4M3, bool DENSE, bool F32>
+template <int D, bool E4M3, int MODE, bool F32>
 __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(PagedDecParams p) {
   constexpr int W = kPagedWaves;
+  constexpr bool DENSE = MODE == kDense, TEAM = MODE == kTeam;
   constexpr int KS = D / 32;             // k-steps of 32 over head_dim
   constexpr int NDB = D / 16;            // 16-row blocks of O^T
   constexpr int LD = D + 8;
@@ -117,16 +122,17 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
   __shared__ __attribute__((aligned(16))) bf16 slot[W][kDecBk * LD];
   __shared__ float refs[W][16], sums[W][16];
   __shared__ int counts[W][16];
+  __shared__ f32x2 tests[TEAM ? 2 : 1][W][16];       // kTeam: a round's maxima and sums
 
   const int lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int Hkv = p.c.Hkv, grp = p.Hq / Hkv, per = Hkv * p.nchunk;
-  const Share sh = share_of<DENSE>(p, blockIdx.x / per);
+  const Share sh = share_of<MODE>(p, blockIdx.x / per);
   if (sh.b < 0) return;                              // the same for the whole workgroup
   const int chunk = blockIdx.x % p.nchunk, hkv = blockIdx.x % per / p.nchunk, b = sh.b;
   const int nh = min(16, grp - 16 * chunk), h0 = hkv * grp + 16 * chunk;
   const int n = sh.n, T = (n + kDecBk - 1) / kDecBk;
-  const int t_lo = min(T, (sh.blk * W + w) * sh.tpw), t_hi = min(T, t_lo + sh.tpw);
+  const int t_lo = min(T, (TEAM ? sh.blk : sh.blk * W + w) * sh.tpw), t_hi = min(T, t_lo + sh.tpw);
   const bool head_valid = col < nh;
   const uint32_t ts = (uint32_t)p.c.token_stride;
 
@@ -184,10 +190,19 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
     int rows0, rows1;
   };
   int in = 0;                            // lane of the next tile's upper group
-  const auto next_tile = [&](int t) {
+  // tile t, the one below the last asked for, of 32 that end at or above t_end (kTeam: any below
+  // the last)
+  int top = t_hi - 1;                    // tile of lane 0
+  const auto next_tile = [&](int t, int t_end) {
     Place x = {0, 0, 0, 0};
-    if (t < t_lo) return x;
-    if (in == 64) {
+    if (t < t_end) return x;
+    if constexpr (TEAM) {
+      if (top - t >= 32) {
+        find_groups(2 * t + 1);
+        top = t;
+      }
+      in = 2 * (top - t);
+    } else if (in == 64) {
       find_groups(2 * t + 1);
       in = 0;
     }
@@ -301,8 +316,9 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
   int cnt = 0;
   unsigned legal = 0, vfetch = 0, vloads = 0;
   unsigned long long hsum = 0;
+  int split_lo = TEAM ? max(t_hi - 1, 0) / p.unit * p.unit : 0;   // first tile of the split
   Tile kr, vr;
-  Place at = next_tile(t_hi - 1);
+  Place at = next_tile(TEAM ? t_hi - 1 - w : t_hi - 1, TEAM ? split_lo : t_lo);
   load_tile(p.c.k, at, true, kr);
   load_tile(p.c.v, at, true, vr);
 
@@ -310,7 +326,7 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
     // every tile counts: K and V of the next one load while a tile is worked on.  (Columns
     // without a head have zero queries; what they hold is never stored.)
     for (int t = t_hi - 1; t >= t_lo; --t) {
-      const Place next = next_tile(t - 1);
+      const Place next = next_tile(t - 1, t_lo);
       to_lds(kr);
       load_tile(p.c.k, next, true, kr);
       float s[8];
@@ -330,6 +346,69 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
     }
     cnt = legal;
     vfetch = vloads = legal;
+  } else if constexpr (TEAM) {
+    // What bounds a call of few splits is the chain of a split's tiles.  Here the wavefronts score
+    // W tiles at once and publish each tile's maximum and sum per head (against that maximum);
+    // behind a barrier every wavefront takes the W tests in order, carrying the split's (md, ld),
+    // and adds its tile's values if its own was retained.  K and V of the next round load
+    // meanwhile; V is fetched for every tile.
+    float md = kNegInf, ld = 0.f;
+    for (int t0 = t_hi - 1, round = 0; t0 >= t_lo; ++round) {
+      int t_next = t0 - W, lo_next = split_lo;
+      if (t_next < split_lo) {               // the split below
+        t_next = split_lo - 1;
+        lo_next = split_lo - p.unit;
+      }
+      const Place next = next_tile(t_next - w, max(lo_next, t_lo));
+      to_lds(kr);
+      load_tile(p.c.k, next, true, kr);
+      float s[8];
+      const float mt = scores(at, s), own = mt == kNegInf ? 0.f : mt;
+#pragma unroll
+      for (int r = 0; r < 8; ++r) s[r] = fast_exp2(__builtin_fmaf(s[r], scale2, -own));
+      const float ps = ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
+      const float all = rows_sum(ps);
+      const bool here = at.rows0 + at.rows1 > 0;
+      if (g == 0) tests[round & 1][w][col] = f32x2{mt, here ? all : -1.f};
+      to_lds(vr);
+      load_tile(p.c.v, next, true, vr);
+      __syncthreads();
+      bool mine = false;
+#pragma unroll
+      for (int u = 0; u < W; ++u) {
+        const f32x2 x = tests[round & 1][u][col];     // (a sum below 0: no key of the tile is there)
+        const bool demand =
+            head_valid && !(x[1] < 0.f) && (ld == 0.f || x[0] - (md + fast_log2(ld)) >= thr2);
+        if (u == w) mine = demand;
+        if (demand) {
+          const float d_new = fmaxf(md, x[0]), ds = d_new == kNegInf ? 0.f : d_new;
+          ld = ld * fast_exp2(md - ds) + x[1] * fast_exp2((x[0] == kNegInf ? 0.f : x[0]) - ds);
+          md = d_new;
+        }
+      }
+      legal += here ? 1u : 0u;
+      if (wave_any(mine)) {
+        ++vloads;
+        raise(mine ? fmaxf(m, mt) : m);
+        const float shift = m == kNegInf ? 0.f : m, f = mine ? fast_exp2(own - shift) : 0.f;
+        if (mine) {
+          l += ps * f;
+          ++cnt;
+          if (p.counters) hsum += tile_hash(b, h0 + col, 0, t0 - w);
+        }
+#pragma unroll
+        for (int r = 0; r < 8; ++r) s[r] = mine ? s[r] * f : 0.f;
+        add_values(s);
+      }
+      if (lo_next != split_lo) {
+        md = kNegInf;
+        ld = 0.f;
+      }
+      t0 = t_next;
+      split_lo = lo_next;
+      at = next;
+    }
+    vfetch = legal;
   } else if (t_hi > t_lo) {
     // md, ld: reference and normaliser of the split being tested, over all its retained keys.
     // While tile t is worked on, K of t - 1 is in registers or on its way (its scores are taken
@@ -339,13 +418,13 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
     constexpr float kHintMargin = 1e-2f;
     float md = kNegInf, ld = 0.f, s[8], sn[8];
     int left = (t_hi - 1) % p.unit + 1;      // tiles of the split from t down
-    Place next = next_tile(t_hi - 2);
+    Place next = next_tile(t_hi - 2, t_lo);
     to_lds(kr);
     load_tile(p.c.k, next, true, kr);
     float mt = scores(at, s);
     vfetch = at.rows0 + at.rows1 > 0;
     for (int t = t_hi - 1; t >= t_lo; --t) {
-      const Place after = next_tile(t - 2);
+      const Place after = next_tile(t - 2, t_lo);
       to_lds(kr);                            // K of t - 1 (zeros past the run's first tile)
       load_tile(p.c.k, after, true, kr);
       const float mtn = scores(next, sn);
@@ -437,10 +516,10 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
     }
   }
   __syncthreads();
+  static_assert(NDB * 64 % (W * 64) == 0, "whole rounds of the workgroup's threads");
 #pragma unroll
   for (int i0 = 0; i0 < NDB * 64; i0 += W * 64) {
     const int i = i0 + threadIdx.x, c = i & 15, d = 16 * (i >> 6) + 4 * ((i & 63) >> 4);
-    if (i >= NDB * 64) break;
     f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int u = 0; u < W; ++u)
@@ -547,43 +626,54 @@ __global__ __launch_bounds__(kJoinThreads) void mala_paged_join_kernel(PagedDecP
 // ragged e4m3 caches 49.4 / 45.6 / 45.2; of 4 KB, 32 ragged ones (D = 64) 25.6 / 20.6 / 20.7.
 int target_groups(int D, bool e4m3) { return kNumCus * (128 / D) * (e4m3 ? 2 : 1); }
 
-// Sequences of up to 16 tiles stay in one workgroup, each wavefront taking up to 4: three more
-// tiles take a wavefront as long as the join of two blocks (3.5 us).
+// Caches of up to 16 tiles stay in one workgroup, without a join: two more tiles take a wavefront
+// 2.4 us (1.6 at D = 64), the join 3.9.  (With 8 wavefronts, caches of 40 tiles could do so too:
+// 8 x 1000 tokens 14.7 instead of 12.9 us, the CUs left free cost more than the join.)
 constexpr int kSingleTiles = 4 * kPagedWaves;
 
+// tau > 0: splits up to which the wavefronts of a workgroup share them.  us per call, a wavefront
+// per split / shared: one cache of 1000 tokens (64 splits of 128) 13.1 / 9.6, of 4096 (256) 14.2 /
+// 11.9, 4096 in splits of 256 18.9 / 12.9, 32768 in splits of 512 (512 of them) 32.0 / 31.0; from
+// 1024 splits on no gain, and a wavefront per split fetches only the V tiles it needs.
+constexpr long kTeamSplits = 512;
+
 struct Plan {
-  int target, unit, min_tpw, blocks;
+  int target, unit, min_tpw, blocks, mode;
 };
 Plan plan_of(int B, int Hq, int Hkv, int D, bool e4m3, int max_len, int split_tokens, bool dense) {
   const int nchunk = (Hq / Hkv + 15) / 16, T = (max_len + kDecBk - 1) / kDecBk;
   Plan x;
-  x.target = std::max(1, target_groups(D, e4m3) / (Hkv * nchunk));
   x.unit = dense ? 1 : split_tokens / kDecBk;
-  x.min_tpw = T <= kSingleTiles ? (T + kPagedWaves - 1) / kPagedWaves : 1;
+  const long splits = (long)B * Hkv * nchunk * ((T + x.unit - 1) / x.unit);
+  x.mode = dense ? kDense : x.unit > 1 && splits <= kTeamSplits ? kTeam : kChain;
+  const int runs = x.mode == kTeam ? 1 : kPagedWaves;      // per block
+  x.target = (int)std::max<long>(1, (x.mode == kTeam ? kTeamSplits : target_groups(D, e4m3)) / (Hkv * nchunk));
+  x.min_tpw = T <= kSingleTiles ? (T + runs - 1) / runs : 1;
   const long tpw = (x.min_tpw + x.unit - 1) / x.unit * (long)x.unit;
-  const long most = (T + kPagedWaves * tpw - 1) / (kPagedWaves * tpw);
+  const long most = (T + runs * tpw - 1) / (runs * tpw);
   x.blocks = (int)std::min<long>({(long)B + x.target, B * most, INT32_MAX});
   return x;
 }
 
-template <int D, bool E4M3, bool DENSE>
+template <int D, bool E4M3, int MODE>
 void launch_t(const PagedDecParams& p, hipStream_t st) {
   const dim3 grid((unsigned)(p.nblk * p.c.Hkv * p.nchunk)), wg(kPagedWaves * 64);
   if (p.o_bf16)
-    hipLaunchKernelGGL((mala_paged_decode_kernel<D, E4M3, DENSE, false>), grid, wg, 0, st, p);
+    hipLaunchKernelGGL((mala_paged_decode_kernel<D, E4M3, MODE, false>), grid, wg, 0, st, p);
   else
-    hipLaunchKernelGGL((mala_paged_decode_kernel<D, E4M3, DENSE, true>), grid, wg, 0, st, p);
-  if (p.nblk <= p.B) return;
-  hipLaunchKernelGGL(mala_paged_join_kernel<D>, dim3((unsigned)(p.B * p.Hq)), dim3(kJoinThreads), 0,
-                     st, p);
+    hipLaunchKernelGGL((mala_paged_decode_kernel<D, E4M3, MODE, true>), grid, wg, 0, st, p);
+  if (p.nblk > p.B)
+    hipLaunchKernelGGL(mala_paged_join_kernel<D>, dim3((unsigned)(p.B * p.Hq)), dim3(kJoinThreads), 0,
+                       st, p);
 }
-template <int D>
-void launch_d(const PagedDecParams& p, hipStream_t st) {
-  const bool dense = p.log2tau == kNegInf;
-  if (p.c.e4m3)
-    dense ? launch_t<D, true, true>(p, st) : launch_t<D, true, false>(p, st);
+template <int D, bool E4M3>
+void launch_e(const PagedDecParams& p, int mode, hipStream_t st) {
+  if (mode == kDense)
+    launch_t<D, E4M3, kDense>(p, st);
+  else if (mode == kTeam)
+    launch_t<D, E4M3, kTeam>(p, st);
   else
-    dense ? launch_t<D, false, true>(p, st) : launch_t<D, false, false>(p, st);
+    launch_t<D, E4M3, kChain>(p, st);
 }
 
 }  // namespace
@@ -603,7 +693,10 @@ hipError_t launch_paged_decode(PagedDecParams p, int D, int split_tokens, hipStr
   p.min_tpw = x.min_tpw;
   p.nblk = x.blocks;
   p.nchunk = (p.Hq / p.c.Hkv + 15) / 16;
-  D == 128 ? launch_d<128>(p, st) : launch_d<64>(p, st);
+  if (D == 128)
+    p.c.e4m3 ? launch_e<128, true>(p, x.mode, st) : launch_e<128, false>(p, x.mode, st);
+  else
+    p.c.e4m3 ? launch_e<64, true>(p, x.mode, st) : launch_e<64, false>(p, x.mode, st);
   return hipGetLastError();
 }
 

@@ -124,13 +124,20 @@ def test_decode_batches(B, n, D, e4m3):
     w.check(w.decode(split=128), w.plain())
 
 
+@pytest.mark.parametrize("many", [False, True])
 @pytest.mark.parametrize("tau", [1e-3, 0.1, 1.0, 5.0])
 @pytest.mark.parametrize("Hq,Hkv,D,P,e4m3,split", [
     (4, 2, 128, 16, False, 256), (8, 1, 64, 32, True, 64), (20, 1, 128, 48, False, 512),
     (3, 3, 64, 64, False, 32), (8, 2, 128, 16, True, 1024)])
-def test_decode_rule(Hq, Hkv, D, P, e4m3, split, tau):
+def test_decode_rule(Hq, Hkv, D, P, e4m3, split, tau, many):
+    # few splits (up to 512 by the longest cache) are shared by the wavefronts of a workgroup,
+    # of many each wavefront takes its own: the same batch several times over the same pages
     w = Batch(3, [1, 0, 33, 64, 500, 1023, 1600], Hq, Hkv, D, P, e4m3, needle=128 / D)
     want = w.plain(tau, split)
+    if many:
+        copies = 1 + 512 // (7 * Hkv * -(-Hq // Hkv // 16) * -(-1600 // split))
+        w.lens, w.table, w.q = w.lens * copies, np.tile(w.table, (copies, 1)), w.q.repeat(copies, 1, 1)
+        want = want * copies
     got = w.decode(tau, split)
     # a decision can differ where the test value lies within its rounding of tau: that of the
     # normaliser (a sum of at most 1600 terms) and of the scores
