@@ -277,6 +277,78 @@ def test_decode_scores_of_minus_infinity():
     w.check(got, want)
 
 
+@pytest.mark.parametrize("Hq,Hkv,D,e4m3,n,tau", [
+    (2, 1, 64, True, 140001, 0.0), (3, 1, 128, False, 40000, 0.0), (2, 1, 64, False, 70000, 1e-3),
+    (17, 1, 128, True, 9000, 1e-3)])
+def test_decode_many_blocks(Hq, Hkv, D, e4m3, n, tau):
+    # one long cache and few heads: as many blocks as the launch ever makes, and their join
+    w = Batch(12, [n, 3, 0], Hq, Hkv, D, 64, e4m3, needle=128 / D)
+    want = w.plain(tau, 256)
+    clear = [x[4] > (n + 100) * pu.U24 + 16 * pu.U24 * 30 for x in want]
+    assert sum(x.sum() for x in clear) >= 0.5 * Hq * 3
+    got = w.decode(tau, 256)
+    w.check(got, want, clear=clear)
+    tiles = got["head_tiles"].cpu().numpy()
+    for b, x in enumerate(want):
+        assert tiles[b][clear[b]].tolist() == x[2][clear[b]].tolist()
+
+
+@pytest.mark.parametrize("ks,vs", [([-0.5, 1.0], [0.75, -1.25]), ([0.0, 0.25], [0.0, 1.0])])
+@pytest.mark.parametrize("tau", [0.0, 0.1])
+def test_decode_scales_of_any_sign(ks, vs, tau):
+    w = Batch(13, [70, 300], 4, 2, 128, 16, True, ks=ks, vs=vs)
+    w.check(w.decode(tau, 64), w.plain(tau, 64))
+
+
+def test_decode_workspace_contents_do_not_matter():
+    # 0xFF bytes are NaN partials and negative block numbers
+    w = Batch(14, [3000, 100, 0, 2047], 8, 2, 128, 16, needle=1.0)
+    for tau in (0.0, 0.1):
+        n = mala.mala_paged_decode_workspace_size(4, 8, 2, 128, 3000, 128)
+        assert n > 0
+        want = w.decode(tau, 128)
+        for fill in (0xFF, 0x7F, 0):
+            ws = torch.full((n,), fill, dtype=torch.uint8, device="cuda")
+            got = w.decode(tau, 128, workspace=ws)
+            assert torch.equal(got["o"], want["o"]) and torch.equal(got["lse"], want["lse"])
+            assert torch.equal(got["head_tiles"], want["head_tiles"])
+
+
+def test_decode_graphs_that_share_a_workspace():
+    # two graphs over different caches and one workspace, replayed in turn with lengths that
+    # change between replays (so do the blocks of a sequence) and eager calls in between
+    ws = [Batch(15 + i, [3000, 500], 8, 2, 128, 16, needle=1.0) for i in range(2)]
+    need = mala.mala_paged_decode_workspace_size(2, 8, 2, 128, 3000, 128)
+    work = torch.empty(need, dtype=torch.uint8, device="cuda")
+    runs = []
+    for i, w in enumerate(ws):
+        r = dict(q=w.q.to(torch.bfloat16).cuda(), t=cuda(w.table), n=cuda([1, 1]), tau=0.1 * i,
+                 o=torch.empty((2, 8, 128), device="cuda"), lse=torch.empty((2, 8), device="cuda"))
+        call = lambda r=r, w=w, out=None: mala.mala_paged_decode(
+            r["q"], w.cache, r["t"], r["n"], 3000, *(out or (r["o"], r["lse"])), None, None, 128,
+            work, w.scale, r["tau"])
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            call()
+        torch.cuda.current_stream().wait_stream(side)
+        r["g"], r["call"] = torch.cuda.CUDAGraph(), call
+        with torch.cuda.graph(r["g"]):
+            call()
+        runs.append(r)
+    for lens in ([3000, 500], [64, 500], [1500, 0], [2999, 33], [0, 1], [3000, 500]):
+        for r in runs:
+            r["n"].copy_(cuda(lens))
+            out = torch.empty_like(r["o"]), torch.empty_like(r["lse"])
+            r["call"](out=out)
+            r["eager"] = out
+        for r in runs:
+            r["g"].replay()
+        torch.cuda.synchronize()
+        for r in runs:
+            assert torch.equal(r["o"], r["eager"][0]) and torch.equal(r["lse"], r["eager"][1])
+
+
 def test_decode_does_not_depend_on_the_batch():
     lens = [700, 33, 512, 1]
     w = Batch(11, lens, 8, 2, 128, 16, needle=1.0)
