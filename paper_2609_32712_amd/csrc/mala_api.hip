@@ -643,7 +643,7 @@ int mala_paged_decode(const void* q, const mala_paged_cache_t* cache, const int3
   p.log2tau = log2_tau(tau);
   const double groups =
       (double)Hq * mala::paged_decode_blocks(B, Hq, cache->Hkv, cache->D, max_len, split_tokens);
-  if (groups > INT32_MAX || (double)B * max_len / mala::kDecBk > INT32_MAX / 2)
+  if (groups > INT32_MAX - 256 || (double)B * max_len / mala::kDecBk > INT32_MAX / 2)
     return fail(MALA_ERR_UNSUPPORTED, "2^31 workgroups or 2^30 tiles, or more");
   hipStream_t s = (hipStream_t)stream;
   hipError_t e;

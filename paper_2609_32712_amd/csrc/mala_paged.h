@@ -68,8 +68,10 @@ struct PagedDecParams {
   unsigned long long* counters;
   int B, Hq, W, max_len;
   int unit;             // tiles per split (tau = 0: 1)
-  int target, min_tpw;  // blocks that the tiles are shared out to; tiles per wavefront at least
+  int target, ragged;   // blocks that the tiles are shared out to, and of sequences of unequal length
+  int min_tpw;          // tiles per wavefront at least
   int nblk;             // blocks of all sequences at most
+  int sorted;           // whether they are dealt in the order of their sizes
   int nchunk;           // ceil((Hq / Hkv) / 16)
   float scale2, log2tau;
 };
@@ -86,6 +88,17 @@ __device__ __forceinline__ int wave_scan(int x) {
   x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);   // row_bcast:15 to rows 1, 3
   x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);   // row_bcast:31 to rows 2, 3
   return x;
+}
+
+// Maximum over the wavefront's lanes of x >= 0.
+__device__ __forceinline__ int wave_max(int x) {
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false));
+  x = max(x, __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false));
+  return __builtin_amdgcn_readlane(x, 63);
 }
 
 hipError_t launch_paged_update(const PagedUpdateParams& p, hipStream_t st);

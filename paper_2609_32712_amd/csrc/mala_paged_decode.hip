@@ -52,30 +52,50 @@ __device__ __forceinline__ Share share_of(const PagedDecParams& p, int at) {
   const auto in_units = [&](unsigned x) { return MODE == kDense ? x : (x + p.unit - 1) / p.unit * p.unit; };
   const int t0 = tiles(lane);          // of the first 64 sequences
   unsigned total = 0;
-  for (int b0 = 0; b0 < p.B; b0 += 64)
-    total += __builtin_amdgcn_readlane(wave_scan(b0 ? tiles(b0 + lane) : t0), 63);
-  // (a floor plus one: at least the even share)
-  const unsigned even = total / (unsigned)(p.target * W) + 1;
-  const unsigned per_block = W * in_units(max(even, (unsigned)p.min_tpw));
-  Share s = {-1, 0, 1, 0, 0, 0};
-  int before = 0;
+  int longest = 0;
   for (int b0 = 0; b0 < p.B; b0 += 64) {
     const int t = b0 ? tiles(b0 + lane) : t0;
-    const int nb = b0 + lane < p.B ? max(1u, (t + per_block - 1) / per_block) : 0;
-    const int end = wave_scan(nb);
-    const int i = __popcll(__builtin_amdgcn_ballot_w64(before + end <= at));
-    if (i < min(64, p.B - b0)) {
+    total += __builtin_amdgcn_readlane(wave_scan(t), 63);
+    longest = max(longest, wave_max(t));
+  }
+  // the longest over 5 / 4 of the average: smaller blocks, which can be dealt more evenly
+  const bool ragged = (float)longest * p.B > 1.25f * total;
+  // (a floor plus one: at least the even share)
+  const unsigned even = total / (unsigned)((ragged ? p.ragged : p.target) * W) + 1;
+  const unsigned per_block = W * in_units(max(even, (unsigned)p.min_tpw));
+  Share s = {-1, 0, 1, 0, 0, 0};
+  int before = 0;                      // blocks of the sequences before
+  for (int b0 = 0; b0 < p.B; b0 += 64) {
+    const int t = b0 ? tiles(b0 + lane) : t0, here = min(64, p.B - b0);
+    const int nb = lane < here ? max(1u, (t + per_block - 1) / per_block) : 0;
+    const int end = wave_scan(nb), all = __builtin_amdgcn_readlane(end, 63);
+    if (at < before + all) {
+      // even runs within a sequence; its blocks take the places [from, from + nb) of these 64
+      // sequences' blocks, the longest runs first
+      const int tpw = in_units((t + nb * W - 1) / max(nb * W, 1));
+      int from = end - nb;
+      if (p.sorted && __builtin_amdgcn_ballot_w64(lane < here && tpw > 4)) {
+        // eight classes of run lengths, the longest class first
+        const int cls = min(7, (int)(tpw * 8u / (per_block / W + 1u)));
+        int base = 0;
+#pragma unroll
+        for (int c = 7; c >= 0; --c) {
+          const int e = wave_scan(cls == c ? nb : 0);
+          if (cls == c) from = base + e - nb;
+          base += __builtin_amdgcn_readlane(e, 63);
+        }
+      }
+      const int place = at - before;
+      const int i = __builtin_ctzll(__builtin_amdgcn_ballot_w64(from <= place && place < from + nb));
       s.b = b0 + i;
       s.blocks = __builtin_amdgcn_readlane(nb, i);
       s.first = before + __builtin_amdgcn_readlane(end, i) - s.blocks;
-      s.blk = at - s.first;
+      s.blk = place - __builtin_amdgcn_readlane(from, i);
+      s.tpw = __builtin_amdgcn_readlane(tpw, i);
       s.n = min(max(p.lens[s.b], 0), p.max_len);
-      // even runs within the sequence
-      const unsigned runs = s.blocks * W;
-      s.tpw = in_units((__builtin_amdgcn_readlane(t, i) + runs - 1) / runs);
       return s;
     }
-    before += __builtin_amdgcn_readlane(end, 63);
+    before += all;
   }
   return s;
 }
@@ -127,9 +147,30 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
   const int lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int Hkv = p.c.Hkv, grp = p.Hq / Hkv, per = Hkv * p.nchunk;
-  const Share sh = share_of<MODE>(p, blockIdx.x / per);
+  // Workgroups are dealt to the CUs in turn, a round of 256 at a time, and the share of HBM that
+  // a CU gets is its own: longest first, and every other round backwards, gives the CUs about
+  // as many tiles each.
+  const int round = blockIdx.x / kNumCus, spot = blockIdx.x % kNumCus;
+  const int item = round * kNumCus + (round % 2 ? kNumCus - 1 - spot : spot);
+  Share sh;
+  if (p.sorted) {
+    __shared__ Share plan;
+    if (w == 0) {
+      const Share x = share_of<MODE>(p, item / per);
+      if (lane == 0) plan = x;
+    }
+    __syncthreads();
+    sh.b = __builtin_amdgcn_readfirstlane(plan.b);
+    sh.blk = __builtin_amdgcn_readfirstlane(plan.blk);
+    sh.blocks = __builtin_amdgcn_readfirstlane(plan.blocks);
+    sh.first = __builtin_amdgcn_readfirstlane(plan.first);
+    sh.tpw = __builtin_amdgcn_readfirstlane(plan.tpw);
+    sh.n = __builtin_amdgcn_readfirstlane(plan.n);
+  } else {
+    sh = share_of<MODE>(p, item / per);
+  }
   if (sh.b < 0) return;                              // the same for the whole workgroup
-  const int chunk = blockIdx.x % p.nchunk, hkv = blockIdx.x % per / p.nchunk, b = sh.b;
+  const int chunk = item % p.nchunk, hkv = item % per / p.nchunk, b = sh.b;
   const int nh = min(16, grp - 16 * chunk), h0 = hkv * grp + 16 * chunk;
   const int n = sh.n, T = (n + kDecBk - 1) / kDecBk;
   const int t_lo = min(T, (TEAM ? sh.blk : sh.blk * W + w) * sh.tpw), t_hi = min(T, t_lo + sh.tpw);
@@ -180,7 +221,7 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
     if (scale2 == 0.f) scale2 = 1e-37f;
   }
   // for the join: where the sequence's partials lie
-  if (sh.blk == 0 && blockIdx.x % per == 0 && threadIdx.x == 0 && p.nblk > p.B)
+  if (sh.blk == 0 && item % per == 0 && threadIdx.x == 0 && p.nblk > p.B)
     p.plan[b] = make_int2(sh.first, sh.blocks);
   const float thr2 = DENSE ? 0.f : p.log2tau - log2f((float)n);    // L = n
 
@@ -626,6 +667,11 @@ __global__ __launch_bounds__(kJoinThreads) void mala_paged_join_kernel(PagedDecP
 // ragged e4m3 caches 49.4 / 45.6 / 45.2; of 4 KB, 32 ragged ones (D = 64) 25.6 / 20.6 / 20.7.
 int target_groups(int D, bool e4m3) { return kNumCus * (128 / D) * (e4m3 ? 2 : 1); }
 
+// And of sequences of unequal length (tau = 0), dealt by their sizes, twice as many: 16 ragged
+// 8192-token caches 57.3 / 52.1, 64 log-uniform ones of up to 32768 127.5 / 124.0, 128 of up to 2048
+// 92.3 / 91.2.  (With tau > 0 blocks are whole splits, and the next smaller ones a third too small.)
+constexpr int kRaggedGroups = 2 * kNumCus;
+
 // Caches of up to 16 tiles stay in one workgroup, without a join: two more tiles take a wavefront
 // 2.4 us (1.6 at D = 64), the join 3.9.  (With 8 wavefronts, caches of 40 tiles could do so too:
 // 8 x 1000 tokens 14.7 instead of 12.9 us, the CUs left free cost more than the join.)
@@ -638,7 +684,7 @@ constexpr int kSingleTiles = 4 * kPagedWaves;
 constexpr long kTeamSplits = 512;
 
 struct Plan {
-  int target, unit, min_tpw, blocks, mode;
+  int target, ragged, unit, min_tpw, blocks, mode;
 };
 Plan plan_of(int B, int Hq, int Hkv, int D, bool e4m3, int max_len, int split_tokens, bool dense) {
   const int nchunk = (Hq / Hkv + 15) / 16, T = (max_len + kDecBk - 1) / kDecBk;
@@ -648,16 +694,20 @@ Plan plan_of(int B, int Hq, int Hkv, int D, bool e4m3, int max_len, int split_to
   x.mode = dense ? kDense : x.unit > 1 && splits <= kTeamSplits ? kTeam : kChain;
   const int runs = x.mode == kTeam ? 1 : kPagedWaves;      // per block
   x.target = (int)std::max<long>(1, (x.mode == kTeam ? kTeamSplits : target_groups(D, e4m3)) / (Hkv * nchunk));
+  x.ragged = x.mode == kDense ? std::max(x.target, kRaggedGroups / (Hkv * nchunk)) : x.target;
   x.min_tpw = T <= kSingleTiles ? (T + runs - 1) / runs : 1;
   const long tpw = (x.min_tpw + x.unit - 1) / x.unit * (long)x.unit;
   const long most = (T + runs * tpw - 1) / (runs * tpw);
-  x.blocks = (int)std::min<long>({(long)B + x.target, B * most, INT32_MAX});
+  x.blocks = (int)std::min<long>({(long)B + x.ragged, B * most, INT32_MAX});
   return x;
 }
 
 template <int D, bool E4M3, int MODE>
 void launch_t(const PagedDecParams& p, hipStream_t st) {
-  const dim3 grid((unsigned)(p.nblk * p.c.Hkv * p.nchunk)), wg(kPagedWaves * 64);
+  // (whole rounds where there are several, for the order of the blocks)
+  unsigned n = (unsigned)(p.nblk * p.c.Hkv * p.nchunk);
+  if (n > (unsigned)kNumCus) n = (n + kNumCus - 1) / kNumCus * kNumCus;
+  const dim3 grid(n), wg(kPagedWaves * 64);
   if (p.o_bf16)
     hipLaunchKernelGGL((mala_paged_decode_kernel<D, E4M3, MODE, false>), grid, wg, 0, st, p);
   else
@@ -689,9 +739,11 @@ hipError_t launch_paged_decode(PagedDecParams p, int D, int split_tokens, hipStr
   const Plan x = plan_of(p.B, p.Hq, p.c.Hkv, D, p.c.e4m3, p.max_len, split_tokens,
                          p.log2tau == kNegInf);
   p.target = x.target;
+  p.ragged = x.ragged;
   p.unit = x.unit;
   p.min_tpw = x.min_tpw;
   p.nblk = x.blocks;
+  p.sorted = p.B > 1 && (long)p.nblk * p.c.Hkv * ((p.Hq / p.c.Hkv + 15) / 16) > kNumCus;
   p.nchunk = (p.Hq / p.c.Hkv + 15) / 16;
   if (D == 128)
     p.c.e4m3 ? launch_e<128, true>(p, x.mode, st) : launch_e<128, false>(p, x.mode, st);
