@@ -3,9 +3,14 @@
 //
 // A wavefront takes a run of tiles (32 keys) of one (sequence, KV head, chunk of up to 16
 // query heads of its group), from its last tile down: S^T = K Q^T and O^T += V^T P^T by
-// 16x16x32 MFMAs, K and V through the wavefront's own LDS slot.  The W wavefronts of
-// a workgroup take neighbouring runs and join their (m, l, O) in LDS; a sequence longer than a
-// workgroup's share leaves partials that a second launch joins.
+// 16x16x32 MFMAs, K and V through the wavefront's own LDS slot.  The wavefronts of a workgroup
+// take neighbouring runs and join their (m, l, O) in LDS; a sequence longer than a workgroup's
+// share leaves partials that a second launch joins.
+//
+// What bounds it (MI355X): large calls HBM, 6.1-6.6 TB/s of K and V on 1 GB and more (16 caches
+// of 131072 tokens, 8.6 GB: 1.30 ms); calls of 100-300 MB the same and about 10 us of launch, first
+// loads (lengths, then table, then K, ~2.5 us), the last workgroups and the join (3.9 us); small
+// ones those alone (one cache of 200 tokens 5.8 us, of 4096 tokens 8 + 3.9 us).
 //
 // A page's 16-row groups are contiguous up to the token stride, so a tile is two buffer
 // resources of 16 rows.  Rows at or past the length, and groups of a page whose table entry
@@ -20,14 +25,15 @@ namespace mala {
 namespace {
 
 // ------------------------------------------------------------------ who works on what
-// Only the device knows the lengths, so it shares out the work: the tiles of all sequences
-// are counted and every wavefront gets about as many, whatever the batch (`tiles_per_wave`),
-// in units of a whole split where tau > 0 (a unit of 1 where every tile is retained anyway).
-// The grid is the bound of what that can come to: with target blocks per KV head and chunk,
-// sum_b ceil(T_b / (W tpw)) <= target + B.
-// How a block of tiles is worked on: kDense (tau = 0) and kChain, a run of tiles per wavefront
-// (kChain: of whole splits, tested one after the other); kTeam, whole splits by all
-// wavefronts, a tile each at a time.
+// Only the device knows the lengths, so it shares out the work: every workgroup counts the tiles
+// of all sequences, takes blocks of about as many for every workgroup of the target, in units
+// of whole splits where tau > 0, and finds its own block (0.6 us for up to 64 sequences).  The
+// grid is the bound of what that can come to: a sequence of T_b tiles has max(1, ceil(T_b /
+// per_block)) blocks, and with per_block >= total / target they are at most target + B.
+//
+// How a block is worked on: kDense (tau = 0) and kChain, a run of tiles per wavefront (kChain: of
+// whole splits, tested one after the other); kTeam, whole splits by all wavefronts, a tile
+// each at a time.
 enum { kDense = 0, kChain = 1, kTeam = 2 };
 constexpr int kPagedWaves = 4;           // wavefronts of a workgroup
 
@@ -38,8 +44,6 @@ struct Share {
   int tpw;           // tiles per wavefront (kTeam: per block) in this sequence
   int n;             // its length
 };
-
-__device__ __forceinline__ int ceil_div(int a, int b) { return (a + b - 1) / b; }
 
 // The share of block number `at` among all sequences' blocks; b = -1 past the last one.
 template <int MODE>
@@ -231,9 +235,8 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
     int rows0, rows1;
   };
   int in = 0;                            // lane of the next tile's upper group
-  // tile t, the one below the last asked for, of 32 that end at or above t_end (kTeam: any below
-  // the last)
-  int top = t_hi - 1;                    // tile of lane 0
+  // where tile t is, the one below the last asked for (kTeam: any below it); nowhere below t_end
+  int top = t_hi - 1;                    // its lane 0 holds this tile (kTeam)
   const auto next_tile = [&](int t, int t_end) {
     Place x = {0, 0, 0, 0};
     if (t < t_end) return x;
@@ -529,6 +532,7 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
   float M = kNegInf, L = 0.f;
 #pragma unroll
   for (int u = 0; u < W; ++u) M = fmaxf(M, refs[u][col]);
+  const float top_m = M;
   if (M == kNegInf) M = 0.f;
 #pragma unroll
   for (int u = 0; u < W; ++u) L += sums[u][col] * fast_exp2(refs[u][col] - M);
@@ -543,17 +547,16 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
       *reinterpret_cast<f32x4*>(out + (db * 64 + lane) * 4) = acc[db] * f;
   }
   if (threadIdx.x < nh) {
-    const float lse = L != 0.f ? (M + fast_log2(L)) * kLn2 : kNegInf;
     int kept = 0;
 #pragma unroll
     for (int u = 0; u < W; ++u) kept += counts[u][col];
     if (sh.blocks == 1) {
       const long bh = (long)b * p.Hq + h0 + col;
-      p.lse[bh] = lse;
+      p.lse[bh] = L != 0.f ? (M + fast_log2(L)) * kLn2 : kNegInf;
       if (p.head_tiles) p.head_tiles[bh] = kept;
     } else {
-      *reinterpret_cast<f32x2*>(p.part + (part + col) * (D + kDecStride) + D) =
-          f32x2{lse, __int_as_float(kept)};
+      *reinterpret_cast<f32x4*>(p.part + (part + col) * (D + kDecStride) + D) =
+          f32x4{top_m, L, __int_as_float(kept), 0.f};
     }
   }
   __syncthreads();
@@ -585,9 +588,11 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
   }
 }
 
-// Joins the partials of the sequences that have more than one block: lse = logsumexp_s lse_s,
-// o = sum_s exp(lse_s - lse) o_s, a workgroup per query head.  LPR lanes read a partial row 16
-// bytes each, the workgroup's NG groups of LPR lanes take the parts in turn.  Latency-bound.
+// Joins the partials (O_s / l_s, m_s, l_s, count) of the sequences that have more than one block:
+// l = sum_s 2^(m_s - m) l_s, o = sum_s 2^(m_s - m) l_s (O_s / l_s) / l, a workgroup per query head.
+// LPR lanes read a partial row 16 bytes each, the workgroup's NG groups of LPR lanes take the
+// parts in turn.  Latency-bound: 3-4 us (where a part's sequence lies, then the states and
+// rows of its parts at once).
 constexpr int kJoinThreads = 256;
 template <int D>
 __global__ __launch_bounds__(kJoinThreads) void mala_paged_join_kernel(PagedDecParams p) {
@@ -605,16 +610,17 @@ __global__ __launch_bounds__(kJoinThreads) void mala_paged_join_kernel(PagedDecP
   float m = kNegInf, z = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   int kept = 0;
-  // LPR of the group's parts at a time: their lse by the lanes, their rows by all of them
+  // LPR of the group's parts at a time: their states by the lanes, their rows by all of them
   for (int c0 = grp; c0 < nb; c0 += LPR * NG) {
     const int s = c0 + cl * NG;
-    const f32x2 x = s < nb ? *reinterpret_cast<const f32x2*>(pp + s * step + D) : f32x2{kNegInf, 0.f};
-    kept += __float_as_int(x[1]);
+    const f32x4 x = s < nb ? *reinterpret_cast<const f32x4*>(pp + s * step + D)
+                           : f32x4{kNegInf, 0.f, 0.f, 0.f};
+    kept += __float_as_int(x[2]);
     float mx = x[0];
 #pragma unroll
     for (int d = LPR / 2; d >= 1; d /= 2) mx = fmaxf(mx, __shfl_xor(mx, d));
     const float m_new = fmaxf(m, mx), ref = m_new == kNegInf ? 0.f : m_new;
-    const float alpha = __expf(m - ref), f = __expf(x[0] - ref);   // 0 for a part without keys
+    const float alpha = fast_exp2(m - ref), f = x[1] * fast_exp2(x[0] - ref);   // 0: no keys
     m = m_new;
     acc *= alpha;
     z = z * alpha + f;                   // of this lane's parts
@@ -644,7 +650,7 @@ __global__ __launch_bounds__(kJoinThreads) void mala_paged_join_kernel(PagedDecP
   kept = 0;
 #pragma unroll
   for (int u = 0; u < NG; ++u) {
-    const float f = __expf(state[u][0] - ref);
+    const float f = fast_exp2(state[u][0] - ref);
     z += state[u][1] * f;
     acc += rows[u * LPR + cl] * f;
     kept += counts[u];
@@ -652,7 +658,7 @@ __global__ __launch_bounds__(kJoinThreads) void mala_paged_join_kernel(PagedDecP
   const long bh = blockIdx.x;
   store_out4(p.o, bh * D + 4 * cl, acc * (z != 0.f ? 1.f / z : 0.f), p.o_bf16);
   if (cl == 0) {
-    p.lse[bh] = z != 0.f ? ref + __logf(z) : kNegInf;
+    p.lse[bh] = z != 0.f ? (ref + fast_log2(z)) * kLn2 : kNegInf;
     if (p.head_tiles) p.head_tiles[bh] = kept;
   }
 }
