@@ -32,7 +32,7 @@ __device__ __forceinline__ void store_once(void* p, T v) {
 // Inputs and outputs never share an address: a request either takes pages or gives some
 // back, and the ring's popped and pushed places are disjoint while free and used pages
 // together fit it.  us per call: 64 decodes 2.9 (6.6 by token, scanned by shuffles), a mix of
-// 512 requests and 116000 tokens 6.2 (10.3; 9.5 with the scans by shuffles).
+// 512 requests and 232000 tokens 6.2 (10.3; 9.5 with the scans by shuffles).
 constexpr int kUpdFew = 4;        // tokens that a request's thread takes itself
 constexpr int kUpdChunk = 1024;   // tokens (or pages given back) a workgroup takes at a time
 

@@ -149,6 +149,13 @@ def test_decode_rule(Hq, Hkv, D, P, e4m3, split, tau, many):
     tiles = got["head_tiles"].cpu().numpy()
     for b, x in enumerate(want):
         assert tiles[b][clear[b]].tolist() == x[2][clear[b]].tolist()
+    # a bf16 output is another instance of the kernels, with the same decisions; and so without
+    # statistics
+    for stats in (True, False):
+        half = w.decode(tau, split, out_dtype=torch.bfloat16, stats=stats)
+        w.check(half, want, True, clear=clear)
+        assert torch.equal(half["lse"], got["lse"])
+    assert torch.equal(w.decode(tau, split, stats=False)["o"], got["o"])
     c = got["counters"].tolist()
     legal = sum(-(-n // 32) for n in w.lens) * Hq
     assert (c[mala.CNT_LEGAL], c[mala.CNT_RETAINED]) == (legal, int(tiles.sum()))
@@ -203,6 +210,27 @@ def test_decode_lengths_are_clamped(D):
     w.check(got, want, where=[0, 2])
     for b in (1, 3):
         assert (got["o"][b] == 0).all() and torch.isneginf(got["lse"][b]).all()
+
+
+def test_one_page_and_one_head_with_any_stride():
+    # the stride of an axis of one entry is never used, whatever it says
+    rng = np.random.default_rng(22)
+    k, v = (torch.zeros(16 * 64, dtype=torch.bfloat16, device="cuda").as_strided(
+        (1, 1, 16, 64), (3, 1, 64, 1)) for _ in range(2))
+    cache = mala.PagedCache(k, v)
+    new = pu.quarters(rng, (2, 13, 64)).to(torch.bfloat16).cuda()
+    new = new.as_strided((2, 1, 13, 64), (13 * 64, 5, 64, 1))
+    mala.mala_paged_write(new[0], new[1], cuda(np.arange(13)), cache)
+    assert torch.equal(k[0, 0, :13], new[0, 0]) and torch.equal(v[0, 0, :13], new[1, 0])
+    q = pu.quarters(rng, (1, 3, 64), 4)
+    got = mala.paged_decode(q.to(torch.bfloat16).cuda(), cache, cuda([[0]]), cuda([13]), 16, 0.125, 0.0)
+    o, lse, tiles, _, _ = pu.decode_seq(q[0].numpy(), new[0].double().cpu().numpy(),
+                                        new[1].double().cpu().numpy(), np.ones(13, bool), 0.125, 0.0,
+                                        64, 13)
+    to, tl = pu.decode_bounds(13, 0.125 * 2 * float(q.abs().sum(2).max()), 2.0, False)
+    assert np.abs(got["o"][0].double().cpu().numpy() - o).max() <= to
+    assert np.abs(got["lse"][0].double().cpu().numpy() - lse).max() <= tl
+    assert got["head_tiles"].tolist() == [[1, 1, 1]]
 
 
 def test_decode_shared_pages():
