@@ -687,6 +687,6 @@ def paged_decode(q, cache, block_table, cache_lens, max_len, scale, tau, split_t
 
 def default_split_tokens(B, Hkv, max_len, num_cus=256, waves_per_simd=2):
     """Tokens per split (a multiple of 32) that give about num_cus * 4 * waves_per_simd splits
-    over batch and KV heads, between 64 and 512."""
+    over batch and KV heads, between 128 (a tile for each wavefront of a workgroup) and 512."""
     tokens = -(-B * Hkv * max_len // (num_cus * 4 * waves_per_simd))
-    return int(max(64, min(512, -(-tokens // 32) * 32)))
+    return int(max(128, min(512, -(-tokens // 32) * 32)))

@@ -596,7 +596,7 @@ int mala_paged_read(const mala_paged_cache_t* cache, const int32_t* block_table,
 size_t mala_paged_decode_workspace_size(int B, int Hq, int Hkv, int D, int max_len,
                                         int split_tokens) {
   if (B <= 0 || Hq <= 0 || Hkv <= 0 || Hq % Hkv || (D != 64 && D != 128) || max_len <= 0 ||
-      split_tokens <= 0 || split_tokens % mala::kDecBk)
+      max_len > mala::kPagedMaxLen || split_tokens <= 0 || split_tokens % mala::kDecBk)
     return 0;
   const size_t n = mala::paged_decode_blocks(B, Hq, Hkv, D, max_len, split_tokens);
   if (n <= (size_t)B) return 0;
@@ -641,6 +641,7 @@ int mala_paged_decode(const void* q, const mala_paged_cache_t* cache, const int3
   p.B = B; p.Hq = Hq; p.W = max_pages; p.max_len = max_len;
   p.scale2 = scale * mala::kLog2e;
   p.log2tau = log2_tau(tau);
+  if (max_len > mala::kPagedMaxLen) return fail(MALA_ERR_UNSUPPORTED, "max_len %d", max_len);
   const double groups =
       (double)Hq * mala::paged_decode_blocks(B, Hq, cache->Hkv, cache->D, max_len, split_tokens);
   if (groups > INT32_MAX - 256 || (double)B * max_len / mala::kDecBk > INT32_MAX / 2)

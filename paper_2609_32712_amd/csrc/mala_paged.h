@@ -3,7 +3,7 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-#include <algorithm>
+#include "mala_paged_dispatch.h"
 
 namespace mala {
 
@@ -75,9 +75,6 @@ struct PagedDecParams {
   int nchunk;           // ceil((Hq / Hkv) / 16)
   float scale2, log2tau;
 };
-
-// Blocks of all sequences at most (their partials are the workspace).
-int paged_decode_blocks(int B, int Hq, int Hkv, int D, int max_len, int split_tokens);
 
 // Inclusive sum over the wavefront's lanes.
 __device__ __forceinline__ int wave_scan(int x) {

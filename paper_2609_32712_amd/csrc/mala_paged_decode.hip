@@ -30,13 +30,6 @@ namespace {
 // of whole splits where tau > 0, and finds its own block (0.6 us for up to 64 sequences).  The
 // grid is the bound of what that can come to: a sequence of T_b tiles has max(1, ceil(T_b /
 // per_block)) blocks, and with per_block >= total / target they are at most target + B.
-//
-// How a block is worked on: kDense (tau = 0) and kChain, a run of tiles per wavefront (kChain: of
-// whole splits, tested one after the other); kTeam, whole splits by all wavefronts, a tile
-// each at a time.
-enum { kDense = 0, kChain = 1, kTeam = 2 };
-constexpr int kPagedWaves = 4;           // wavefronts of a workgroup
-
 struct Share {
   int b, blk;        // sequence, block of it
   int blocks;        // blocks of the sequence
@@ -53,7 +46,7 @@ __device__ __forceinline__ Share share_of(const PagedDecParams& p, int at) {
   const auto tiles = [&](int b) {
     return b < p.B ? (min(max(p.lens[b], 0), p.max_len) + kDecBk - 1) / kDecBk : 0;
   };
-  const auto in_units = [&](unsigned x) { return MODE == kDense ? x : (x + p.unit - 1) / p.unit * p.unit; };
+  const unsigned unit = MODE == kDense ? 1 : p.unit;
   const int t0 = tiles(lane);          // of the first 64 sequences
   unsigned total = 0;
   int longest = 0;
@@ -62,21 +55,18 @@ __device__ __forceinline__ Share share_of(const PagedDecParams& p, int at) {
     total += __builtin_amdgcn_readlane(wave_scan(t), 63);
     longest = max(longest, wave_max(t));
   }
-  // the longest over 5 / 4 of the average: smaller blocks, which can be dealt more evenly
-  const bool ragged = (float)longest * p.B > 1.25f * total;
-  // (a floor plus one: at least the even share)
-  const unsigned even = total / (unsigned)((ragged ? p.ragged : p.target) * W) + 1;
-  const unsigned per_block = W * in_units(max(even, (unsigned)p.min_tpw));
+  const unsigned per_block =
+      paged_block_tiles(total, longest, p.B, p.target, p.ragged, p.min_tpw, unit, W);
   Share s = {-1, 0, 1, 0, 0, 0};
   int before = 0;                      // blocks of the sequences before
   for (int b0 = 0; b0 < p.B; b0 += 64) {
     const int t = b0 ? tiles(b0 + lane) : t0, here = min(64, p.B - b0);
-    const int nb = lane < here ? max(1u, (t + per_block - 1) / per_block) : 0;
+    const int nb = lane < here ? paged_blocks_of(t, per_block) : 0;
     const int end = wave_scan(nb), all = __builtin_amdgcn_readlane(end, 63);
     if (at < before + all) {
       // even runs within a sequence; its blocks take the places [from, from + nb) of these 64
       // sequences' blocks, the longest runs first
-      const int tpw = in_units((t + nb * W - 1) / max(nb * W, 1));
+      const int tpw = paged_run_tiles(t, max(nb, 1), unit, W);
       int from = end - nb;
       if (p.sorted && __builtin_amdgcn_ballot_w64(lane < here && tpw > 4)) {
         // eight classes of run lengths, the longest class first
@@ -664,50 +654,6 @@ __global__ __launch_bounds__(kJoinThreads) void mala_paged_join_kernel(PagedDecP
 }
 
 // ------------------------------------------------------------------ launches
-// Workgroups that a large call is shared out to.  A CU gets its own share of HBM's rate, so it is
-// the CU with the most tiles that sets the time: equal workgroups should be as many as there are
-// CUs, or a multiple.  With tiles of 16 KB (K and V of 32 bf16 rows of 128) the four wavefronts
-// of one workgroup keep 64 KB on their way, which is enough; smaller tiles need more of them.
-// us per call with 256 / 336-512 / 608-1024 workgroups: 16 ragged 8192-token caches 52.6 / 63.5 /
-// 58.4, 32 x 2048 tokens 47.0 / 50.4 / 50.4, one of 32768 28.9 / 31 / 32; of 8 KB tiles, 64
-// ragged e4m3 caches 49.4 / 45.6 / 45.2; of 4 KB, 32 ragged ones (D = 64) 25.6 / 20.6 / 20.7.
-int target_groups(int D, bool e4m3) { return kNumCus * (128 / D) * (e4m3 ? 2 : 1); }
-
-// And of sequences of unequal length (tau = 0), dealt by their sizes, twice as many: 16 ragged
-// 8192-token caches 57.3 / 52.1, 64 log-uniform ones of up to 32768 127.5 / 124.0, 128 of up to 2048
-// 92.3 / 91.2.  (With tau > 0 blocks are whole splits, and the next smaller ones a third too small.)
-constexpr int kRaggedGroups = 2 * kNumCus;
-
-// Caches of up to 16 tiles stay in one workgroup, without a join: two more tiles take a wavefront
-// 2.4 us (1.6 at D = 64), the join 3.9.  (With 8 wavefronts, caches of 40 tiles could do so too:
-// 8 x 1000 tokens 14.7 instead of 12.9 us, the CUs left free cost more than the join.)
-constexpr int kSingleTiles = 4 * kPagedWaves;
-
-// tau > 0: splits up to which the wavefronts of a workgroup share them.  us per call, a wavefront
-// per split / shared: one cache of 1000 tokens (64 splits of 128) 13.1 / 9.6, of 4096 (256) 14.2 /
-// 11.9, 4096 in splits of 256 18.9 / 12.9, 32768 in splits of 512 (512 of them) 32.0 / 31.0; from
-// 1024 splits on no gain, and a wavefront per split fetches only the V tiles it needs.
-constexpr long kTeamSplits = 512;
-
-struct Plan {
-  int target, ragged, unit, min_tpw, blocks, mode;
-};
-Plan plan_of(int B, int Hq, int Hkv, int D, bool e4m3, int max_len, int split_tokens, bool dense) {
-  const int nchunk = (Hq / Hkv + 15) / 16, T = (max_len + kDecBk - 1) / kDecBk;
-  Plan x;
-  x.unit = dense ? 1 : split_tokens / kDecBk;
-  const long splits = (long)B * Hkv * nchunk * ((T + x.unit - 1) / x.unit);
-  x.mode = dense ? kDense : x.unit > 1 && splits <= kTeamSplits ? kTeam : kChain;
-  const int runs = x.mode == kTeam ? 1 : kPagedWaves;      // per block
-  x.target = (int)std::max<long>(1, (x.mode == kTeam ? kTeamSplits : target_groups(D, e4m3)) / (Hkv * nchunk));
-  x.ragged = x.mode == kDense ? std::max(x.target, kRaggedGroups / (Hkv * nchunk)) : x.target;
-  x.min_tpw = T <= kSingleTiles ? (T + runs - 1) / runs : 1;
-  const long tpw = (x.min_tpw + x.unit - 1) / x.unit * (long)x.unit;
-  const long most = (T + runs * tpw - 1) / (runs * tpw);
-  x.blocks = (int)std::min<long>({(long)B + x.ragged, B * most, INT32_MAX});
-  return x;
-}
-
 template <int D, bool E4M3, int MODE>
 void launch_t(const PagedDecParams& p, hipStream_t st) {
   // (whole rounds where there are several, for the order of the blocks)
@@ -734,23 +680,16 @@ void launch_e(const PagedDecParams& p, int mode, hipStream_t st) {
 
 }  // namespace
 
-int paged_decode_blocks(int B, int Hq, int Hkv, int D, int max_len, int split_tokens) {
-  int n = 0;
-  for (int i = 0; i < 4; ++i)
-    n = std::max(n, plan_of(B, Hq, Hkv, D, i & 1, max_len, split_tokens, i & 2).blocks);
-  return n;
-}
-
 hipError_t launch_paged_decode(PagedDecParams p, int D, int split_tokens, hipStream_t st) {
-  const Plan x = plan_of(p.B, p.Hq, p.c.Hkv, D, p.c.e4m3, p.max_len, split_tokens,
-                         p.log2tau == kNegInf);
+  const PagedPlan x = paged_plan(p.B, p.Hq, p.c.Hkv, D, p.c.e4m3, p.max_len, split_tokens,
+                                 p.log2tau == kNegInf);
   p.target = x.target;
   p.ragged = x.ragged;
   p.unit = x.unit;
   p.min_tpw = x.min_tpw;
   p.nblk = x.blocks;
-  p.sorted = p.B > 1 && (long)p.nblk * p.c.Hkv * ((p.Hq / p.c.Hkv + 15) / 16) > kNumCus;
-  p.nchunk = (p.Hq / p.c.Hkv + 15) / 16;
+  p.nchunk = x.nchunk;
+  p.sorted = p.B > 1 && (long)p.nblk * p.c.Hkv * p.nchunk > kNumCus;
   if (D == 128)
     p.c.e4m3 ? launch_e<128, true>(p, x.mode, st) : launch_e<128, false>(p, x.mode, st);
   else

@@ -1,0 +1,112 @@
+// How a paged decode is shared out: the host's launch rules and the arithmetic that the
+// kernels share with them.  Plain C++ (the tests compile it for the CPU).
+#pragma once
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "mala_dispatch.h"
+
+#ifdef __HIP__
+#define MALA_HOST_DEVICE __host__ __device__
+#else
+#define MALA_HOST_DEVICE
+#endif
+
+namespace mala {
+
+constexpr int kPagedTile = 32;           // keys per decision tile
+constexpr int kPagedWaves = 4;           // wavefronts of a workgroup
+
+// How a block of tiles is worked on: kDense (tau = 0) and kChain, a run of tiles per wavefront
+// (kChain: of whole splits, tested one after the other); kTeam, whole splits by all
+// wavefronts, a tile each at a time.
+enum { kDense = 0, kChain = 1, kTeam = 2 };
+constexpr int paged_runs(int mode) { return mode == kTeam ? 1 : kPagedWaves; }   // per block
+
+// Tiles per block of a batch of B sequences, `total` tiles in all and `longest` in one, whole
+// units per run.  Where the longest is over 5 / 4 of the average, blocks are smaller: they can be
+// dealt more evenly.  (A floor plus one is at least the even share, so that at most target + B
+// blocks come of it.)
+MALA_HOST_DEVICE inline unsigned paged_block_tiles(unsigned total, int longest, int B, int target,
+                                                   int ragged, int min_tpw, unsigned unit, int runs) {
+  const int blocks = (float)longest * B > 1.25f * total ? ragged : target;
+  const unsigned even = total / ((unsigned)blocks * runs) + 1;
+  const unsigned tpw = even > (unsigned)min_tpw ? even : (unsigned)min_tpw;
+  return runs * (unit == 1 ? tpw : (tpw + unit - 1) / unit * unit);
+}
+// Blocks of a sequence of t tiles, and tiles per run of it: even runs, whole units.
+MALA_HOST_DEVICE inline int paged_blocks_of(int t, unsigned per_block) {
+  const int n = (int)((t + per_block - 1) / per_block);
+  return n > 1 ? n : 1;
+}
+MALA_HOST_DEVICE inline int paged_run_tiles(int t, int blocks, unsigned unit, int runs) {
+  const unsigned n = ((unsigned)t + blocks * runs - 1) / (unsigned)(blocks * runs);
+  return (int)(unit == 1 ? n : (n + unit - 1) / unit * unit);
+}
+
+// Workgroups that a large call is shared out to.  A CU gets its own share of HBM's rate, so it is
+// the CU with the most tiles that sets the time: equal workgroups should be as many as there are
+// CUs, or a multiple.  With tiles of 16 KB (K and V of 32 bf16 rows of 128) the four wavefronts
+// of one workgroup keep 64 KB on their way, which is enough; smaller tiles need more of them.
+// us per call with 256 / 336-512 / 608-1024 workgroups: 16 ragged 8192-token caches 52.6 / 63.5 /
+// 58.4, 32 x 2048 tokens 47.0 / 50.4 / 50.4, one of 32768 28.9 / 31 / 32; of 8 KB tiles, 64
+// ragged e4m3 caches 49.4 / 45.6 / 45.2; of 4 KB, 32 ragged ones (D = 64) 25.6 / 20.6 / 20.7.
+inline int paged_target_groups(int D, bool e4m3) { return kNumCus * (128 / D) * (e4m3 ? 2 : 1); }
+
+// And of sequences of unequal length (tau = 0), dealt by their sizes, twice as many: 16 ragged
+// 8192-token caches 57.3 / 52.1, 64 log-uniform ones of up to 32768 127.5 / 124.0, 128 of up to 2048
+// 92.3 / 91.2.  (With tau > 0 blocks are whole splits, and the next smaller ones a third too small.)
+constexpr int kRaggedGroups = 2 * kNumCus;
+
+// Caches of up to 16 tiles stay in one workgroup, without a join: two more tiles take a wavefront
+// 2.4 us (1.6 at D = 64), the join 3.9.  (With 8 wavefronts, caches of 40 tiles could do so too:
+// 8 x 1000 tokens 14.7 instead of 12.9 us, the CUs left free cost more than the join.)
+constexpr int kSingleTiles = 4 * kPagedWaves;
+
+// tau > 0: splits up to which the wavefronts of a workgroup share them.  us per call, a wavefront
+// per split / shared: one cache of 1000 tokens (64 splits of 128) 13.1 / 9.6, of 4096 (256) 14.2 /
+// 11.9, 4096 in splits of 256 18.9 / 12.9, 32768 in splits of 512 (512 of them) 32.0 / 31.0; from
+// 1024 splits on no gain, and a wavefront per split fetches only the V tiles it needs.
+constexpr long kTeamSplits = 512;
+
+struct PagedPlan {
+  int target, ragged;   // blocks per KV head and chunk that a call is shared out to, if ragged
+  int unit;             // tiles per split (tau = 0: 1)
+  int min_tpw;          // tiles per run at least
+  int blocks;           // of all sequences at most
+  int mode, nchunk;
+};
+inline PagedPlan paged_plan(int B, int Hq, int Hkv, int D, bool e4m3, int max_len,
+                            int split_tokens, bool dense) {
+  const int T = (max_len + kPagedTile - 1) / kPagedTile;
+  PagedPlan x;
+  const int nchunk = x.nchunk = (Hq / Hkv + 15) / 16;
+  x.unit = dense ? 1 : split_tokens / kPagedTile;
+  const long splits = (long)B * Hkv * nchunk * ((T + x.unit - 1) / x.unit);
+  x.mode = dense ? kDense : x.unit > 1 && splits <= kTeamSplits ? kTeam : kChain;
+  const int runs = paged_runs(x.mode);
+  x.target = (int)std::max<long>(1, (x.mode == kTeam ? kTeamSplits
+                                                             : paged_target_groups(D, e4m3)) /
+                                       (Hkv * nchunk));
+  x.ragged = x.mode == kDense ? std::max(x.target, kRaggedGroups / (Hkv * nchunk)) : x.target;
+  x.min_tpw = T <= kSingleTiles ? (T + runs - 1) / runs : 1;
+  const long tpw = (x.min_tpw + x.unit - 1) / x.unit * (long)x.unit;
+  const long most = (T + runs * tpw - 1) / (runs * tpw);
+  x.blocks = (int)std::min<long>({(long)B + x.ragged, B * most, (long)INT32_MAX});
+  return x;
+}
+
+// The longest cache whose tiles and rows can be counted in 32 bits.
+constexpr int kPagedMaxLen = INT32_MAX - 64;
+
+// Blocks of all sequences at most, whatever the type and tolerance (the workspace holds their
+// partials).
+inline int paged_decode_blocks(int B, int Hq, int Hkv, int D, int max_len, int split_tokens) {
+  int n = 0;
+  for (int i = 0; i < 4; ++i)
+    n = std::max(n, paged_plan(B, Hq, Hkv, D, i & 1, max_len, split_tokens, i & 2).blocks);
+  return n;
+}
+
+}  // namespace mala
