@@ -581,8 +581,8 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
 // Joins the partials (O_s / l_s, m_s, l_s, count) of the sequences that have more than one block:
 // l = sum_s 2^(m_s - m) l_s, o = sum_s 2^(m_s - m) l_s (O_s / l_s) / l, a workgroup per query head.
 // LPR lanes read a partial row 16 bytes each, the workgroup's NG groups of LPR lanes take the
-// parts in turn.  Latency-bound: 3-4 us (where a part's sequence lies, then the states and
-// rows of its parts at once).
+// parts in turn.  Latency-bound: 3-4 us (where the sequence's parts lie, then their states and
+// rows at once).
 constexpr int kJoinThreads = 256;
 template <int D>
 __global__ __launch_bounds__(kJoinThreads) void mala_paged_join_kernel(PagedDecParams p) {
@@ -600,29 +600,31 @@ __global__ __launch_bounds__(kJoinThreads) void mala_paged_join_kernel(PagedDecP
   float m = kNegInf, z = 0.f;
   f32x4 acc = {0.f, 0.f, 0.f, 0.f};
   int kept = 0;
-  // LPR of the group's parts at a time: their states by the lanes, their rows by all of them
-  for (int c0 = grp; c0 < nb; c0 += LPR * NG) {
-    const int s = c0 + cl * NG;
-    const f32x4 x = s < nb ? *reinterpret_cast<const f32x4*>(pp + s * step + D)
-                           : f32x4{kNegInf, 0.f, 0.f, 0.f};
-    kept += __float_as_int(x[2]);
-    float mx = x[0];
+  // four of the group's parts at a time: every lane takes their states (one address for the
+  // group's lanes) and its piece of their rows
+  for (int s0 = grp; s0 < nb; s0 += 4 * NG) {
+    f32x4 x[4], r[4];
+    float m_new = m;
 #pragma unroll
-    for (int d = LPR / 2; d >= 1; d /= 2) mx = fmaxf(mx, __shfl_xor(mx, d));
-    const float m_new = fmaxf(m, mx), ref = m_new == kNegInf ? 0.f : m_new;
-    const float alpha = fast_exp2(m - ref), f = x[1] * fast_exp2(x[0] - ref);   // 0: no keys
+    for (int u = 0; u < 4; ++u) {
+      const int s = s0 + u * NG;
+      const float* part = pp + (long)(s < nb ? s : s0) * step;
+      x[u] = *reinterpret_cast<const f32x4*>(part + D);
+      r[u] = *reinterpret_cast<const f32x4*>(part + 4 * cl);
+      if (s >= nb) x[u] = f32x4{kNegInf, 0.f, 0.f, 0.f};
+      m_new = fmaxf(m_new, x[u][0]);
+    }
+    const float ref = m_new == kNegInf ? 0.f : m_new, alpha = fast_exp2(m - ref);
     m = m_new;
     acc *= alpha;
-    z = z * alpha + f;                   // of this lane's parts
-    const int n = min(LPR, (nb - c0 + NG - 1) / NG);
-#pragma unroll 8
-    for (int j = 0; j < n; ++j)
-      acc += __shfl(f, j, LPR) * *reinterpret_cast<const f32x4*>(pp + (c0 + j * NG) * step + 4 * cl);
-  }
+    z *= alpha;
 #pragma unroll
-  for (int d = LPR / 2; d >= 1; d /= 2) {
-    z += __shfl_xor(z, d);
-    kept += __shfl_xor(kept, d);
+    for (int u = 0; u < 4; ++u) {
+      const float f = x[u][1] * fast_exp2(x[u][0] - ref);   // 0 for a part without keys
+      z += f;
+      kept += __float_as_int(x[u][2]);
+      if (s0 + u * NG < nb) acc += f * r[u];
+    }
   }
   rows[tid] = acc;                       // the groups' sums
   if (cl == 0) {
