@@ -409,7 +409,8 @@ size_t mala_paged_decode_workspace_size(int B, int Hq, int Hkv, int D, int max_l
  * mala_decode over a paged cache.
  *   q: bf16 [B, Hq, D]; block_table: int32 [B, max_pages]; cache_lens: int32 [B]: sequence b
  *       holds n_b valid tokens, its own included (clamped into [0, max_len]); L = n_b
- *   max_len: the longest cache (the launch is sized by it), at most max_pages * page_size
+ *   max_len: the longest cache (the launch is sized by it), at most max_pages * page_size and
+ *       2^31 - 65; a batch that could need 2^24 workgroups or 2^30 tiles is not supported
  *   Keys of a page whose table entry is outside [0, num_pages) are masked: pages may be
  *       missing (a window that has moved on), and a sequence without keys gets o = 0, lse =
  *       -inf.  A tile of B_k keys of which none is left is not retained.

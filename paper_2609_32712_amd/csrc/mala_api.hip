@@ -642,10 +642,11 @@ int mala_paged_decode(const void* q, const mala_paged_cache_t* cache, const int3
   p.scale2 = scale * mala::kLog2e;
   p.log2tau = log2_tau(tau);
   if (max_len > mala::kPagedMaxLen) return fail(MALA_ERR_UNSUPPORTED, "max_len %d", max_len);
+  // (bounds the decode's grid and the join's, of 256 threads per workgroup)
   const double groups =
-      (double)Hq * mala::paged_decode_blocks(B, Hq, cache->Hkv, cache->D, max_len, split_tokens);
-  if (groups > INT32_MAX - 256 || (double)B * max_len / mala::kDecBk > INT32_MAX / 2)
-    return fail(MALA_ERR_UNSUPPORTED, "2^31 workgroups or 2^30 tiles, or more");
+      (double)(Hq + 8) * mala::paged_decode_blocks(B, Hq, cache->Hkv, cache->D, max_len, split_tokens);
+  if (groups * 256 + 65536 > UINT32_MAX || (double)B * max_len / mala::kDecBk > INT32_MAX / 2)
+    return fail(MALA_ERR_UNSUPPORTED, "a launch of 2^32 threads or 2^30 tiles, or more");
   hipStream_t s = (hipStream_t)stream;
   hipError_t e;
   if (counters &&

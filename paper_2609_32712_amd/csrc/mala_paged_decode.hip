@@ -140,17 +140,19 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
 
   const int lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
   const int w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int Hkv = p.c.Hkv, grp = p.Hq / Hkv, per = Hkv * p.nchunk;
+  const int Hkv = p.c.Hkv, grp = p.Hq / Hkv;
   // Workgroups are dealt to the CUs in turn, a round of 256 at a time, and the share of HBM that
   // a CU gets is its own: longest first, and every other round backwards, gives the CUs about
   // as many tiles each.
   const int round = blockIdx.x / kNumCus, spot = blockIdx.x % kNumCus;
-  const int item = round * kNumCus + (round % 2 ? kNumCus - 1 - spot : spot);
+  const int place = round * kNumCus + (round % 2 ? kNumCus - 1 - spot : spot);
+  // (block of a sequence, KV head), and chunk of the KV head's query heads
+  const int item = paged_item(place, p.nchunk), chunk = paged_chunk(place, p.nchunk);
   Share sh;
   if (p.sorted) {
     __shared__ Share plan;
     if (w == 0) {
-      const Share x = share_of<MODE>(p, item / per);
+      const Share x = share_of<MODE>(p, item / Hkv);
       if (lane == 0) plan = x;
     }
     __syncthreads();
@@ -161,10 +163,10 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
     sh.tpw = __builtin_amdgcn_readfirstlane(plan.tpw);
     sh.n = __builtin_amdgcn_readfirstlane(plan.n);
   } else {
-    sh = share_of<MODE>(p, item / per);
+    sh = share_of<MODE>(p, item / Hkv);
   }
   if (sh.b < 0) return;                              // the same for the whole workgroup
-  const int chunk = item % p.nchunk, hkv = item % per / p.nchunk, b = sh.b;
+  const int hkv = item % Hkv, b = sh.b;
   const int nh = min(16, grp - 16 * chunk), h0 = hkv * grp + 16 * chunk;
   const int n = sh.n, T = (n + kDecBk - 1) / kDecBk;
   const int t_lo = min(T, (TEAM ? sh.blk : sh.blk * W + w) * sh.tpw), t_hi = min(T, t_lo + sh.tpw);
@@ -215,7 +217,7 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
     if (scale2 == 0.f) scale2 = 1e-37f;
   }
   // for the join: where the sequence's partials lie
-  if (sh.blk == 0 && item % per == 0 && threadIdx.x == 0 && p.nblk > p.B)
+  if (sh.blk == 0 && hkv == 0 && chunk == 0 && threadIdx.x == 0 && p.nblk > p.B)
     p.plan[b] = make_int2(sh.first, sh.blocks);
   const float thr2 = DENSE ? 0.f : p.log2tau - log2f((float)n);    // L = n
 
@@ -658,10 +660,7 @@ __global__ __launch_bounds__(kJoinThreads) void mala_paged_join_kernel(PagedDecP
 // ------------------------------------------------------------------ launches
 template <int D, bool E4M3, int MODE>
 void launch_t(const PagedDecParams& p, hipStream_t st) {
-  // (whole rounds where there are several, for the order of the blocks)
-  unsigned n = (unsigned)(p.nblk * p.c.Hkv * p.nchunk);
-  if (n > (unsigned)kNumCus) n = (n + kNumCus - 1) / kNumCus * kNumCus;
-  const dim3 grid(n), wg(kPagedWaves * 64);
+  const dim3 grid(paged_grid(p.nblk * p.c.Hkv, p.nchunk)), wg(kPagedWaves * 64);
   if (p.o_bf16)
     hipLaunchKernelGGL((mala_paged_decode_kernel<D, E4M3, MODE, false>), grid, wg, 0, st, p);
   else

@@ -17,6 +17,7 @@ namespace mala {
 
 constexpr int kPagedTile = 32;           // keys per decision tile
 constexpr int kPagedWaves = 4;           // wavefronts of a workgroup
+constexpr int kXcds = 8;                 // workgroups are dealt to the XCDs in turn
 
 // How a block of tiles is worked on: kDense (tau = 0) and kChain, a run of tiles per wavefront
 // (kChain: of whole splits, tested one after the other); kTeam, whole splits by all
@@ -43,6 +44,23 @@ MALA_HOST_DEVICE inline int paged_blocks_of(int t, unsigned per_block) {
 MALA_HOST_DEVICE inline int paged_run_tiles(int t, int blocks, unsigned unit, int runs) {
   const unsigned n = ((unsigned)t + blocks * runs - 1) / (unsigned)(blocks * runs);
   return (int)(unit == 1 ? n : (n + unit - 1) / unit * unit);
+}
+
+// Where a KV head has more than 16 query heads, its chunks of 16 read the same K and V: workgroups
+// kXcds places apart run on one XCD and share its L2 (16 x 8192 tokens, 64 heads on 2: 50.6 us with
+// the chunks next to each other, 35.4 so).  The item (block of a sequence, KV head) and the
+// chunk at a place:
+MALA_HOST_DEVICE inline int paged_item(int place, int nchunk) {
+  return nchunk == 1 ? place : place / kXcds / nchunk * kXcds + place % kXcds;
+}
+MALA_HOST_DEVICE inline int paged_chunk(int place, int nchunk) {
+  return nchunk == 1 ? 0 : place / kXcds % nchunk;
+}
+// Places that cover all chunks of the items; whole rounds of the CUs where there are several, since
+// every other round is dealt backwards.
+inline unsigned paged_grid(int items, int nchunk) {
+  const unsigned n = nchunk == 1 ? items : ((unsigned)items + kXcds - 1) / kXcds * kXcds * nchunk;
+  return n > (unsigned)kNumCus ? (n + kNumCus - 1) / kNumCus * kNumCus : n;
 }
 
 // Workgroups that a large call is shared out to.  A CU gets its own share of HBM's rate, so it is

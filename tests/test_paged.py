@@ -321,6 +321,22 @@ def test_decode_many_blocks(Hq, Hkv, D, e4m3, n, tau):
         assert tiles[b][clear[b]].tolist() == x[2][clear[b]].tolist()
 
 
+@pytest.mark.parametrize("Hq,Hkv,D,tau", [(40, 1, 128, 0.0), (66, 2, 64, 0.0), (40, 1, 64, 0.1)])
+def test_decode_many_chunks(Hq, Hkv, D, tau):
+    # three chunks of heads per KV head, more workgroups than CUs, a number that no round divides
+    rng = np.random.default_rng(16)
+    w = Batch(16, [0, 1] + rng.integers(1, 150, 99).tolist(), Hq, Hkv, D, 16, needle=128 / D)
+    want = w.plain(tau, 64)
+    smax = w.scale * 2 * float(w.q.abs().sum(2).max())     # (as for the rule's other batches)
+    clear = [x[4] > 250 * pu.U24 + 16 * pu.U24 * (smax + 1) for x in want]
+    assert sum(x.sum() for x in clear) >= 0.9 * Hq * len(want)
+    got = w.decode(tau, 64)
+    w.check(got, want, clear=clear)
+    tiles = got["head_tiles"].cpu().numpy()
+    for b, x in enumerate(want):
+        assert tiles[b][clear[b]].tolist() == x[2][clear[b]].tolist()
+
+
 @pytest.mark.parametrize("ks,vs", [([-0.5, 1.0], [0.75, -1.25]), ([0.0, 0.25], [0.0, 1.0])])
 @pytest.mark.parametrize("tau", [0.0, 0.1])
 def test_decode_scales_of_any_sign(ks, vs, tau):

@@ -88,7 +88,7 @@ def test_read_refusals(kw, want):
     (dict(tau=float("inf")), BAD), (dict(tau=float("nan")), BAD), (dict(out=2), BAD),
     (dict(q=24), BAD), (dict(o=20), BAD), (dict(W=4000, mx=128000, ws=None), WS),
     (dict(W=4000, mx=128000, nbytes=100), WS), (dict(W=4000, mx=128000, ws=24), WS),
-    (dict(B=1 << 28), UNSUP),
+    (dict(B=1 << 28), UNSUP), (dict(B=1 << 21, mx=32), UNSUP),
     (dict(W=1 << 27, mx=2 ** 31 - 1), UNSUP), (dict(W=1 << 26, mx=1 << 30, B=1 << 6), UNSUP)])
 def test_decode_refusals(kw, want):
     a = dict(q=16, table=16, lens=16, o=16, lse=16, split=64, ws=32, nbytes=1 << 62, B=2, Hq=8,

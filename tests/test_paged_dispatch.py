@@ -45,6 +45,23 @@ int main() {
     }
     if (blocks > x.blocks) bad = "more blocks than the grid";
     if (x.blocks > paged_decode_blocks(B, Hq, Hkv, D, max_len, split)) bad = "more than the workspace";
+    // the places of a small grid: every chunk of every item once, the chunks of one on one XCD
+    const long items = (long)x.blocks * Hkv;
+    if (items * x.nchunk < 20000) {
+      const unsigned grid = paged_grid((int)items, x.nchunk);
+      if (grid > 256 && grid % 256) bad = "part of a round";
+      std::vector<int> seen(items * x.nchunk), xcd(items, -1);
+      for (unsigned at = 0; at < grid; ++at) {
+        const int item = paged_item((int)at, x.nchunk), chunk = paged_chunk((int)at, x.nchunk);
+        if (item < 0 || chunk < 0 || chunk >= x.nchunk) bad = "no such chunk";
+        else if (item < items) {
+          ++seen[(long)item * x.nchunk + chunk];
+          if (xcd[item] >= 0 && xcd[item] != (int)(at % 8)) bad = "chunks apart";
+          xcd[item] = at % 8;
+        }
+      }
+      for (int n : seen) if (n != 1) bad = "a chunk left out or done twice";
+    }
     std::printf("%d %d %ld %s.\n", x.mode, x.blocks, blocks, bad);
   }
 }
