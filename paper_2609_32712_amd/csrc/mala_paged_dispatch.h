@@ -77,10 +77,17 @@ inline int paged_target_groups(int D, bool e4m3) { return kNumCus * (128 / D) * 
 // 92.3 / 91.2.  (With tau > 0 blocks are whole splits, and the next smaller ones a third too small.)
 constexpr int kRaggedGroups = 2 * kNumCus;
 
-// Caches of up to 16 tiles stay in one workgroup, without a join: two more tiles take a wavefront
-// 2.4 us (1.6 at D = 64), the join 3.9.  (With 8 wavefronts, caches of 40 tiles could do so too:
-// 8 x 1000 tokens 14.7 instead of 12.9 us, the CUs left free cost more than the join.)
-constexpr int kSingleTiles = 4 * kPagedWaves;
+// Caches of up to so many tiles stay in one workgroup each, without a join: a tile more takes a
+// wavefront 1.2 us (0.8 at D = 64), the join 2.5 behind its launch.  Few workgroups leave CUs free
+// that the blocks of a split cache could use: 16 tiles; where workgroups are as many as half the
+// CUs 24 (tau = 0), as many as the CUs 32.  us per call in blocks / whole (8 KV heads, D = 128): one
+// cache of 512 tokens 7.9 / 7.9, of 768 8.0 / 9.7; 8 of 768 11.0 / 12.3; 16 of 768 14.4 / 13.4 (tau > 0
+// 15.6 / 17.1), of 1024 17.0 / 16.4, of 0..1024 14.6 / 15.3; 32 of 1024 26.0 / 23.8 (27.1 / 25.3), of
+// 0..1024 19.5 / 17.8 (21.4 / 18.1), log-uniform 11.2 / 12.0; 64 of 0..768 26.5 / 20.3; 128 e4m3 ones (D =
+// 64) of 0..1024 25.1 / 17.3.  64 tiles: 64 of 0..2048 52.8 / 48.6, but log-uniform 21.5 / 28.3.
+inline int paged_single_tiles(long groups, bool dense) {
+  return groups >= kNumCus ? 32 : dense && groups >= kNumCus / 2 ? 24 : 16;
+}
 
 // tau > 0: splits up to which the wavefronts of a workgroup share them.  us per call, a wavefront
 // per split / shared: one cache of 1000 tokens (64 splits of 128) 13.1 / 9.6, of 4096 (256) 14.2 /
@@ -108,7 +115,7 @@ inline PagedPlan paged_plan(int B, int Hq, int Hkv, int D, bool e4m3, int max_le
                                                              : paged_target_groups(D, e4m3)) /
                                        (Hkv * nchunk));
   x.ragged = x.mode == kDense ? std::max(x.target, kRaggedGroups / (Hkv * nchunk)) : x.target;
-  x.min_tpw = T <= kSingleTiles ? (T + runs - 1) / runs : 1;
+  x.min_tpw = T <= paged_single_tiles((long)B * Hkv * nchunk, dense) ? (T + runs - 1) / runs : 1;
   const long tpw = (x.min_tpw + x.unit - 1) / x.unit * (long)x.unit;
   const long most = (T + runs * tpw - 1) / (runs * tpw);
   x.blocks = (int)std::min<long>({(long)B + x.ragged, B * most, (long)INT32_MAX});

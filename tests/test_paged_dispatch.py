@@ -124,9 +124,14 @@ def test_modes_of_measured_calls(ask):
         (32, 32, 8, 128, 0, 2048, 256, 1, full(32, 2048)),       # a sequence per workgroup
         (1, 8, 1, 128, 0, 512, 256, 1, full(1, 512)),            # 16 tiles: one workgroup
         (1, 8, 1, 128, 0, 513, 256, 1, full(1, 513)),            # 17: joined
+        (16, 32, 8, 128, 0, 768, 256, 1, full(16, 768)),         # 24, 128 workgroups: one each
+        (16, 32, 8, 128, 0, 768, 128, 0, full(16, 768)),         # ... but not at tau > 0
+        (32, 32, 8, 128, 0, 1024, 128, 0, full(32, 1024)),       # 32, a workgroup per CU: one each
+        (32, 32, 8, 128, 0, 1025, 128, 1, full(32, 1025)),       # 33: could need a join
     ]
     got = ask(cases)
-    assert [g[0] for g in got] == [0, 2, 1, 0, 0, 0, 0]
+    assert [g[0] for g in got] == [0, 2, 1, 0, 0, 0, 0, 0, 1, 1, 0]
     assert [g[2] for g in got][:3] == [1, 32, 32]
     assert got[0][1] == 1 and got[3][2] * 8 <= 256 and got[4][2] == 32
     assert got[5][1] == got[5][2] == 1 and got[6][2] > 1
+    assert got[7][1] == 16 and got[8][1] > 16 and got[9][1] == 32 and got[10][1] > 32
