@@ -393,7 +393,7 @@ int mala_paged_write(const void* k_new, const void* v_new, int64_t new_token_str
  * cu_seqlens[b] .. (int32 [num_seqs + 1], non-decreasing, inside [0, total]; a run longer than
  * max_seqlen is cut to its first max_seqlen rows).  Rows that no sequence covers are not
  * written.  Rows of a page whose table entry is outside [0, num_pages) are zeros.  e4m3: value
- * x scale, rounded once.
+ * x scale in fp32, rounded to bf16 (nearest even).
  *   block_table: int32 [num_seqs, max_pages]; max_seqlen <= max_pages * page_size.
  *   total * D * 2 < 2^32, as for mala_fwd_varlen.
  */

@@ -9,8 +9,8 @@
 //
 // What bounds it (MI355X): large calls HBM, 6.1-6.6 TB/s of K and V on 1 GB and more (16 caches
 // of 131072 tokens, 8.6 GB: 1.30 ms); calls of 100-300 MB the same and about 10 us of launch, first
-// loads (lengths, then table, then K, ~2.5 us), the last workgroups and the join (3.9 us); small
-// ones those alone (one cache of 200 tokens 5.8 us, of 4096 tokens 8 + 3.9 us).
+// loads (lengths, then table, then K, ~2.5 us), the last workgroups and the join (2.5-4.6 us); small
+// ones those alone (one cache of 200 tokens 5.8 us, of 4096 tokens 8 + 2.9 us).
 //
 // A page's 16-row groups are contiguous up to the token stride, so a tile is two buffer
 // resources of 16 rows.  Rows at or past the length, and groups of a page whose table entry
@@ -583,7 +583,7 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
 // Joins the partials (O_s / l_s, m_s, l_s, count) of the sequences that have more than one block:
 // l = sum_s 2^(m_s - m) l_s, o = sum_s 2^(m_s - m) l_s (O_s / l_s) / l, a workgroup per query head.
 // LPR lanes read a partial row 16 bytes each, the workgroup's NG groups of LPR lanes take the
-// parts in turn.  Latency-bound: 3-4 us (where the sequence's parts lie, then their states and
+// parts in turn.  Latency-bound: 2.5-4.6 us (where the sequence's parts lie, then their states and
 // rows at once).
 constexpr int kJoinThreads = 256;
 template <int D>
