@@ -323,7 +323,8 @@ enum { MALA_CACHE_BF16 = 0, MALA_CACHE_E4M3 = 1 };
  * r * token_stride of k_pages and of v_pages (both the same strides; the D elements of a row
  * are contiguous), e.g. [num_pages, Hkv, page_size, D] or [num_pages, page_size, Hkv, D]
  * tensors, or K and V halves of one tensor.  Pointers are 16-byte aligned, strides multiples
- * of 16 bytes, at least D elements, and 16 rows (16 x token_stride) take less than 2^31 bytes.
+ * of 16 bytes, at least D elements, 16 rows (16 x token_stride) take less than 2^31 bytes, and
+ * all pages and all heads (num_pages x page_stride, Hkv x head_stride) at most 2^60 bytes.
  * page_size is a multiple of 16, D 64 or 128, num_pages x page_size below 2^31.
  * k_scale, v_scale: fp32 [Hkv] device arrays of an e4m3 cache, NULL for scales of 1 (and for
  * bf16).  The struct itself is host memory, read during the call. */

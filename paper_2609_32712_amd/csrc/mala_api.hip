@@ -476,13 +476,16 @@ int check_cache(const mala_paged_cache_t* c, mala::PagedCache* out) {
   if ((int64_t)c->num_pages * c->page_size > INT32_MAX)
     return fail(MALA_ERR_UNSUPPORTED, "num_pages x page_size reaches 2^31");
   const int64_t size = c->dtype == MALA_CACHE_E4M3 ? 1 : 2;
-  for (int64_t s : {c->page_stride, c->head_stride, c->token_stride}) {
-    if (s < c->D || (s * size) % 16)
+  const int64_t per_16 = 16 / size;       // elements
+  for (int64_t s : {c->page_stride, c->head_stride, c->token_stride})
+    if (s < c->D || s % per_16)
       return fail(MALA_ERR_INVALID_ARG, "cache strides must be at least D and multiples of 16 bytes");
-    if (s > INT64_MAX / 2 / c->num_pages)
-      return fail(MALA_ERR_UNSUPPORTED, "cache stride too large");
-  }
-  if (c->token_stride * size * mala::kPageRows > INT32_MAX)
+  // (compared by division: products of strides as given can pass 64 bits.  Every axis below 2^60
+  // bytes, so that the kernels' sums of them fit too.)
+  constexpr int64_t kMost = (int64_t)1 << 60;
+  if (c->page_stride > kMost / size / c->num_pages || c->head_stride > kMost / size / c->Hkv)
+    return fail(MALA_ERR_UNSUPPORTED, "cache stride too large");
+  if (c->token_stride > INT32_MAX / (size * mala::kPageRows))
     return fail(MALA_ERR_UNSUPPORTED, "16 rows of the cache span 2^31 bytes");
   if ((uintptr_t)c->k_pages % 16 || (uintptr_t)c->v_pages % 16)
     return fail(MALA_ERR_INVALID_ARG, "k_pages or v_pages not 16-byte aligned");
