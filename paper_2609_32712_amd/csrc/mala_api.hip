@@ -533,13 +533,21 @@ int mala_paged_update(const int32_t* lens, const int32_t* new_lens, int32_t* blo
     return fail(MALA_ERR_UNSUPPORTED, "page_size %d is not a multiple of %d", page_size, mala::kPageRows);
   if ((double)num_seqs * max_pages * page_size > INT32_MAX || (int64_t)num_pages * page_size > INT32_MAX)
     return fail(MALA_ERR_UNSUPPORTED, "num_seqs x max_pages x page_size or num_pages x page_size reaches 2^31");
-  const void* in[] = {lens, new_lens, block_table, free_ring, free_state};
-  const void* out[] = {lens_out, cu_seqlens, slots, positions, free_state_out};
-  for (int i = 0; i < 5; ++i)
-    for (int j = 0; j < 5; ++j)
-      if (out[j] && (in[i] == out[j] || (i < j && out[i] == out[j])))
+  // block_table and free_ring are inputs and outputs; an output shares no byte with any other array
+  const struct {
+    const int32_t* p;
+    int64_t n;
+  } arrays[] = {{lens, num_seqs}, {new_lens, num_seqs}, {free_state, 2},
+                {block_table, (int64_t)num_seqs * max_pages}, {free_ring, ring_size},
+                {lens_out, num_seqs}, {cu_seqlens, (int64_t)num_seqs + 1}, {slots, max_tokens},
+                {positions, max_tokens}, {free_state_out, 4}};
+  constexpr int kArrays = 10, kFirstOutput = 3;
+  for (int j = kFirstOutput; j < kArrays; ++j)
+    for (int i = 0; i < j; ++i) {
+      const uintptr_t a = (uintptr_t)arrays[i].p, b = (uintptr_t)arrays[j].p;
+      if (a && b && arrays[i].n && arrays[j].n && a < b + 4 * arrays[j].n && b < a + 4 * arrays[i].n)
         return fail(MALA_ERR_INVALID_ARG, "an output shares its memory with another argument");
-  if (block_table == free_ring) return fail(MALA_ERR_INVALID_ARG, "block_table is free_ring");
+    }
   const mala::PagedUpdateParams p = {lens, new_lens, block_table, free_ring, free_state, lens_out,
                                      cu_seqlens, slots, positions, free_state_out, num_seqs,
                                      max_pages, page_size, num_pages, ring_size, max_tokens};

@@ -30,3 +30,45 @@ def test_cache_strides_whose_products_pass_64_bits(kw):
 def test_large_cache_strides_that_fit(kw):
     assert mala.load_library().mala_paged_write(16, 16, 512, 128, 16, ctypes.byref(_cache(**kw)), 0,
                                                 None) == mala.MALA_OK
+
+
+# name, entries of each of mala_paged_update's arrays for R = 4, W = 8, C = 100, T = 64
+UPDATE = (("lens", 4), ("new_lens", 4), ("table", 32), ("ring", 100), ("state", 2), ("lens_out", 4),
+          ("cu", 5), ("slots", 64), ("positions", 64), ("state_out", 4))
+
+
+def _update(at, T=64):
+    return mala.load_library().mala_paged_update(*(at[n] for n, _ in UPDATE), 4, 8, 16, 100, 100, T, None)
+
+
+def _apart():
+    at, out = 4096, {}
+    for name, n in UPDATE:
+        out[name] = at
+        at += 4 * n                       # one behind the other, without a gap
+    return out
+
+
+OUTPUTS = [n for n, _ in UPDATE[5:]]
+PAIRS = [(o, n) for o in OUTPUTS for n, _ in UPDATE if n != o] + [("ring", "table")]
+
+
+@pytest.mark.parametrize("out,other", PAIRS)
+def test_update_refuses_arrays_that_overlap(out, other):
+    size = dict(UPDATE)
+    for shift in (-4 * (size[out] - 1), 0, 4 * (size[other] - 1)):     # by one entry, from either end
+        at = {n: (1 << 20) + (i << 12) for i, (n, _) in enumerate(UPDATE)}
+        at[out] = at[other] + shift
+        _refused(_update(at), BAD)
+
+
+def test_update_takes_arrays_that_touch():
+    # (a status of its own: without a GPU the launch fails, behind all refusals)
+    import torch
+    if torch.cuda.is_available():
+        pytest.skip("addresses of no tensors: for machines without a GPU")
+    assert _update(_apart()) == mala.MALA_ERR_HIP
+    # arrays of no entries overlap nothing, wherever they are
+    at = _apart()
+    at["slots"] = at["positions"] = at["table"] + 8
+    assert _update(at, T=0) == mala.MALA_ERR_HIP
