@@ -122,6 +122,33 @@ __device__ __forceinline__ float rows_sum(float x) {
   return halves_sum(__uint_as_float(r[0]) + __uint_as_float(r[1]));
 }
 
+// a b as an fp32, whatever takes it
+__device__ __forceinline__ float rounded_product(float a, float b) {
+#pragma clang fp contract(off)
+  return a * b;
+}
+
+// The rule's state of one split and head: m, l, reference and normaliser of the keys retained.
+// kChain and kTeam decide by these functions alone.  Which of the two a call takes goes by its
+// batch, and what is retained must not: so each operation rounds as it is written here (fused ones
+// are written out, here and wherever a product meets a sum below, and the compiler adds none).
+struct SplitState {
+  float m = kNegInf, l = 0.f;
+  __device__ __forceinline__ float run() const { return m + fast_log2(l); }
+  // a tile's largest score mt against the state's log-sum (l = 0: the split's first tile)
+  __device__ __forceinline__ bool retains(float mt, float run, float thr2) const {
+#pragma clang fp contract(off)
+    return l == 0.f || mt - run >= thr2;
+  }
+  // adds a tile: `sum` of its 2^(score - mt), or of scores of -inf alone 0
+  __device__ __forceinline__ void add(float mt, float sum) {
+#pragma clang fp contract(off)
+    const float own = mt == kNegInf ? 0.f : mt, top = fmaxf(m, mt), ref = top == kNegInf ? 0.f : top;
+    l = __builtin_fmaf(l, fast_exp2(m - ref), sum * fast_exp2(own - ref));
+    m = top;
+  }
+};
+
 template <int D, bool E4M3, int MODE>
 __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(PagedDecParams p) {
   constexpr int W = kPagedWaves;
@@ -318,7 +345,7 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
     float x = fmaxf(s[0], s[4]);
 #pragma unroll
     for (int r = 1; r < 4; ++r) x = fmaxf(x, fmaxf(s[r], s[4 + r]));
-    return rows_max(x) * scale2;
+    return rounded_product(rows_max(x), scale2);
   };
 
   // m, l: reference and normaliser of what this wavefront retained (l of this lane's keys;
@@ -384,10 +411,10 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
   } else if constexpr (TEAM) {
     // What bounds a call of few splits is the chain of a split's tiles.  Here the wavefronts score
     // W tiles at once and publish each tile's maximum and sum per head (against that maximum);
-    // behind a barrier every wavefront takes the W tests in order, carrying the split's (md, ld),
+    // behind a barrier every wavefront takes the W tests in order, carrying the split's state,
     // and adds its tile's values if its own was retained.  K and V of the next round load
     // meanwhile; V is fetched for every tile.
-    float md = kNegInf, ld = 0.f;
+    SplitState state;
     for (int t0 = t_hi - 1, round = 0; t0 >= t_lo; ++round) {
       int t_next = t0 - W, lo_next = split_lo;
       if (t_next < split_lo) {               // the split below
@@ -412,14 +439,9 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
 #pragma unroll
       for (int u = 0; u < W; ++u) {
         const f32x2 x = tests[round & 1][u][col];     // (a sum below 0: no key of the tile is there)
-        const bool demand =
-            head_valid && !(x[1] < 0.f) && (ld == 0.f || x[0] - (md + fast_log2(ld)) >= thr2);
+        const bool demand = head_valid && !(x[1] < 0.f) && state.retains(x[0], state.run(), thr2);
         if (u == w) mine = demand;
-        if (demand) {
-          const float d_new = fmaxf(md, x[0]), ds = d_new == kNegInf ? 0.f : d_new;
-          ld = ld * fast_exp2(md - ds) + x[1] * fast_exp2((x[0] == kNegInf ? 0.f : x[0]) - ds);
-          md = d_new;
-        }
+        if (demand) state.add(x[0], x[1]);
       }
       legal += here ? 1u : 0u;
       if (wave_any(mine)) {
@@ -427,7 +449,7 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
         raise(mine ? fmaxf(m, mt) : m);
         const float shift = m == kNegInf ? 0.f : m, f = mine ? fast_exp2(own - shift) : 0.f;
         if (mine) {
-          l += ps * f;
+          l = __builtin_fmaf(ps, f, l);
           ++cnt;
           if (p.counters) hsum += tile_hash(b, h0 + col, 0, t0 - w);
         }
@@ -435,23 +457,20 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
         for (int r = 0; r < 8; ++r) s[r] = mine ? s[r] * f : 0.f;
         add_values(s);
       }
-      if (lo_next != split_lo) {
-        md = kNegInf;
-        ld = 0.f;
-      }
+      if (lo_next != split_lo) state = SplitState();
       t0 = t_next;
       split_lo = lo_next;
       at = next;
     }
     vfetch = legal;
   } else if (t_hi > t_lo) {
-    // md, ld: reference and normaliser of the split being tested, over all its retained keys.
     // While tile t is worked on, K of t - 1 is in registers or on its way (its scores are taken
     // first), K of t - 2 and V of t load.  V of t - 1 is fetched when the state before tile t's
     // update may retain it: the normaliser only grows, so a tile that fails this test fails the
     // real one too (a margin covers the rounding).
     constexpr float kHintMargin = 1e-2f;
-    float md = kNegInf, ld = 0.f, s[8], sn[8];
+    SplitState state;                        // of the split being tested
+    float s[8], sn[8];
     int left = (t_hi - 1) % p.unit + 1;      // tiles of the split from t down
     Place next = next_tile(t_hi - 2, t_lo);
     to_lds(kr);
@@ -464,11 +483,11 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
       load_tile(p.c.k, after, true, kr);
       const float mtn = scores(next, sn);
       const bool here = at.rows0 + at.rows1 > 0, there = next.rows0 + next.rows1 > 0;
-      const float run = md + fast_log2(ld);
-      const bool demand = head_valid && here && (ld == 0.f || mt - run >= thr2);
+      const float run = state.run();
+      const bool demand = head_valid && here && state.retains(mt, run, thr2);
       const bool last = --left == 0;         // the next tile starts a split: always retained
       const bool hint =
-          there && (last || wave_any(head_valid && (ld == 0.f || mtn - run >= thr2 - kHintMargin)));
+          there && (last || wave_any(head_valid && state.retains(mtn, run, thr2 - kHintMargin)));
       const bool any = wave_any(demand);
       if (any) to_lds(vr);
       load_tile(p.c.v, next, hint, vr);
@@ -487,20 +506,17 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
         const float ps = ((s[0] + s[1]) + (s[2] + s[3])) + ((s[4] + s[5]) + (s[6] + s[7]));
         const float all = rows_sum(ps);
         if (demand) {
-          const float d_new = fmaxf(md, mt), ds = d_new == kNegInf ? 0.f : d_new;
-          ld = ld * fast_exp2(md - ds) + all * fast_exp2(own - ds);
-          md = d_new;
+          state.add(mt, all);
           ++cnt;
           if (p.counters) hsum += tile_hash(b, h0 + col, 0, t);
         }
-        l += ps * f;
+        l = __builtin_fmaf(ps, f, l);
 #pragma unroll
         for (int r = 0; r < 8; ++r) s[r] *= f;
         add_values(s);
       }
       if (last) {
-        md = kNegInf;
-        ld = 0.f;
+        state = SplitState();
         left = p.unit;
       }
 #pragma unroll
@@ -526,7 +542,7 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
   const float top_m = M;
   if (M == kNegInf) M = 0.f;
 #pragma unroll
-  for (int u = 0; u < W; ++u) L += sums[u][col] * fast_exp2(refs[u][col] - M);
+  for (int u = 0; u < W; ++u) L = __builtin_fmaf(sums[u][col], fast_exp2(refs[u][col] - M), L);
   const long part = (long)(sh.first + sh.blk) * p.Hq + h0;   // of the block's first head
   {
     // (0 for a wavefront without keys)
@@ -579,6 +595,10 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
   }
 }
 
+__device__ __forceinline__ f32x4 fma4(f32x4 a, float f, f32x4 c) {
+  return __builtin_elementwise_fma(a, f32x4{f, f, f, f}, c);
+}
+
 // Joins the partials (O_s / l_s, m_s, l_s, count) of the sequences that have more than one block:
 // l = sum_s 2^(m_s - m) l_s, o = sum_s 2^(m_s - m) l_s (O_s / l_s) / l, a workgroup per query head.
 // LPR lanes read a partial row 16 bytes each, the workgroup's NG groups of LPR lanes take the
@@ -621,10 +641,11 @@ __global__ __launch_bounds__(kJoinThreads) void mala_paged_join_kernel(PagedDecP
     z *= alpha;
 #pragma unroll
     for (int u = 0; u < 4; ++u) {
-      const float f = x[u][1] * fast_exp2(x[u][0] - ref);   // 0 for a part without keys
-      z += f;
+      // f: 0 for a part without keys, and past the last part, where r is the row of part s0 again
+      const float e = fast_exp2(x[u][0] - ref), f = x[u][1] * e;
+      z = __builtin_fmaf(x[u][1], e, z);
       kept += __float_as_int(x[u][2]);
-      if (s0 + u * NG < nb) acc += f * r[u];
+      acc = fma4(r[u], f, acc);
     }
   }
   rows[tid] = acc;                       // the groups' sums
@@ -644,8 +665,8 @@ __global__ __launch_bounds__(kJoinThreads) void mala_paged_join_kernel(PagedDecP
 #pragma unroll
   for (int u = 0; u < NG; ++u) {
     const float f = fast_exp2(state[u][0] - ref);
-    z += state[u][1] * f;
-    acc += rows[u * LPR + cl] * f;
+    z = __builtin_fmaf(state[u][1], f, z);
+    acc = fma4(rows[u * LPR + cl], f, acc);
     kept += counts[u];
   }
   const long bh = blockIdx.x;

@@ -44,3 +44,45 @@ def test_bf16_outputs_are_the_fp32_ones_rounded_once(lens, Hq, Hkv, D, e4m3, tau
     assert torch.equal(half["o"], full["o"].to(torch.bfloat16))
     assert torch.equal(half["lse"], full["lse"])
     assert torch.equal(half["head_tiles"], full["head_tiles"])
+
+
+def _near_ties(s, n, tau, split):
+    """Tolerances at which some decision is a tie: of every head and split of scores s [Hq, n]
+    (64 bits), the test value nearest to tau in the split's chain of decisions."""
+    out = []
+    for x in s:
+        for lo in range(0, n, split):
+            run, best = -np.inf, None
+            for a in range(lo + (min(n, lo + split) - 1 - lo) // 32 * 32, lo - 1, -32):
+                tile = x[a:min(a + 32, n)]
+                T = np.inf if run == -np.inf else n * np.exp(tile.max() - run)
+                if best is None or abs(np.log(T / tau)) < abs(np.log(best / tau)):
+                    best = T
+                if T >= tau:
+                    run = np.logaddexp.reduce(np.append(tile, run))
+            if np.isfinite(best):
+                out.append(best)
+    return out
+
+
+@pytest.mark.parametrize("D,e4m3,split", [(128, False, 256), (64, True, 128), (128, True, 512)])
+def test_retained_sets_do_not_depend_on_the_batch_at_ties(D, e4m3, split):
+    # alone the sequence's splits are shared by wavefronts, in a batch of 70 of them each
+    # wavefront takes its own: every decision has to be the same, those on the border of the
+    # tolerance (to the last bit of it, and a few to either side) among them
+    Hq, Hkv, n, tau = 8, 2, 2000, 0.05
+    w = Normals(2, [n] * 70, Hq, Hkv, D, e4m3=e4m3, q_scale=2.0)
+    w.q[1:], w.table[1:] = w.q[:1], w.table[:1]
+    pos = np.arange(n)
+    rows = w.cache.k_pages.float().double().cpu().numpy()[w.table[0].cpu().numpy()[pos // w.P], :, pos % w.P]
+    q = w.q[0].double().cpu().numpy()
+    s = np.stack([rows[:, h // (Hq // Hkv)] @ q[h] for h in range(Hq)]) * w.scale
+    some = 0
+    for t in _near_ties(s, n, tau, split):
+        for t32 in np.float32(t) * (1 + np.arange(-2, 3, dtype=np.float32) * np.float32(2 ** -23)):
+            alone = w.decode(float(t32), split, rows=slice(1))
+            batch = w.decode(float(t32), split)
+            tiles = batch["head_tiles"]
+            assert (tiles == tiles[0]).all() and torch.equal(alone["head_tiles"][0], tiles[0]), t32
+            some += int((tiles[0] < -(-n // 32)).any())
+    assert some > 100
