@@ -135,10 +135,12 @@ __device__ __forceinline__ float rounded_product(float a, float b) {
 struct SplitState {
   float m = kNegInf, l = 0.f;
   __device__ __forceinline__ float run() const { return m + fast_log2(l); }
-  // a tile's largest score mt against the state's log-sum (l = 0: the split's first tile)
+  // of a tile with the largest score mt (l = 0: the split's first one)
   __device__ __forceinline__ bool retains(float mt, float run, float thr2) const {
-#pragma clang fp contract(off)
-    return l == 0.f || mt - run >= thr2;
+    return l == 0.f || paged_retains(mt, run, thr2);
+  }
+  __device__ __forceinline__ bool may_retain(float mt, float run, float thr2) const {
+    return l == 0.f || paged_may_retain(mt, run, thr2);
   }
   // adds a tile: `sum` of its 2^(score - mt), or of scores of -inf alone 0
   __device__ __forceinline__ void add(float mt, float sum) {
@@ -466,9 +468,7 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
   } else if (t_hi > t_lo) {
     // While tile t is worked on, K of t - 1 is in registers or on its way (its scores are taken
     // first), K of t - 2 and V of t load.  V of t - 1 is fetched when the state before tile t's
-    // update may retain it: the normaliser only grows, so a tile that fails this test fails the
-    // real one too (a margin covers the rounding).
-    constexpr float kHintMargin = 1e-2f;
+    // update may retain it.
     SplitState state;                        // of the split being tested
     float s[8], sn[8];
     int left = (t_hi - 1) % p.unit + 1;      // tiles of the split from t down
@@ -487,7 +487,7 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
       const bool demand = head_valid && here && state.retains(mt, run, thr2);
       const bool last = --left == 0;         // the next tile starts a split: always retained
       const bool hint =
-          there && (last || wave_any(head_valid && state.retains(mtn, run, thr2 - kHintMargin)));
+          there && (last || wave_any(head_valid && state.may_retain(mtn, run, thr2)));
       const bool any = wave_any(demand);
       if (any) to_lds(vr);
       load_tile(p.c.v, next, hint, vr);

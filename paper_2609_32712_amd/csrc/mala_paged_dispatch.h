@@ -46,6 +46,24 @@ MALA_HOST_DEVICE inline int paged_run_tiles(int t, int blocks, unsigned unit, in
   return (int)(unit == 1 ? n : (n + unit - 1) / unit * unit);
 }
 
+// The rule's test of a tile with the largest score mt (base 2) against its split's log-sum `run`, and
+// the early one, with the log-sum before the tile above has been added: what the first would
+// retain the second must not rule out.  A log-sum only grows, but as an fp32: adding a tile can
+// take it down by the rounding of the sum (1e-5 at most) and where that crosses a step of fp32
+// by the step, 2^-23 |run|.  The margin covers both, and the differences' own rounding.
+MALA_HOST_DEVICE inline bool paged_retains(float mt, float run, float thr2) {
+#ifdef __clang__
+#pragma clang fp contract(off)
+#endif
+  return mt - run >= thr2;
+}
+MALA_HOST_DEVICE inline bool paged_may_retain(float mt, float run, float thr2) {
+#ifdef __clang__
+#pragma clang fp contract(off)
+#endif
+  return mt - run >= thr2 - __builtin_fmaf(__builtin_fabsf(run), 0x1p-21f, 1e-2f);
+}
+
 // Where a KV head has more than 16 query heads, its chunks of 16 read the same K and V: workgroups
 // kXcds places apart run on one XCD and share its L2 (16 x 8192 tokens, 64 heads on 2: 50.6 us with
 // the chunks next to each other, 35.4 so).  The item (block of a sequence, KV head) and the
