@@ -69,11 +69,10 @@ __device__ __forceinline__ Share share_of(const PagedDecParams& p, int at) {
       const int tpw = paged_run_tiles(t, max(nb, 1), unit, W);
       int from = end - nb;
       if (p.sorted && __builtin_amdgcn_ballot_w64(lane < here && tpw > 4)) {
-        // eight classes of run lengths, the longest class first
-        const int cls = min(7, (int)(tpw * 8u / (per_block / W + 1u)));
+        const int cls = paged_run_class(tpw, per_block, W);
         int base = 0;
 #pragma unroll
-        for (int c = 7; c >= 0; --c) {
+        for (int c = kPagedClasses - 1; c >= 0; --c) {
           const int e = wave_scan(cls == c ? nb : 0);
           if (cls == c) from = base + e - nb;
           base += __builtin_amdgcn_readlane(e, 63);

@@ -46,6 +46,13 @@ MALA_HOST_DEVICE inline int paged_run_tiles(int t, int blocks, unsigned unit, in
   return (int)(unit == 1 ? n : (n + unit - 1) / unit * unit);
 }
 
+// Blocks are dealt in classes of run lengths, the longest class (7) first; tpw <= per_block / runs.
+constexpr int kPagedClasses = 8;
+MALA_HOST_DEVICE inline int paged_run_class(int tpw, unsigned per_block, int runs) {
+  const int c = (int)(tpw * (unsigned)kPagedClasses / (per_block / runs + 1u));
+  return c < kPagedClasses - 1 ? c : kPagedClasses - 1;
+}
+
 // The rule's test of a tile with the largest score mt (base 2) against its split's log-sum `run`, and
 // the early one, with the log-sum before the tile above has been added: what the first would
 // retain the second must not rule out.  A log-sum only grows, but as an fp32: adding a tile can
