@@ -668,10 +668,10 @@ def paged_read(cache, block_table, cu_seqlens, max_seqlen, total, stream=None):
 def paged_decode(q, cache, block_table, cache_lens, max_len, scale, tau, split_tokens=None,
                  stats=True, workspace=None, stream=None, out_dtype=torch.float32):
     """decode over a PagedCache: block_table int32 [B, max_pages], cache_lens int32 [B] (at
-    most max_len); split_tokens: None for default_split_tokens."""
+    most max_len); split_tokens: None for default_split_tokens(), whatever the batch."""
     B, Hq, D = q.shape
     if split_tokens is None:
-        split_tokens = default_split_tokens(B, cache.Hkv, max_len)
+        split_tokens = default_split_tokens()
     with _on_stream(stream):
         o = torch.empty((B, Hq, D), dtype=out_dtype, device=q.device)
         lse = torch.empty((B, Hq), dtype=torch.float32, device=q.device)
@@ -685,8 +685,11 @@ def paged_decode(q, cache, block_table, cache_lens, max_len, scale, tau, split_t
     return dict(o=o, lse=lse, head_tiles=ht, counters=cnt)
 
 
-def default_split_tokens(B, Hkv, max_len, num_cus=256, waves_per_simd=2):
-    """Tokens per split (a multiple of 32) that give about num_cus * 4 * waves_per_simd splits
-    over batch and KV heads, between 128 (a tile for each wavefront of a workgroup) and 512."""
-    tokens = -(-B * Hkv * max_len // (num_cus * 4 * waves_per_simd))
-    return int(max(128, min(512, -(-tokens // 32) * 32)))
+def default_split_tokens(B=None, Hkv=None, max_len=None, num_cus=256, waves_per_simd=2):
+    """Tokens per split of paged_decode where the caller gives none.  The retained set depends on
+    them, so they are the same for every batch and max_len: a request retains the same tiles
+    alone and beside others, eagerly and in a graph captured for longer caches (the arguments
+    have no bearing).  A tile for each wavefront of a workgroup; us per call with 128 / 256 /
+    512 (32 heads on 8, tau = 1e-3): 1 x 4096 tokens 10.9 / 12.5 / 16.2, 1 x 32768 27.9 / 31.3 /
+    28.1, 16 ragged caches of up to 8192 50.3 / 49.6 / 54.8, 64 of them 176 / 177 / 182."""
+    return 128

@@ -86,3 +86,18 @@ def test_retained_sets_do_not_depend_on_the_batch_at_ties(D, e4m3, split):
             assert (tiles == tiles[0]).all() and torch.equal(alone["head_tiles"][0], tiles[0]), t32
             some += int((tiles[0] < -(-n // 32)).any())
     assert some > 100
+
+
+@pytest.mark.parametrize("tau", [1.0, 300.0])
+@pytest.mark.parametrize("D", [64, 128])
+def test_default_split_gives_a_request_the_same_tiles_in_every_batch(D, tau):
+    # alone, beside others, and sized for longer caches (as a captured step is)
+    w = Normals(3, [3000, 700, 8000] * 12, 16, 4, D, q_scale=2.0)
+    call = lambda rows, n: mala.paged_decode(w.q[rows], w.cache, w.table[rows].contiguous(), w.n[rows], n,
+                                             w.scale, tau)
+    whole = call(slice(None), 8000)
+    if tau > 1:       # (L = n: against splits of 128 keys of 8000 a test value is 60 and more)
+        assert int(whole["counters"][mala.CNT_RETAINED]) < int(whole["counters"][mala.CNT_LEGAL])
+    for b, n in enumerate(w.lens[:3]):
+        for longest in (n, 8000):
+            assert torch.equal(call(slice(b, b + 1), longest)["head_tiles"][0], whole["head_tiles"][b])

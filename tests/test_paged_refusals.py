@@ -72,3 +72,16 @@ def test_update_takes_arrays_that_touch():
     at = _apart()
     at["slots"] = at["positions"] = at["table"] + 8
     assert _update(at, T=0) == mala.MALA_ERR_HIP
+
+
+def test_default_split_does_not_go_by_the_batch(monkeypatch):
+    import torch
+    seen = []
+    monkeypatch.setattr(mala, "mala_paged_decode", lambda *a, **kw: seen.append(a[9]))
+
+    class Cache:
+        Hkv = 4
+    for B, n in ((1, 100), (1, 100000), (64, 100), (200, 30000)):
+        mala.paged_decode(torch.zeros((B, 8, 64)), Cache, None, None, n, 0.125, 1e-3)
+        mala.paged_decode(torch.zeros((B, 8, 64)), Cache, None, None, n, 0.125, 1e-3, 512)
+    assert seen[1::2] == [512] * 4 and set(seen[::2]) == {mala.default_split_tokens()}
