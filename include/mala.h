@@ -355,6 +355,12 @@ typedef struct {
  *       Pages are taken from the head in the order of requests and positions; pages given
  *       back go behind the last free one in the same order and can be taken from the next
  *       call on.  A ring of num_pages entries holds them all.
+ *       What a shrinking request gives back is its table entries as they are: each has to be a
+ *       page of the pool that is in no other row.  Entries that are not (missing pages of a
+ *       window that has moved on, a prefix that requests share) would become free pages too: a
+ *       request that then took one would keep its length and get slots of -1, or another
+ *       request's rows.  Do not shrink a request over such entries: put the pages that are
+ *       its own behind the last free one, raise count by as many, and pass lens 0 for it.
  *   A request whose pages do not fit the free ones any more, in the order of requests, is
  *   refused: it takes none, keeps its length, and its tokens get slot -1.  (Requests that
  *   need no page are never refused.)  No page belongs to two requests.

@@ -642,7 +642,11 @@ def _on_stream(stream):
 def paged_update(lens, new_lens, block_table, free_ring, free_state, max_tokens, page_size,
                  num_pages, stream=None):
     """One step's page tables (block_table and free_ring are updated in place): a dict of
-    lens, cu_seqlens, slots, positions ([max_tokens]) and free_state of the next step."""
+    lens, cu_seqlens, slots, positions ([max_tokens]) and free_state of the next step.
+
+    A request that shrinks gives its table entries back as they are, so each of those has to be a
+    page of the pool and in no other row: where a window has left entries of -1, or requests
+    share a prefix, put the request's own pages on the ring and pass lens 0 for it instead."""
     R = lens.shape[0]
     with _on_stream(stream):
         i32 = dict(dtype=torch.int32, device=lens.device)

@@ -101,3 +101,45 @@ def test_default_split_gives_a_request_the_same_tiles_in_every_batch(D, tau):
     for b, n in enumerate(w.lens[:3]):
         for longest in (n, 8000):
             assert torch.equal(call(slice(b, b + 1), longest)["head_tiles"][0], whole["head_tiles"][b])
+
+
+def test_a_windowed_request_leaves_and_its_pages_are_taken_again():
+    # missing pages are no pages to give back: the caller puts the row's own on the ring and
+    # passes length 0.  The next requests need every page of the pool, and get rows of their own.
+    rng = np.random.default_rng(9)
+    P, W, N, Hkv, Hq, D = 16, 8, 10, 2, 4, 64
+    i32 = lambda a: torch.tensor(a, dtype=torch.int32, device="cuda")
+    k, v = pu.pool(N, Hkv, P, D)
+    cache = mala.PagedCache(k, v)
+    table = torch.full((3, W), -1, dtype=torch.int32, device="cuda")
+    ring, state = i32(rng.permutation(N)), i32([7, N])
+    step = mala.paged_update(i32([0, 0, 0]), i32([100, 48, 0]), table, ring, state, 160, P, N)
+    lens, state = step["lens"], step["free_state"]
+    assert lens.tolist() == [100, 48, 0] and state.tolist()[:3] == [7, 0, 0]
+
+    def put(row, places):                 # own pages of a row: behind the last free one
+        head, count = state.tolist()[:2]
+        at = (head + count + torch.arange(len(places), device="cuda")) % N
+        ring[at] = table[row, places]
+        table[row, places] = -1
+        state[1] += len(places)
+
+    put(0, [0, 1, 2])                     # the window moves on by three pages
+    put(0, [3, 4, 5, 6])                  # and the request leaves
+    step = mala.paged_update(i32([0, 48, 0]), i32([0, 48, 112]), table, ring, state, 200, P, N)
+    assert step["lens"].tolist() == [0, 48, 112] and int(step["free_state"][2]) == 0
+    lens, state, cu = step["lens"].tolist(), step["free_state"].tolist(), step["cu_seqlens"].tolist()
+    held = [p for r in range(3) for p in table[r, :pu.pages_of(lens[r], P)].tolist()]
+    free = [int(ring[(state[0] + i) % N]) for i in range(state[1])]
+    assert sorted(held + free) == list(range(N))
+    rows = slice(cu[2], cu[3])
+    assert (step["slots"][rows] >= 0).all()
+    x = pu.quarters(rng, (2, Hkv, 200, D))
+    mala.mala_paged_write(x[0].bfloat16().cuda(), x[1].bfloat16().cuda(), step["slots"], cache)
+    q = pu.quarters(rng, (Hq, D), 4)
+    got = mala.paged_decode(q[None].bfloat16().cuda(), cache, table[2:3].contiguous(), i32([112]), 112, 0.125, 0.0)
+    o, lse, _, _, _ = pu.decode_seq(q.numpy(), x[0, :, rows].numpy(), x[1, :, rows].numpy(),
+                                    np.ones(112, bool), 0.125, 0.0, 128, 112)
+    to, tl = pu.decode_bounds(112, 0.125 * 2 * float(q.abs().sum(1).max()), 2.0, False)
+    assert np.abs(got["o"][0].double().cpu().numpy() - o).max() <= to
+    assert np.abs(got["lse"][0].double().cpu().numpy() - lse).max() <= tl
