@@ -373,8 +373,9 @@ class PagedCache:
     do, e.g. of [num_pages, page_size, Hkv, D], or of K and V in one tensor).  k_scale and
     v_scale: fp32 [Hkv] of an e4m3 cache (an element stands for its value x scale; None: 1).
 
-    Kept by the caller for as long as the cache lives; it holds the tensors, and the calls
-    below take it.  page_size is a multiple of 16, D 64 or 128."""
+    Kept by the caller for as long as the cache lives; it holds the tensors, which stay the ones
+    it was made with, and the calls below take it.  page_size is a multiple of 16, D 64 or
+    128."""
 
     def __init__(self, k_pages, v_pages, k_scale=None, v_scale=None):
         N, Hkv, P, D = _dims(k_pages, "k_pages", 4)
@@ -399,6 +400,21 @@ class PagedCache:
             k_pages.data_ptr(), v_pages.data_ptr(), _addr(k_scale), _addr(v_scale), st[0], st[1],
             st[2], N, P, Hkv, D, _CACHE[k_pages.dtype])
         self._ref = ctypes.byref(self._struct)
+
+    # The addresses that the calls use were taken from these tensors: others in their place would
+    # be kept but not used, and the first ones used but not kept.
+    _FIXED = frozenset(("k_pages", "v_pages", "k_scale", "v_scale", "num_pages", "Hkv", "page_size",
+                        "D", "device", "_struct", "_ref"))
+
+    def __setattr__(self, name, value):
+        if name in self._FIXED and "_ref" in self.__dict__:
+            raise AttributeError("%s of a PagedCache cannot be changed: make another" % name)
+        object.__setattr__(self, name, value)
+
+    def __delattr__(self, name):
+        if name in self._FIXED:
+            raise AttributeError("%s of a PagedCache cannot be deleted" % name)
+        object.__delattr__(self, name)
 
 
 _CACHE = {torch.bfloat16: CACHE_BF16, torch.float8_e4m3fn: CACHE_E4M3}

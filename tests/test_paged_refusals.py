@@ -85,3 +85,27 @@ def test_default_split_does_not_go_by_the_batch(monkeypatch):
         mala.paged_decode(torch.zeros((B, 8, 64)), Cache, None, None, n, 0.125, 1e-3)
         mala.paged_decode(torch.zeros((B, 8, 64)), Cache, None, None, n, 0.125, 1e-3, 512)
     assert seen[1::2] == [512] * 4 and set(seen[::2]) == {mala.default_split_tokens()}
+
+
+def _handle():
+    """A cache handle without tensors (the constructor takes those of a GPU only)."""
+    c = object.__new__(mala.PagedCache)
+    object.__setattr__(c, "_struct", _cache())
+    object.__setattr__(c, "_ref", ctypes.byref(c._struct))
+    for n in ("k_pages", "v_pages", "k_scale", "v_scale", "Hkv", "D", "device", "num_pages", "page_size"):
+        object.__setattr__(c, n, getattr(c._struct, n, -1))
+    return c
+
+
+@pytest.mark.parametrize("name", ["k_pages", "v_pages", "k_scale", "v_scale", "Hkv", "D", "num_pages",
+                                  "page_size", "device", "_ref"])
+def test_a_cache_handle_does_not_change(name):
+    # its addresses were taken when it was made: other tensors would be kept but not used, and the
+    # first ones used but not kept
+    c = _handle()
+    with pytest.raises(AttributeError, match="PagedCache"):
+        setattr(c, name, 1)
+    with pytest.raises(AttributeError, match="PagedCache"):
+        delattr(c, name)
+    c.note = 1                            # (a caller's own)
+    del c.note
