@@ -460,6 +460,13 @@ def _shape(t, name, ndim):
     return shape if len(shape) == ndim else _dims(t, name, ndim)
 
 
+def _int32(x, name):
+    """x, of which ctypes would pass the low 32 bits on."""
+    if -0x80000000 <= x <= 0x7fffffff:
+        return x
+    raise ValueError("%s (%s) does not fit 32 bits" % (name, x))
+
+
 def _launch(device, stream, call, *args):
     """call(*args, stream) with the tensors' device current, on the given stream or on that
     device's current one."""
@@ -490,7 +497,8 @@ def mala_paged_update(lens, new_lens, block_table, free_ring, free_state, lens_o
     _launch(dev, stream, (_lib or load_library()).mala_paged_update, lens.data_ptr(),
             new_lens.data_ptr(), block_table.data_ptr(), free_ring.data_ptr(),
             free_state.data_ptr(), lens_out.data_ptr(), cu_seqlens.data_ptr(), slots.data_ptr(),
-            _addr(positions), free_state_out.data_ptr(), R, W, page_size, num_pages, C, T)
+            _addr(positions), free_state_out.data_ptr(), R, W, _int32(page_size, "page_size"),
+            _int32(num_pages, "num_pages"), C, T)
 
 
 def mala_paged_write(k_new, v_new, slots, cache, stream=None):
@@ -527,12 +535,12 @@ def mala_paged_read(cache, block_table, cu_seqlens, max_seqlen, k, v, stream=Non
           (v, "v", torch.bfloat16, shape))
     _launch(c.device, stream, (_lib or load_library()).mala_paged_read, c._ref,
             block_table.data_ptr(), cu_seqlens.data_ptr(), k.data_ptr(), v.data_ptr(), S, W,
-            int(max_seqlen), total)
+            _int32(int(max_seqlen), "max_seqlen"), total)
 
 
 def mala_paged_decode_workspace_size(B, Hq, Hkv, D, max_len, split_tokens):
-    return int(load_library().mala_paged_decode_workspace_size(B, Hq, Hkv, D, max_len,
-                                                               split_tokens))
+    return int(load_library().mala_paged_decode_workspace_size(
+        B, Hq, Hkv, D, _int32(max_len, "max_len"), _int32(split_tokens, "split_tokens")))
 
 
 def mala_paged_decode(q, cache, block_table, cache_lens, max_len, o, lse, head_tiles, counters,
@@ -554,8 +562,9 @@ def mala_paged_decode(q, cache, block_table, cache_lens, max_len, o, lse, head_t
             raise TypeError("workspace must be on the device of the cache")
     _launch(c.device, stream, (_lib or load_library()).mala_paged_decode, q.data_ptr(), c._ref,
             block_table.data_ptr(), cache_lens.data_ptr(), o.data_ptr(), lse.data_ptr(),
-            _addr(head_tiles), _addr(counters), split_tokens, _addr(workspace), nbytes, B, Hq, W,
-            int(max_len), scale, tau, OUT_BF16 if bf16 else OUT_F32)
+            _addr(head_tiles), _addr(counters), _int32(split_tokens, "split_tokens"), _addr(workspace),
+            nbytes, B, Hq, W, _int32(int(max_len), "max_len"), scale, tau,
+            OUT_BF16 if bf16 else OUT_F32)
 
 
 # ---------------------------------------------------------------- allocating wrappers

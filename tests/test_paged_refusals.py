@@ -109,3 +109,34 @@ def test_a_cache_handle_does_not_change(name):
         delattr(c, name)
     c.note = 1                            # (a caller's own)
     del c.note
+
+
+@pytest.mark.parametrize("big", [1 << 31, (1 << 32) + 64, -(1 << 31) - 1, 1 << 70])
+def test_the_binding_refuses_numbers_that_do_not_fit(monkeypatch, big):
+    # ctypes would pass their low 32 bits on: 2^32 + 64 as 64
+    import torch
+    monkeypatch.setattr(mala, "_args", lambda *a: None)
+    monkeypatch.setattr(mala, "_device", lambda *a: 0)
+    monkeypatch.setattr(torch._C, "_cuda_getCurrentRawStream", lambda d: 0, raising=False)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: 0, raising=False)
+    called = []
+
+    class Lib:
+        def __getattr__(self, name):
+            return lambda *a: called.append((name, a)) or 0
+    monkeypatch.setattr(mala, "_lib", Lib())
+    c, i = _handle(), torch.zeros(4, dtype=torch.int32)
+    table, q, kv = torch.zeros((4, 4), dtype=torch.int32), torch.zeros((4, 8, 128)), torch.zeros((4, 9, 128))
+    read = lambda n: mala.mala_paged_read(c, table, i, n, kv, kv)
+    decode = lambda n, split: mala.mala_paged_decode(q, c, table, i, n, q, q, None, None, split, None, 0.1, 0.0)
+    update = lambda page, pages: mala.mala_paged_update(i, i, table, i, i, i, i, i, None, i, page, pages)
+    for call, good in ((read, (64,)), (decode, (64, 128)), (update, (16, 100))):
+        call(*good)
+        assert len(called) == 1 and all(n in called[0][1] for n in good)
+        called.clear()
+        for j in range(len(good)):
+            with pytest.raises((ValueError, OverflowError), match="32 bits"):
+                call(*good[:j], big, *good[j + 1:])
+        assert not called
+    with pytest.raises((ValueError, OverflowError), match="32 bits"):
+        mala.mala_paged_decode_workspace_size(4, 8, 2, 128, big, 64)
