@@ -388,7 +388,8 @@ int mala_paged_update(const int32_t* lens, const int32_t* new_lens, int32_t* blo
  * slots[t].  A slot outside [0, num_pages * page_size) is skipped (padding).  Slots are
  * distinct: of tokens with the same slot, any one's bytes stay, 16 at a time.
  *   e4m3: value / scale in fp32, rounded to nearest even, values beyond +-448 to +-448; NaN
- *   stays NaN.  num_tokens may be 0.
+ *   stays NaN.  num_tokens may be 0; num_tokens rows of one head are below 2^36 bytes of the
+ *   cache.
  */
 int mala_paged_write(const void* k_new, const void* v_new, int64_t new_token_stride,
                      int64_t new_head_stride, const int32_t* slots,

@@ -570,6 +570,9 @@ int mala_paged_write(const void* k_new, const void* v_new, int64_t new_token_str
     return fail(MALA_ERR_INVALID_ARG, "rows of k_new and v_new must be 16-byte aligned");
   if (new_token_stride > INT64_MAX / 8 / num_tokens || new_head_stride > INT64_MAX / 8 / cache->Hkv)
     return fail(MALA_ERR_UNSUPPORTED, "k_new stride too large");
+  // (a thread per 16 bytes of a row of the cache)
+  if ((int64_t)num_tokens * (cache->D / (p.c.e4m3 ? 16 : 8)) > UINT32_MAX - 255)
+    return fail(MALA_ERR_UNSUPPORTED, "a launch of 2^32 threads or more (num_tokens %d)", num_tokens);
   p.k = (const char*)k_new;
   p.v = (const char*)v_new;
   p.token_stride = new_token_stride * 2;

@@ -140,3 +140,11 @@ def test_the_binding_refuses_numbers_that_do_not_fit(monkeypatch, big):
         assert not called
     with pytest.raises((ValueError, OverflowError), match="32 bits"):
         mala.mala_paged_decode_workspace_size(4, 8, 2, 128, big, 64)
+
+
+@pytest.mark.parametrize("kw", [dict(T=1 << 28), dict(T=1 << 29, dtype=mala.CACHE_E4M3),
+                                dict(T=(1 << 31) - 1, D=64, token_stride=64)])
+def test_write_refuses_a_launch_of_2_to_the_32_threads(kw):
+    T = kw.pop("T")
+    c = ctypes.byref(_cache(**kw))
+    _refused(mala.load_library().mala_paged_write(16, 32, 512, 128, 16, c, T, None), UNSUP)
