@@ -7,10 +7,10 @@
 // take neighbouring runs and join their (m, l, O) in LDS; a sequence longer than a workgroup's
 // share leaves partials that a second launch joins.
 //
-// What bounds it (MI355X): large calls HBM, 6.1-6.6 TB/s of K and V on 1 GB and more (16 caches
-// of 131072 tokens, 8.6 GB: 1.30 ms); calls of 100-300 MB the same and about 10 us of launch, first
-// loads (lengths, then table, then K, ~2.5 us), the last workgroups and the join (2.5-4.6 us); small
-// ones those alone (one cache of 200 tokens 5.8 us, of 4096 tokens 8 + 2.9 us).
+// What bounds it (MI355X): large calls HBM, 6.2-6.9 TB/s of K and V on 1 GB and more (16 caches
+// of 131072 tokens, 8.6 GB: 1.24 ms); calls of 100-300 MB the same and about 10 us of launch, first
+// loads (lengths, then table, then K, ~2.5 us), the last workgroups and the join (2.5-4.7 us); small
+// ones those alone (one cache of 200 tokens 6.1 us, of 4096 tokens 7.9 + 3.6 us).
 //
 // A page's 16-row groups are contiguous up to the token stride, so a tile is two buffer
 // resources of 16 rows.  Rows at or past the length, and groups of a page whose table entry
@@ -95,8 +95,9 @@ __device__ __forceinline__ Share share_of(const PagedDecParams& p, int at) {
 
 // The next bf16 term of eight probabilities; x becomes what is left.  Three terms hold all 24 bits
 // of an fp32, whatever the type of the output, so that a bf16 output is the fp32 one rounded once.
-// (Two terms, 16 bits, save no time: us per call with two / three 49.9 / 50.0 for 16 ragged 8192-token
-// caches, 41.1 / 41.2 for 64 ragged e4m3 ones, 1278 / 1278 for 16 of 131072 tokens.)
+// (Two terms, 16 bits, save time only where several chunks of heads share K and V: us per call with
+// two / three 49.9 / 50.0 for 16 ragged 8192-token caches, 41.1 / 41.2 for 64 ragged e4m3 ones, 1278 /
+// 1278 for 16 of 131072 tokens, 33.8 / 36.4 for 16 of 8192 with 64 heads on 2.)
 __device__ __forceinline__ bf16x8 take_bf16x8(float (&x)[8]) {
 #pragma clang fp contract(off)
   i32x4 u;
@@ -601,7 +602,7 @@ __device__ __forceinline__ f32x4 fma4(f32x4 a, float f, f32x4 c) {
 // Joins the partials (O_s / l_s, m_s, l_s, count) of the sequences that have more than one block:
 // l = sum_s 2^(m_s - m) l_s, o = sum_s 2^(m_s - m) l_s (O_s / l_s) / l, a workgroup per query head.
 // LPR lanes read a partial row 16 bytes each, the workgroup's NG groups of LPR lanes take the
-// parts in turn.  Latency-bound: 2.5-4.6 us (where the sequence's parts lie, then their states and
+// parts in turn.  Latency-bound: 2.5-4.7 us (where the sequence's parts lie, then their states and
 // rows at once).
 constexpr int kJoinThreads = 256;
 template <int D>
