@@ -73,8 +73,8 @@ MALA_HOST_DEVICE inline bool paged_may_retain(float mt, float run, float thr2) {
 
 // Where a KV head has more than 16 query heads, its chunks of 16 read the same K and V: workgroups
 // kXcds places apart run on one XCD and share its L2 (16 x 8192 tokens, 64 heads on 2, when it was
-// taken: 50.6 us with the chunks next to each other, 35.4 so; 36.5 now, with a third term of P).  The item (block of a sequence, KV head) and the
-// chunk at a place:
+// taken: 50.6 us with the chunks next to each other, 35.4 so; 36.5 now, with a third term of P).
+// The item (block of a sequence, KV head) and the chunk at a place:
 MALA_HOST_DEVICE inline int paged_item(int place, int nchunk) {
   return nchunk == 1 ? place : place / kXcds / nchunk * kXcds + place % kXcds;
 }
