@@ -61,12 +61,15 @@ typedef enum {
                                 Nq > Nk, tau < 0 or NaN, scale not finite or <= 0,
                                 num_splits < 1, an output type not MALA_OUT_*; paged cache:
                                 misaligned rows, a stride below D, split_tokens not a
-                                positive multiple of B_k, outputs that are inputs */
+                                positive multiple of B_k, outputs that are inputs; rotary
+                                positions: a layout not MALA_ROPE_*, rotary_dim not in
+                                1 .. D, a scale that is not finite */
   MALA_ERR_UNSUPPORTED = -2, /* head_dim not in {64, 128}, causal == 0 (the paper's
                                 traversal is defined for causal attention only), a
                                 forward/backward K/V slice of 2^32 bytes or more, a page
                                 size that is not a multiple of 16, or a pool, table or
-                                grid of 2^31 tokens, entries or workgroups or more */
+                                grid of 2^31 tokens, entries or workgroups or more, a
+                                rotary_dim that is not a multiple of 16 */
   MALA_ERR_WORKSPACE = -3,   /* workspace NULL or smaller than the *_workspace_size query */
   MALA_ERR_HIP = -4          /* a HIP launch/runtime call failed; see mala_last_error() */
 } mala_status;
@@ -302,6 +305,53 @@ int mala_decode_noalloc(const void* q, const void* k_cache, const void* v_cache,
                         float scale, float tau, int out_dtype, void* stream);
 
 /*
+ * Rotary positions of queries and keys, and of their gradients.
+ *
+ * A row at position n turns pair i < rotary_dim / 2 by theta = n x inv_freq[i]:
+ *   (a, b) -> scale x (a cos theta - b sin theta, b cos theta + a sin theta)
+ * and elements from rotary_dim on stay as they are.  Pairs are elements i and i + rotary_dim / 2
+ * (MALA_ROPE_HALF) or 2 i and 2 i + 1 (MALA_ROPE_INTERLEAVED).
+ *   positions: int32 device array, token t of batch b at [b x positions_batch_stride + t] (0: the
+ *       same for every batch); any value, negative ones too.  NULL: token t is at position t.
+ *   inv_freq: double [rotary_dim / 2] device array, radians per position, scaled as a longer
+ *       context needs.  The angle is reduced in 64 bits, so that cos and sin are right to fp32 at
+ *       any position (for |theta| below 2^50).
+ *   rotary_dim: a multiple of 16, at most D.  scale: finite; of the turned elements alone.
+ * The structs here are host memory, read during the call.
+ */
+enum { MALA_ROPE_HALF = 0, MALA_ROPE_INTERLEAVED = 1 };
+typedef struct {
+  const int32_t* positions;
+  int64_t positions_batch_stride;
+  const double* inv_freq;
+  int32_t rotary_dim;
+  int32_t layout; /* MALA_ROPE_* */
+  float scale;
+} mala_rope_t;
+
+/* Rows to turn: D contiguous elements at element b x batch_stride + h x head_stride + t x
+ * token_stride of x, and of out for the result; pointers 16-byte aligned, strides multiples of 16
+ * bytes (those of out at least D; of an axis of one entry, any).  out is x with the same strides
+ * (in place), or memory between whose first and last byte none of x lies.  Outputs share no row with
+ * each other or with the other tensor's x. */
+typedef struct {
+  const void* x;
+  void* out;
+  int64_t x_batch_stride, x_head_stride, x_token_stride;
+  int64_t out_batch_stride, out_head_stride, out_token_stride;
+  int32_t heads;
+} mala_rope_rows_t;
+
+/*
+ * Turns the rows of q and, unless k is NULL, of k, in one launch: B x heads x T rows each of D (64
+ * or 128).  in_dtype, out_dtype: MALA_OUT_* of all x and of all out; computed in fp32 and rounded
+ * once.  inverse = 1: by -theta, which is the transposed map (the scale stays): the gradients of
+ * the turned q and k become those of q and k.  B and T may be 0.
+ */
+int mala_rope(const mala_rope_rows_t* q, const mala_rope_rows_t* k, const mala_rope_t* rope, int B,
+              int T, int D, int in_dtype, int out_dtype, int inverse, void* stream);
+
+/*
  * Paged KV cache.
  *
  * K and V rows of every sequence live in pages of page_size tokens of one pool, so that
@@ -310,14 +360,18 @@ int mala_decode_noalloc(const void* q, const void* k_cache, const void* v_cache,
  * page_size] * page_size + i % page_size.  The functions that belong together:
  *   mala_paged_update  page tables, slots and positions of a step from the lengths
  *   mala_paged_write   new K / V rows into their slots
+ *   mala_paged_rope_write  the same of keys to be rotated, with the step's queries
  *   mala_paged_read    cached rows of a packed batch, for mala_fwd_varlen (prefill against
  *                      cached keys)
  *   mala_paged_decode  mala_decode over the pages
  */
 
 /* Element type of a cache: bf16, or OCP e4m3 (4 exponent, 3 mantissa bits, no infinities)
- * with one fp32 scale per KV head, an element standing for e4m3 value x scale. */
-enum { MALA_CACHE_BF16 = 0, MALA_CACHE_E4M3 = 1 };
+ * with one fp32 scale per KV head, an element standing for e4m3 value x scale; or e4m3 in blocks:
+ * MALA_SCALE_BLOCK rows of a page, from a multiple of that on, of one KV head share a scale 2^e
+ * that the writes find by themselves, for K and for V. */
+enum { MALA_CACHE_BF16 = 0, MALA_CACHE_E4M3 = 1, MALA_CACHE_E4M3_BLOCK = 2 };
+enum { MALA_SCALE_BLOCK = 16 };
 
 /* The pool: row r of page i, KV head h starts at element i * page_stride + h * head_stride +
  * r * token_stride of k_pages and of v_pages (both the same strides; the D elements of a row
@@ -326,8 +380,11 @@ enum { MALA_CACHE_BF16 = 0, MALA_CACHE_E4M3 = 1 };
  * of 16 bytes, at least D elements, 16 rows (16 x token_stride) take less than 2^31 bytes, and
  * all pages and all heads (num_pages x page_stride, Hkv x head_stride) at most 2^60 bytes.
  * page_size is a multiple of 16, D 64 or 128, num_pages x page_size below 2^31.
- * k_scale, v_scale: fp32 [Hkv] device arrays of an e4m3 cache, NULL for scales of 1 (and for
- * bf16).  The struct itself is host memory, read during the call. */
+ * k_scale, v_scale: fp32 [Hkv] device arrays of a MALA_CACHE_E4M3, NULL for scales of 1 (and for
+ * the others).  k_block_scale, v_block_scale: [num_pages, Hkv, page_size / MALA_SCALE_BLOCK] device
+ * arrays of a MALA_CACHE_E4M3_BLOCK, e + 127 a byte (OCP e8m0), e in [-117, 120] (bytes outside are
+ * read as the nearer end); not read for the other types.  Value x scale is a bf16 exactly.  The
+ * struct itself is host memory, read during the call. */
 typedef struct {
   void* k_pages;
   void* v_pages;
@@ -341,6 +398,8 @@ typedef struct {
   int32_t Hkv;
   int32_t D;
   int32_t dtype; /* MALA_CACHE_* */
+  uint8_t* k_block_scale;
+  uint8_t* v_block_scale;
 } mala_paged_cache_t;
 
 /*
@@ -390,10 +449,30 @@ int mala_paged_update(const int32_t* lens, const int32_t* new_lens, int32_t* blo
  *   e4m3: value / scale in fp32, rounded to nearest even, values beyond +-448 to +-448; NaN
  *   stays NaN.  num_tokens may be 0; num_tokens rows of one head are below 2^36 bytes of the
  *   cache.
+ *   e4m3 in blocks: e is the least integer with |x| <= 448 x 2^e for every finite x of the block's new
+ *   rows (at least -117).  A block that gets its row 0 starts anew with that e; any other keeps its e
+ *   or takes the larger one, and if it grew every other row of the block is rounded again under the
+ *   new scale.  Values are rounded to nearest even; infinities become the largest value (448 x 2^e; 240
+ *   x 2^120), NaN stays NaN.  Neither the pages nor the scales need a value before a block's row 0 has
+ *   been written; after that its other rows mean nothing until they are.  The tokens of one block in
+ *   a call (slots of it) lie within 64 consecutive tokens; two calls that run at the same time write
+ *   to different blocks.
  */
 int mala_paged_write(const void* k_new, const void* v_new, int64_t new_token_stride,
                      int64_t new_head_stride, const int32_t* slots,
                      const mala_paged_cache_t* cache, int num_tokens, void* stream);
+
+/*
+ * The keys and values of a step into the cache and its queries rotated, in one launch: the keys turn
+ * as mala_rope turns them (the same bits, a bf16 each), and go to their slots with the values as by
+ * mala_paged_write; the queries' rows (bf16, of num_tokens tokens; q may be NULL) turn from q->x to
+ * q->out (batch strides are not used).  rope: one position per token.  What mala_rope,
+ * mala_paged_write and the cache's type ask for holds here.
+ */
+int mala_paged_rope_write(const mala_rope_rows_t* q, const void* k_new, const void* v_new,
+                          int64_t new_token_stride, int64_t new_head_stride, const int32_t* slots,
+                          const mala_rope_t* rope, const mala_paged_cache_t* cache, int num_tokens,
+                          void* stream);
 
 /*
  * Cached rows of a packed batch, contiguous: k, v: bf16 [Hkv, total, D] out, the layout of
@@ -401,7 +480,7 @@ int mala_paged_write(const void* k_new, const void* v_new, int64_t new_token_str
  * cu_seqlens[b] .. (int32 [num_seqs + 1], non-decreasing, inside [0, total]; a run longer than
  * max_seqlen is cut to its first max_seqlen rows).  Rows that no sequence covers are not
  * written.  Rows of a page whose table entry is outside [0, num_pages) are zeros.  e4m3: value
- * x scale in fp32, rounded to bf16 (nearest even).
+ * x scale in fp32, rounded to bf16 (nearest even; exact for blocks).
  *   block_table: int32 [num_seqs, max_pages]; max_seqlen <= max_pages * page_size.
  *   total * D * 2 < 2^32, as for mala_fwd_varlen.
  */

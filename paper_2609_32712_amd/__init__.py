@@ -9,14 +9,18 @@ Low-level functions carry the C names and arguments (mala_fwd, mala_bwd,
 mala_fwd_varlen, mala_bwd_varlen, mala_decode, mala_decode_noalloc, mala_geometry,
 mala_bwd_workspace_size, mala_bwd_varlen_workspace_size, mala_decode_workspace_size, and for
 a paged KV cache mala_paged_update, mala_paged_write, mala_paged_read, mala_paged_decode,
-mala_paged_decode_workspace_size); fwd / bwd / fwd_varlen / bwd_varlen / decode and
-paged_update / paged_read / paged_decode allocate their outputs and return them in a dict.
+mala_paged_decode_workspace_size; rotary positions: mala_rope, and with the write into a paged
+cache mala_paged_rope_write); fwd / bwd / fwd_varlen / bwd_varlen / decode, rope / rope_bwd and
+paged_update / paged_rope_write / paged_read / paged_decode allocate their outputs and return
+them in a dict.  rope_frequencies makes the frequencies that a rotation takes.
 """
 from __future__ import annotations
 
 import contextlib
 import ctypes
+import math
 import os
+import struct
 
 import torch
 
@@ -35,8 +39,11 @@ EXPORTS = ("mala_geometry", "mala_strerror", "mala_last_error", "mala_fwd",
            "mala_bwd_workspace_size", "mala_bwd", "mala_fwd_varlen", "mala_bwd_varlen",
            "mala_decode_workspace_size", "mala_decode", "mala_decode_noalloc",
            "mala_bwd_varlen_workspace_size", "mala_paged_update", "mala_paged_write",
-           "mala_paged_read", "mala_paged_decode_workspace_size", "mala_paged_decode")
-CACHE_BF16, CACHE_E4M3 = 0, 1
+           "mala_paged_read", "mala_paged_decode_workspace_size", "mala_paged_decode",
+           "mala_rope", "mala_paged_rope_write")
+CACHE_BF16, CACHE_E4M3, CACHE_E4M3_BLOCK = 0, 1, 2
+SCALE_BLOCK = 16                  # MALA_SCALE_BLOCK: rows of a block of a CACHE_E4M3_BLOCK
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
 DECODE_SCRATCH_BYTES = 16 << 20   # MALA_DECODE_SCRATCH_BYTES
 
 
@@ -56,7 +63,12 @@ class _PagedCacheStruct(ctypes.Structure):
                 ("page_stride", ctypes.c_int64), ("head_stride", ctypes.c_int64),
                 ("token_stride", ctypes.c_int64), ("num_pages", ctypes.c_int32),
                 ("page_size", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("D", ctypes.c_int32),
-                ("dtype", ctypes.c_int32)]
+                ("dtype", ctypes.c_int32), ("k_block_scale", ctypes.c_void_p),
+                ("v_block_scale", ctypes.c_void_p)]
+
+
+# The structs of mala_rope as bytes (a ctypes.Structure per call takes longer than a small one).
+_ROPE, _ROPE_ROWS = struct.Struct("PqPiif4x"), struct.Struct("PPqqqqqqi4x")
 
 
 _lib = None
@@ -107,6 +119,11 @@ def load_library():
     lib.mala_paged_decode_workspace_size.restype = sz
     lib.mala_paged_decode.argtypes = [vp, cache] + [vp] * 6 + [i, vp, sz] + [i] * 4 + [f, f, i, vp]
     lib.mala_paged_decode.restype = i
+    text = ctypes.c_char_p
+    lib.mala_rope.argtypes = [text] * 3 + [i] * 6 + [vp]
+    lib.mala_rope.restype = i
+    lib.mala_paged_rope_write.argtypes = [text, vp, vp, i64, i64, vp, text, cache, i, vp]
+    lib.mala_paged_rope_write.restype = i
     _lib = lib
     return lib
 
@@ -371,7 +388,9 @@ class PagedCache:
     """The pages of a KV cache: k_pages and v_pages [num_pages, Hkv, page_size, D], bf16 or
     float8_e4m3fn, with the same strides, rows of D contiguous (views of other orders will
     do, e.g. of [num_pages, page_size, Hkv, D], or of K and V in one tensor).  k_scale and
-    v_scale: fp32 [Hkv] of an e4m3 cache (an element stands for its value x scale; None: 1).
+    v_scale: fp32 [Hkv] of an e4m3 cache (an element stands for its value x scale; None: 1), or
+    float8_e8m0fnu [num_pages, Hkv, page_size / SCALE_BLOCK], contiguous: a scale for each block of
+    SCALE_BLOCK rows and head, which the writes find (the tensors need no value before).
 
     Kept by the caller for as long as the cache lives; it holds the tensors, which stay the ones
     it was made with, and the calls below take it.  page_size is a multiple of 16, D 64 or
@@ -387,8 +406,18 @@ class PagedCache:
             raise ValueError("v_pages must have the shape and strides of k_pages")
         if D > 1 and k_pages.stride(3) != 1:
             raise ValueError("the rows of k_pages must be contiguous")
-        _spec(k_scale, "k_scale", torch.float32, (Hkv,), optional=True)
-        _spec(v_scale, "v_scale", torch.float32, (Hkv,), optional=True)
+        code = _CACHE[k_pages.dtype]
+        blocks = any(getattr(s, "dtype", None) is torch.float8_e8m0fnu for s in (k_scale, v_scale))
+        if blocks:
+            if code != CACHE_E4M3:
+                raise TypeError("scales of blocks need pages of %s" % torch.float8_e4m3fn)
+            code = CACHE_E4M3_BLOCK
+            shape = (N, Hkv, P // SCALE_BLOCK)
+            _spec(k_scale, "k_scale", torch.float8_e8m0fnu, shape)
+            _spec(v_scale, "v_scale", torch.float8_e8m0fnu, shape)
+        else:
+            _spec(k_scale, "k_scale", torch.float32, (Hkv,), optional=True)
+            _spec(v_scale, "v_scale", torch.float32, (Hkv,), optional=True)
         _on_device((("k_pages", k_pages), ("v_pages", v_pages), ("k_scale", k_scale),
                     ("v_scale", v_scale)))
         self.k_pages, self.v_pages, self.k_scale, self.v_scale = k_pages, v_pages, k_scale, v_scale
@@ -396,9 +425,10 @@ class PagedCache:
         self.device = k_pages.get_device()
         # (the stride of an axis of one entry is never used)
         st = [k_pages.stride(i) if k_pages.shape[i] > 1 else max(D, 16) for i in range(3)]
-        self._struct = _PagedCacheStruct(
-            k_pages.data_ptr(), v_pages.data_ptr(), _addr(k_scale), _addr(v_scale), st[0], st[1],
-            st[2], N, P, Hkv, D, _CACHE[k_pages.dtype])
+        scales = _addr(k_scale), _addr(v_scale)
+        heads, per_block = ((None, None), scales) if blocks else (scales, (None, None))
+        self._struct = _PagedCacheStruct(k_pages.data_ptr(), v_pages.data_ptr(), *heads, st[0], st[1],
+                                         st[2], N, P, Hkv, D, code, *per_block)
         self._ref = ctypes.byref(self._struct)
 
     # The addresses that the calls use were taken from these tensors: others in their place would
@@ -501,10 +531,8 @@ def mala_paged_update(lens, new_lens, block_table, free_ring, free_state, lens_o
             _int32(num_pages, "num_pages"), C, T)
 
 
-def mala_paged_write(k_new, v_new, slots, cache, stream=None):
-    """k_new, v_new: bf16 [Hkv, T, D] with the same strides, rows of D contiguous (e.g. the
-    transposed slices of a [T, 2, Hkv, D] projection); slots: int32 [T]."""
-    c = _cache(cache)
+def _new_rows(k_new, v_new, slots, c):
+    """The checks of the rows that a write takes; (T, token stride, head stride)."""
     Hkv, T, D = _shape(k_new, "k_new", 3)
     _shape(v_new, "v_new", 3)
     if k_new.dtype != torch.bfloat16 or v_new.dtype != torch.bfloat16:
@@ -513,16 +541,104 @@ def mala_paged_write(k_new, v_new, slots, cache, stream=None):
     if Hkv != c.Hkv or D != c.D:
         raise ValueError("k_new must have shape %s, got %s" % ((c.Hkv, T, c.D), (Hkv, T, D)))
     st = k_new.stride()
-    if v_new.shape != k_new.shape or v_new.stride() != st:
+    if v_new.shape != k_new.shape or (v_new.stride() != st and T):
         raise ValueError("v_new must have the shape and strides of k_new")
-    if st[2] != 1:
+    if st[2] != 1 and T:
         raise ValueError("the rows of k_new must be contiguous")
     if k_new.get_device() != c.device or v_new.get_device() != c.device:
         raise TypeError("k_new and v_new must be CUDA (HIP) tensors on the device of the cache")
     _args(c.device, (slots, "slots", torch.int32, (T,)))
+    return T, st[1] if T > 1 else D, st[0] if Hkv > 1 else D
+
+
+def mala_paged_write(k_new, v_new, slots, cache, stream=None):
+    """k_new, v_new: bf16 [Hkv, T, D] with the same strides, rows of D contiguous (e.g. the
+    transposed slices of a [T, 2, Hkv, D] projection); slots: int32 [T].
+
+    Of a cache with scales of blocks, the tokens of one block have to lie within 64 consecutive
+    tokens (as paged_update packs them); the block's scale is found or raised as they come."""
+    c = _cache(cache)
+    T, token_stride, head_stride = _new_rows(k_new, v_new, slots, c)
     _launch(c.device, stream, (_lib or load_library()).mala_paged_write, k_new.data_ptr(),
-            v_new.data_ptr(), st[1] if T > 1 else D, st[0] if Hkv > 1 else D, slots.data_ptr(),
-            c._ref, T)
+            v_new.data_ptr(), token_stride, head_stride, slots.data_ptr(), c._ref, T)
+
+
+def _rope_rows(x, out, name, shape, dtypes, device):
+    """The bytes of a mala_rope_rows_t of x and out [(B,) H, T, D], rows contiguous."""
+    if not isinstance(out, torch.Tensor) or out.shape != shape:
+        raise ValueError("%s_out must have shape %s" % (name, tuple(shape)))
+    if (x.dtype, out.dtype) != dtypes:
+        raise TypeError("%s and %s_out must have dtypes %s, got %s"
+                        % (name, name, dtypes, (x.dtype, out.dtype)))
+    if x.get_device() != device or out.get_device() != device or device < 0:
+        raise TypeError("%s and %s_out must be CUDA (HIP) tensors on the device of the others"
+                        % (name, name))
+    a, b = x.stride(), out.stride()
+    if (a[-1] != 1 or b[-1] != 1) and x.numel():
+        raise ValueError("the rows of %s and %s_out must be contiguous" % (name, name))
+    if len(shape) == 3:
+        a, b = (0, *a), (0, *b)
+    return _ROPE_ROWS.pack(x.data_ptr(), out.data_ptr(), a[0], a[1], a[2], b[0], b[1], b[2], shape[-3])
+
+
+def _rope_turn(positions, inv_freq, layout, scale, B, T, device):
+    """The bytes of a mala_rope_t; positions [T], [B, T] or None."""
+    _args(device, (inv_freq, "inv_freq", torch.float64, _shape(inv_freq, "inv_freq", 1)))
+    at, stride = None, 0
+    if positions is not None:
+        if isinstance(positions, torch.Tensor) and positions.dim() == 2:
+            stride = T
+        _args(device, (positions, "positions", torch.int32, (B, T) if stride else (T,)))
+        at = positions.data_ptr()
+    return _ROPE.pack(at or 0, stride, inv_freq.data_ptr(), 2 * inv_freq.shape[0], layout, scale)
+
+
+def mala_rope(q, k, q_out, k_out, positions, inv_freq, layout=ROPE_HALF, scale=1.0, inverse=False,
+              stream=None):
+    """q [B, Hq, T, D] or [Hq, T, D] and, unless it is None, k of Hkv heads, bf16 or fp32, rows of D
+    contiguous and other strides free, into q_out and k_out (bf16 or fp32; q_out may be q, k_out k).
+    positions: int32 [T] or [B, T], None for 0 .. T - 1; inv_freq: float64 [rotary_dim / 2] on the
+    device (rope_frequencies); scale: of the turned part; inverse: the transposed rotation, which
+    takes the gradients of q_out and k_out to those of q and k."""
+    if not isinstance(q, torch.Tensor) or q.dim() not in (3, 4):
+        raise ValueError("q must be a [B, H, T, D] or [H, T, D] tensor")
+    shape, dev = q.shape, _device(q, "q")
+    B, T, D = shape[0] if len(shape) == 4 else 1, shape[-2], shape[-1]
+    if not isinstance(q_out, torch.Tensor) or q.dtype not in _OUT or q_out.dtype not in _OUT:
+        raise TypeError("q and q_out must be tensors of dtype %s" % (_OUT,))
+    dtypes = q.dtype, q_out.dtype
+    rows, more = _rope_rows(q, q_out, "q", shape, dtypes, dev), None
+    if k is not None:
+        if not isinstance(k, torch.Tensor) or k.dim() != len(shape) or (B, T, D) != (
+                k.shape[0] if len(shape) == 4 else 1, k.shape[-2], k.shape[-1]):
+            raise ValueError("k must have the batch, tokens and head size of q")
+        more = _rope_rows(k, k_out, "k", k.shape, dtypes, dev)
+    elif k_out is not None:
+        raise ValueError("k_out without k")
+    turn = _rope_turn(positions, inv_freq, layout, scale, B, T, dev)
+    _launch(dev, stream, (_lib or load_library()).mala_rope, rows, more, turn, B, T, D,
+            OUT_BF16 if dtypes[0] is torch.bfloat16 else OUT_F32,
+            OUT_BF16 if dtypes[1] is torch.bfloat16 else OUT_F32, 1 if inverse else 0)
+
+
+def mala_paged_rope_write(q, q_out, k_new, v_new, positions, slots, cache, inv_freq, layout=ROPE_HALF,
+                          scale=1.0, stream=None):
+    """mala_rope of a step's queries (bf16 [Hq, T, D] into q_out, both None for none) and keys, and
+    mala_paged_write of the turned keys and the values, in one launch and with their results.
+    positions, slots: int32 [T]."""
+    c = _cache(cache)
+    T, token_stride, head_stride = _new_rows(k_new, v_new, slots, c)
+    rows = None
+    if q is not None:
+        shape = _shape(q, "q", 3)
+        if shape[1] != T or shape[2] != c.D:
+            raise ValueError("q must have %d tokens of %d, got shape %s" % (T, c.D, tuple(shape)))
+        rows = _rope_rows(q, q_out, "q", shape, (torch.bfloat16, torch.bfloat16), c.device)
+    elif q_out is not None:
+        raise ValueError("q_out without q")
+    turn = _rope_turn(positions, inv_freq, layout, scale, 1, T, c.device)
+    _launch(c.device, stream, (_lib or load_library()).mala_paged_rope_write, rows, k_new.data_ptr(),
+            v_new.data_ptr(), token_stride, head_stride, slots.data_ptr(), turn, c._ref, T)
 
 
 def mala_paged_read(cache, block_table, cu_seqlens, max_seqlen, k, v, stream=None):
@@ -657,6 +773,60 @@ def default_num_splits(B, Hkv, Nk, num_cus=256, waves_per_simd=2):
     return int(max(1, min(want, tiles // 16 if tiles >= 16 else 1)))
 
 
+# ---------------------------------------------------------------- rotary positions
+def rope_frequencies(rotary_dim, base=10000.0, factor=1.0, scaling="none", original_len=None,
+                     beta_fast=32.0, beta_slow=1.0, device=None):
+    """(inv_freq, scale) of a rotation of rotary_dim elements: float64 [rotary_dim / 2] on the device
+    and the factor of the turned part, for a context `factor` times the one trained on.
+
+    "none": base^(-2 i / rotary_dim).  "linear": those over factor.  "ntk": of the base times
+    factor^(rotary_dim / (rotary_dim - 2)), which leaves the fastest as it is and takes the slowest
+    to 1 / factor.  "yarn": by parts, after the turns that a frequency makes over original_len
+    tokens: from beta_fast turns on as they are, up to beta_slow over factor, linear in the turns
+    between; scale 0.1 ln(factor) + 1."""
+    if rotary_dim <= 0 or rotary_dim % 2:
+        raise ValueError("rotary_dim (%s) must be positive and even" % rotary_dim)
+    if not (base > 0 and math.isfinite(base)) or not (factor > 0 and math.isfinite(factor)):
+        raise ValueError("base and factor must be finite and above 0")
+    if scaling == "ntk":
+        if rotary_dim <= 2:
+            raise ValueError("ntk needs rotary_dim above 2")
+        base = base * factor ** (rotary_dim / (rotary_dim - 2))
+    f = float(base) ** (-2.0 * torch.arange(rotary_dim // 2, dtype=torch.float64) / rotary_dim)
+    scale = 1.0
+    if scaling == "linear":
+        f = f / factor
+    elif scaling == "yarn":
+        if original_len is None or not original_len > 0 or not beta_fast > beta_slow:
+            raise ValueError("yarn needs original_len above 0 and beta_fast above beta_slow")
+        keep = ((original_len * f / (2 * math.pi) - beta_slow) / (beta_fast - beta_slow)).clamp(0.0, 1.0)
+        f = f * keep + f / factor * (1.0 - keep)
+        scale = 0.1 * math.log(factor) + 1.0 if factor > 1 else 1.0
+    elif scaling not in ("none", "ntk"):
+        raise ValueError("scaling must be none, linear, ntk or yarn, got %r" % (scaling,))
+    return f.to(device), scale
+
+
+def rope(q, k, positions, inv_freq, layout=ROPE_HALF, scale=1.0, out_dtype=torch.bfloat16, stream=None):
+    """q [B, Hq, T, D] or [Hq, T, D] and k (or None) at their positions, contiguous: a dict of q and
+    k for fwd / fwd_varlen (see mala_rope)."""
+    with _on_stream(stream):
+        q_out = torch.empty(q.shape, dtype=out_dtype, device=q.device)
+        k_out = None if k is None else torch.empty(k.shape, dtype=out_dtype, device=q.device)
+    mala_rope(q, k, q_out, k_out, positions, inv_freq, layout, scale, stream=stream)
+    return dict(q=q_out, k=k_out)
+
+
+def rope_bwd(dq, dk, positions, inv_freq, layout=ROPE_HALF, scale=1.0, grad_dtype=torch.float32, stream=None):
+    """Gradients of what rope took, from those of what it gave (e.g. dq and dk of bwd): a dict of dq
+    and dk."""
+    with _on_stream(stream):
+        q = torch.empty(dq.shape, dtype=grad_dtype, device=dq.device)
+        k = None if dk is None else torch.empty(dk.shape, dtype=grad_dtype, device=dq.device)
+    mala_rope(dq, dk, q, k, positions, inv_freq, layout, scale, inverse=True, stream=stream)
+    return dict(dq=q, dk=k)
+
+
 # ---------------------------------------------------------------- paged KV cache, allocating
 def _on_stream(stream):
     """Allocations inside belong to the stream the kernels run on, so that memory freed when
@@ -682,6 +852,18 @@ def paged_update(lens, new_lens, block_table, free_ring, free_state, max_tokens,
                       out["cu_seqlens"], out["slots"], out["positions"], out["free_state"],
                       page_size, num_pages, stream=stream)
     return out
+
+
+def paged_rope_write(q, k_new, v_new, positions, slots, cache, inv_freq, layout=ROPE_HALF, scale=1.0,
+                     tokens_first=False, stream=None):
+    """A step's keys (turned) and values into the cache, and its queries turned: a dict of q, [Hq, T,
+    D] as q is (for fwd_varlen), or [T, Hq, D] with tokens_first (for paged_decode)."""
+    Hq, T, D = _shape(q, "q", 3)
+    with _on_stream(stream):
+        out = torch.empty((T, Hq, D) if tokens_first else (Hq, T, D), dtype=q.dtype, device=q.device)
+    mala_paged_rope_write(q, out.transpose(0, 1) if tokens_first else out, k_new, v_new, positions, slots,
+                          cache, inv_freq, layout, scale, stream=stream)
+    return dict(q=out)
 
 
 def paged_read(cache, block_table, cu_seqlens, max_seqlen, total, stream=None):

@@ -5,12 +5,14 @@
 #include <stdio.h>
 #include <string.h>
 
+#include <algorithm>
 #include <mutex>
 
 #include "mala.h"
 #include "mala_device.h"
 #include "mala_kernels.h"
 #include "mala_paged.h"
+#include "mala_rope.h"
 
 namespace {
 
@@ -465,17 +467,21 @@ int check_cache(const mala_paged_cache_t* c, mala::PagedCache* out) {
     return fail(MALA_ERR_INVALID_ARG, "null cache, k_pages or v_pages");
   if (c->num_pages <= 0 || c->page_size <= 0 || c->Hkv <= 0)
     return fail(MALA_ERR_INVALID_ARG, "non-positive size (num_pages, page_size, Hkv)");
-  if (c->dtype != MALA_CACHE_BF16 && c->dtype != MALA_CACHE_E4M3)
-    return fail(MALA_ERR_INVALID_ARG, "cache dtype must be MALA_CACHE_BF16 or MALA_CACHE_E4M3, got %d", c->dtype);
-  if (c->dtype == MALA_CACHE_BF16 && (c->k_scale || c->v_scale))
-    return fail(MALA_ERR_INVALID_ARG, "a bf16 cache has no scales");
+  if (c->dtype != MALA_CACHE_BF16 && c->dtype != MALA_CACHE_E4M3 && c->dtype != MALA_CACHE_E4M3_BLOCK)
+    return fail(MALA_ERR_INVALID_ARG, "cache dtype must be a MALA_CACHE_*, got %d", c->dtype);
+  if (c->dtype != MALA_CACHE_E4M3 && (c->k_scale || c->v_scale))
+    return fail(MALA_ERR_INVALID_ARG, "only a MALA_CACHE_E4M3 has scales per head");
+  // (the block scales are behind the fields that a bf16 or e4m3 cache has to give)
+  const bool block = c->dtype == MALA_CACHE_E4M3_BLOCK;
+  if (block && (!c->k_block_scale || !c->v_block_scale))
+    return fail(MALA_ERR_INVALID_ARG, "null k_block_scale or v_block_scale");
   if (c->D != 64 && c->D != 128)
     return fail(MALA_ERR_UNSUPPORTED, "head_dim %d not in {64, 128}", c->D);
   if (c->page_size % mala::kPageRows)
     return fail(MALA_ERR_UNSUPPORTED, "page_size %d is not a multiple of %d", c->page_size, mala::kPageRows);
   if ((int64_t)c->num_pages * c->page_size > INT32_MAX)
     return fail(MALA_ERR_UNSUPPORTED, "num_pages x page_size reaches 2^31");
-  const int64_t size = c->dtype == MALA_CACHE_E4M3 ? 1 : 2;
+  const int64_t size = c->dtype == MALA_CACHE_BF16 ? 2 : 1;
   const int64_t per_16 = 16 / size;       // elements
   for (int64_t s : {c->page_stride, c->head_stride, c->token_stride})
     if (s < c->D || s % per_16)
@@ -500,8 +506,104 @@ int check_cache(const mala_paged_cache_t* c, mala::PagedCache* out) {
     out->num_pages = c->num_pages;
     out->page_size = c->page_size;
     out->Hkv = c->Hkv;
-    out->e4m3 = c->dtype == MALA_CACHE_E4M3;
+    out->kb = block ? c->k_block_scale : nullptr;
+    out->vb = block ? c->v_block_scale : nullptr;
+    out->fmt = block ? mala::kCacheBlock : c->dtype == MALA_CACHE_E4M3 ? mala::kCacheE4M3 : mala::kCacheBf16;
   }
+  return MALA_OK;
+}
+
+// The arguments of a write, and its kernel form (nothing past the cache where there is no token).
+int check_write(const void* k_new, const void* v_new, int64_t new_token_stride, int64_t new_head_stride,
+                const int32_t* slots, const mala_paged_cache_t* cache, int num_tokens,
+                mala::PagedWriteParams* p) {
+  const int st = check_cache(cache, &p->c);
+  if (st) return st;
+  if (num_tokens < 0) return fail(MALA_ERR_INVALID_ARG, "negative num_tokens");
+  if (!num_tokens) return MALA_OK;
+  if (!k_new || !v_new || !slots) return fail(MALA_ERR_INVALID_ARG, "null k_new, v_new or slots");
+  if ((uintptr_t)k_new % 16 || (uintptr_t)v_new % 16 || new_token_stride % 8 || new_head_stride % 8 ||
+      new_token_stride < 0 || new_head_stride < 0)
+    return fail(MALA_ERR_INVALID_ARG, "rows of k_new and v_new must be 16-byte aligned");
+  if (new_token_stride > INT64_MAX / 8 / num_tokens || new_head_stride > INT64_MAX / 8 / cache->Hkv)
+    return fail(MALA_ERR_UNSUPPORTED, "k_new stride too large");
+  // (a thread per 16 bytes of a row of the cache; of blocks, 256 per kBlockChunk tokens)
+  const int threads = p->c.fmt == mala::kCacheBlock ? 256 / mala::kBlockChunk
+                                                    : cache->D / (p->c.fmt == mala::kCacheBf16 ? 8 : 16);
+  if ((int64_t)num_tokens * threads > UINT32_MAX - 255)
+    return fail(MALA_ERR_UNSUPPORTED, "a launch of 2^32 threads or more (num_tokens %d)", num_tokens);
+  p->k = (const char*)k_new;
+  p->v = (const char*)v_new;
+  p->token_stride = new_token_stride * 2;
+  p->head_stride = new_head_stride * 2;
+  p->slots = slots;
+  p->T = num_tokens;
+  p->chunk = 0;
+  return MALA_OK;
+}
+
+// ---------------------------------------------------------------- rotary positions
+int64_t extent(const int64_t stride[3], const int64_t n[3], int64_t row) {
+  int64_t bytes = row;
+  for (int i = 0; i < 3; ++i) bytes += stride[i] * (n[i] - 1);
+  return bytes;
+}
+
+// One tensor's rows, B x heads x T of them (all above 0).
+int check_rows(const mala_rope_rows_t* r, const char* name, int B, int T, int D, int in_size, int out_size,
+               mala::RopeRows* out) {
+  if (!r->x || !r->out) return fail(MALA_ERR_INVALID_ARG, "null x or out of %s", name);
+  if (r->heads <= 0) return fail(MALA_ERR_INVALID_ARG, "non-positive heads of %s", name);
+  if (r->heads > 65535) return fail(MALA_ERR_UNSUPPORTED, "%d heads of %s", r->heads, name);
+  if ((uintptr_t)r->x % 16 || (uintptr_t)r->out % 16)
+    return fail(MALA_ERR_INVALID_ARG, "x or out of %s not 16-byte aligned", name);
+  const int64_t n[3] = {B, r->heads, T};
+  int64_t in[3] = {r->x_batch_stride, r->x_head_stride, r->x_token_stride};
+  int64_t to[3] = {r->out_batch_stride, r->out_head_stride, r->out_token_stride};
+  int64_t in_b[3], to_b[3];
+  for (int i = 0; i < 3; ++i) {
+    if (n[i] == 1) in[i] = to[i] = 0;
+    if (in[i] < 0 || to[i] < 0 || in[i] % (16 / in_size) || to[i] % (16 / out_size))
+      return fail(MALA_ERR_INVALID_ARG, "strides of %s must be multiples of 16 bytes, not negative", name);
+    // every axis below 2^60 bytes (compared by division)
+    constexpr int64_t kMost = (int64_t)1 << 60;
+    if (in[i] > kMost / in_size / n[i] || to[i] > kMost / out_size / n[i])
+      return fail(MALA_ERR_UNSUPPORTED, "stride of %s too large", name);
+    // rows of an output that share memory would be written by several threads
+    if (n[i] > 1 && to[i] < D)
+      return fail(MALA_ERR_INVALID_ARG, "rows of the output of %s overlap", name);
+    in_b[i] = in[i] * in_size;
+    to_b[i] = to[i] * out_size;
+  }
+  bool same = r->x == r->out && in_size == out_size;
+  for (int i = 0; i < 3; ++i) same = same && in[i] == to[i];
+  const uintptr_t a = (uintptr_t)r->x, b = (uintptr_t)r->out;
+  if (!same && a < b + extent(to_b, n, (int64_t)D * out_size) && b < a + extent(in_b, n, (int64_t)D * in_size))
+    return fail(MALA_ERR_INVALID_ARG, "the output of %s meets its input without being it", name);
+  *out = {(const char*)r->x, (char*)r->out, in_b[0], in_b[1], in_b[2], to_b[0], to_b[1], to_b[2], r->heads};
+  return MALA_OK;
+}
+
+int check_turn(const mala_rope_t* rope, int B, int T, int D, int inverse, mala::Turn* out) {
+  if (!rope || !rope->inv_freq) return fail(MALA_ERR_INVALID_ARG, "null rope or inv_freq");
+  if (D != 64 && D != 128) return fail(MALA_ERR_UNSUPPORTED, "head_dim %d not in {64, 128}", D);
+  if (rope->layout != MALA_ROPE_HALF && rope->layout != MALA_ROPE_INTERLEAVED)
+    return fail(MALA_ERR_INVALID_ARG, "layout must be a MALA_ROPE_*, got %d", rope->layout);
+  if (rope->rotary_dim <= 0 || rope->rotary_dim > D)
+    return fail(MALA_ERR_INVALID_ARG, "rotary_dim %d not in 1 .. %d", rope->rotary_dim, D);
+  if (rope->rotary_dim % 16) return fail(MALA_ERR_UNSUPPORTED, "rotary_dim %d is not a multiple of 16", rope->rotary_dim);
+  if (!isfinite(rope->scale)) return fail(MALA_ERR_INVALID_ARG, "scale of the rotation must be finite");
+  if ((uintptr_t)rope->inv_freq % 8 || (uintptr_t)rope->positions % 4)
+    return fail(MALA_ERR_INVALID_ARG, "inv_freq or positions misaligned");
+  if (rope->positions_batch_stride < 0)
+    return fail(MALA_ERR_INVALID_ARG, "negative positions_batch_stride");
+  if (rope->positions_batch_stride > ((int64_t)1 << 58) / std::max(B, 1))
+    return fail(MALA_ERR_UNSUPPORTED, "positions_batch_stride too large");
+  // (D / 16 threads per row)
+  if ((int64_t)B * T > (UINT32_MAX - 255) / (D / 16))
+    return fail(MALA_ERR_UNSUPPORTED, "a launch of 2^32 threads or more (%d x %d tokens)", B, T);
+  *out = {rope->positions, rope->positions_batch_stride, rope->inv_freq, rope->rotary_dim,
+          rope->layout == MALA_ROPE_INTERLEAVED, rope->scale, inverse ? -rope->scale : rope->scale};
   return MALA_OK;
 }
 
@@ -560,27 +662,49 @@ int mala_paged_write(const void* k_new, const void* v_new, int64_t new_token_str
                      const mala_paged_cache_t* cache, int num_tokens, void* stream) {
   g_err[0] = 0;
   mala::PagedWriteParams p;
-  int st = check_cache(cache, &p.c);
-  if (st) return st;
-  if (num_tokens < 0) return fail(MALA_ERR_INVALID_ARG, "negative num_tokens");
-  if (!num_tokens) return MALA_OK;
-  if (!k_new || !v_new || !slots) return fail(MALA_ERR_INVALID_ARG, "null k_new, v_new or slots");
-  if ((uintptr_t)k_new % 16 || (uintptr_t)v_new % 16 || new_token_stride % 8 || new_head_stride % 8 ||
-      new_token_stride < 0 || new_head_stride < 0)
-    return fail(MALA_ERR_INVALID_ARG, "rows of k_new and v_new must be 16-byte aligned");
-  if (new_token_stride > INT64_MAX / 8 / num_tokens || new_head_stride > INT64_MAX / 8 / cache->Hkv)
-    return fail(MALA_ERR_UNSUPPORTED, "k_new stride too large");
-  // (a thread per 16 bytes of a row of the cache)
-  if ((int64_t)num_tokens * (cache->D / (p.c.e4m3 ? 16 : 8)) > UINT32_MAX - 255)
-    return fail(MALA_ERR_UNSUPPORTED, "a launch of 2^32 threads or more (num_tokens %d)", num_tokens);
-  p.k = (const char*)k_new;
-  p.v = (const char*)v_new;
-  p.token_stride = new_token_stride * 2;
-  p.head_stride = new_head_stride * 2;
-  p.slots = slots;
-  p.T = num_tokens;
+  const int st = check_write(k_new, v_new, new_token_stride, new_head_stride, slots, cache, num_tokens, &p);
+  if (st || !num_tokens) return st;
   const hipError_t e = mala::launch_paged_write(p, cache->D, (hipStream_t)stream);
   return e == hipSuccess ? MALA_OK : hip_fail(e, "mala_paged_write: kernel launch");
+}
+
+int mala_rope(const mala_rope_rows_t* q, const mala_rope_rows_t* k, const mala_rope_t* rope, int B, int T,
+              int D, int in_dtype, int out_dtype, int inverse, void* stream) {
+  g_err[0] = 0;
+  if (!q) return fail(MALA_ERR_INVALID_ARG, "null q");
+  if (B < 0 || T < 0) return fail(MALA_ERR_INVALID_ARG, "negative size (B, T)");
+  mala::RopeParams p = {};
+  int st = check_turn(rope, B, T, D, inverse, &p.turn);
+  if (!st) st = check_dtype(in_dtype, "in_dtype");
+  if (!st) st = check_dtype(out_dtype, "out_dtype");
+  if (st || !B || !T) return st;
+  const int in_size = in_dtype == MALA_OUT_BF16 ? 2 : 4, out_size = out_dtype == MALA_OUT_BF16 ? 2 : 4;
+  if ((st = check_rows(q, "q", B, T, D, in_size, out_size, &p.r[0]))) return st;
+  if (k && (st = check_rows(k, "k", B, T, D, in_size, out_size, &p.r[1]))) return st;
+  p.B = B;
+  p.T = T;
+  const hipError_t e = mala::launch_rope(p, D, in_size == 4, out_size == 4, (hipStream_t)stream);
+  return e == hipSuccess ? MALA_OK : hip_fail(e, "mala_rope: kernel launch");
+}
+
+int mala_paged_rope_write(const mala_rope_rows_t* q, const void* k_new, const void* v_new,
+                          int64_t new_token_stride, int64_t new_head_stride, const int32_t* slots,
+                          const mala_rope_t* rope, const mala_paged_cache_t* cache, int num_tokens,
+                          void* stream) {
+  g_err[0] = 0;
+  mala::PagedRopeWriteParams p = {};
+  int st = check_write(k_new, v_new, new_token_stride, new_head_stride, slots, cache, num_tokens, &p.w);
+  if (!st) st = check_turn(rope, 1, num_tokens, cache->D, 0, &p.q.turn);
+  if (st || !num_tokens) return st;
+  if (q && (st = check_rows(q, "q", 1, num_tokens, cache->D, 2, 2, &p.q.r[0]))) return st;
+  p.q.B = 1;
+  p.q.T = num_tokens;
+  // a workgroup per rope_tokens(D) tokens, and per head at most; in one dimension
+  const double groups = ((double)num_tokens / mala::rope_tokens(cache->D) + 1) *
+                            (p.q.r[0].H + 2.0 * cache->Hkv) + num_tokens / mala::kBlockChunk + 2048;
+  if (groups * 256 > UINT32_MAX) return fail(MALA_ERR_UNSUPPORTED, "a launch of 2^32 threads or more");
+  const hipError_t e = mala::launch_paged_rope_write(p, cache->D, (hipStream_t)stream);
+  return e == hipSuccess ? MALA_OK : hip_fail(e, "mala_paged_rope_write: kernel launch");
 }
 
 int mala_paged_read(const mala_paged_cache_t* cache, const int32_t* block_table,

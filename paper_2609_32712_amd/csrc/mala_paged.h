@@ -3,12 +3,20 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include "mala_device.h"
 #include "mala_paged_dispatch.h"
+#include "mala_rope_dispatch.h"
 
 namespace mala {
 
 constexpr int kPageRows = 16;   // page sizes are multiples of this: 16 rows from a multiple of
                                 // 16 on lie in one page, so they share one base address
+
+// What a cache holds: bf16; e4m3 with a scale per KV head; e4m3 with a scale 2^e for each block of
+// kPageRows rows and KV head, e + 127 a byte in [127 + kScaleMin, 127 + kScaleMax] (others read as
+// the nearer of the two): value x scale is then a bf16 that is no subnormal, and finite.
+enum { kCacheBf16 = 0, kCacheE4M3 = 1, kCacheBlock = 2 };
+constexpr int kScaleMin = -117, kScaleMax = 120;
 
 // Pages of K and V: row r of page i, KV head h at byte i * page_stride + h * head_stride +
 // r * token_stride of k and v.  Strides in bytes (multiples of 16).
@@ -17,9 +25,11 @@ struct PagedCache {
   char* v;
   const float* ks;   // [Hkv] e4m3 scales, or null (1)
   const float* vs;
+  uint8_t* kb;       // [num_pages, Hkv, page_size / kPageRows] exponents of a kCacheBlock
+  uint8_t* vb;
   int64_t page_stride, head_stride, token_stride;
   int num_pages, page_size, Hkv;
-  int e4m3;
+  int fmt;           // kCache*
 };
 
 struct PagedUpdateParams {
@@ -43,6 +53,7 @@ struct PagedWriteParams {
   int64_t token_stride, head_stride;
   const int32_t* slots;
   int T;
+  int chunk;            // set by the launch
 };
 
 struct PagedReadParams {
@@ -76,6 +87,18 @@ struct PagedDecParams {
   float scale2, log2tau;
 };
 
+// e4m3 bytes of 4 fp32 values (nearest even; beyond +-448 the largest finite value, NaN stays)
+__device__ __forceinline__ int to_e4m3x4(float a, float b, float c, float d) {
+  const auto lim = [](float x) { return x != x ? x : fminf(fmaxf(x, -448.f), 448.f); };
+  int r = __builtin_amdgcn_cvt_pk_fp8_f32(lim(a), lim(b), 0, false);
+  return __builtin_amdgcn_cvt_pk_fp8_f32(lim(c), lim(d), r, true);
+}
+
+// 2^e of a block's byte, as an fp32's bits
+__device__ __forceinline__ uint32_t block_scale_bits(uint32_t byte) {
+  return min(max(byte, 127u + kScaleMin), 127u + kScaleMax) << 23;
+}
+
 // Inclusive sum over the wavefront's lanes.
 __device__ __forceinline__ int wave_scan(int x) {
   x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);   // row_shr:1
@@ -100,6 +123,7 @@ __device__ __forceinline__ int wave_max(int x) {
 
 hipError_t launch_paged_update(const PagedUpdateParams& p, hipStream_t st);
 hipError_t launch_paged_write(const PagedWriteParams& p, int D, hipStream_t st);
+hipError_t launch_paged_block_write(PagedWriteParams p, int D, hipStream_t st);
 hipError_t launch_paged_read(const PagedReadParams& p, int D, hipStream_t st);
 hipError_t launch_paged_decode(PagedDecParams p, int D, int split_tokens, hipStream_t st);
 

@@ -9,8 +9,6 @@ namespace mala {
 
 namespace {
 
-typedef int i32x2 __attribute__((ext_vector_type(2)));
-
 // Data that a call moves once: past the caches' retention.  (e4m3 rows are read by the write
 // as two halves of 32 bytes per lane, which an ordinary load keeps close for the second.)
 template <class T>
@@ -219,13 +217,6 @@ __global__ __launch_bounds__(NT) void mala_paged_update_kernel(PagedUpdateParams
 }
 
 // ------------------------------------------------------------------ rows into pages
-// e4m3 bytes of 4 fp32 values (nearest even; beyond +-448 the largest finite value, NaN stays)
-__device__ __forceinline__ int to_e4m3x4(float a, float b, float c, float d) {
-  const auto lim = [](float x) { return x != x ? x : fminf(fmaxf(x, -448.f), 448.f); };
-  int r = __builtin_amdgcn_cvt_pk_fp8_f32(lim(a), lim(b), 0, false);
-  return __builtin_amdgcn_cvt_pk_fp8_f32(lim(c), lim(d), r, true);
-}
-
 // A thread moves 16 bytes of a row of the cache, of K and of V; a workgroup stays with a head.
 // HBM-bound.
 template <int D, bool E4M3>
@@ -266,7 +257,7 @@ __global__ __launch_bounds__(256) void mala_paged_write_kernel(PagedWriteParams 
 // ------------------------------------------------------------------ pages to packed rows
 // A workgroup takes kReadRows consecutive packed rows (of every head).  HBM-bound.
 constexpr int kReadRows = 4;
-template <int D, bool E4M3>
+template <int D, int FMT>
 __global__ __launch_bounds__(256) void mala_paged_read_kernel(PagedReadParams p) {
   constexpr int CPR = D / 8;             // pieces of 8 values per row
   __shared__ int s_seq;
@@ -294,7 +285,7 @@ __global__ __launch_bounds__(256) void mala_paged_read_kernel(PagedReadParams p)
 #pragma unroll 4
   for (int h = tid / (CPR * kReadRows); h < Hkv; h += HEADS) {
     const long dst = (((long)h * p.total + row) * D + c * 8) * 2;
-    if constexpr (E4M3) {
+    if constexpr (FMT != kCacheBf16) {
       const long src = at + h * p.c.head_stride + c * 8;
       i32x2 a = {0, 0}, v = a;
       if (there) {
@@ -314,8 +305,18 @@ __global__ __launch_bounds__(256) void mala_paged_read_kernel(PagedReadParams p)
         }
         store_once(out + dst, __builtin_bit_cast(i32x4, y));
       };
-      put(p.k, a, p.c.ks ? p.c.ks[h] : 1.f);
-      put(p.v, v, p.c.vs ? p.c.vs[h] : 1.f);
+      float ks = 1.f, vs = 1.f;
+      if constexpr (FMT == kCacheBlock) {
+        const unsigned blocks = P / kPageRows;
+        const int64_t b = there ? ((int64_t)number * Hkv + h) * blocks + off / kPageRows : 0;
+        ks = __uint_as_float(block_scale_bits(p.c.kb[b]));
+        vs = __uint_as_float(block_scale_bits(p.c.vb[b]));
+      } else {
+        if (p.c.ks) ks = p.c.ks[h];
+        if (p.c.vs) vs = p.c.vs[h];
+      }
+      put(p.k, a, ks);
+      put(p.v, v, vs);
     } else {
       const long src = at + h * p.c.head_stride + c * 16;
       i32x4 a = {0, 0, 0, 0}, v = a;
@@ -350,24 +351,33 @@ static void launch_write_t(const PagedWriteParams& p, hipStream_t st) {
 }
 
 hipError_t launch_paged_write(const PagedWriteParams& p, int D, hipStream_t st) {
+  if (p.c.fmt == kCacheBlock) return launch_paged_block_write(p, D, st);
+  const bool e4m3 = p.c.fmt == kCacheE4M3;
   if (D == 128)
-    p.c.e4m3 ? launch_write_t<128, true>(p, st) : launch_write_t<128, false>(p, st);
+    e4m3 ? launch_write_t<128, true>(p, st) : launch_write_t<128, false>(p, st);
   else
-    p.c.e4m3 ? launch_write_t<64, true>(p, st) : launch_write_t<64, false>(p, st);
+    e4m3 ? launch_write_t<64, true>(p, st) : launch_write_t<64, false>(p, st);
   return hipGetLastError();
 }
 
-template <int D, bool E4M3>
+template <int D, int FMT>
 static void launch_read_t(const PagedReadParams& p, hipStream_t st) {
   const unsigned grid = (unsigned)(((long)p.total + kReadRows - 1) / kReadRows);
-  hipLaunchKernelGGL((mala_paged_read_kernel<D, E4M3>), dim3(grid), dim3(256), 0, st, p);
+  hipLaunchKernelGGL((mala_paged_read_kernel<D, FMT>), dim3(grid), dim3(256), 0, st, p);
+}
+
+template <int D>
+static void launch_read_d(const PagedReadParams& p, hipStream_t st) {
+  if (p.c.fmt == kCacheBlock)
+    launch_read_t<D, kCacheBlock>(p, st);
+  else if (p.c.fmt == kCacheE4M3)
+    launch_read_t<D, kCacheE4M3>(p, st);
+  else
+    launch_read_t<D, kCacheBf16>(p, st);
 }
 
 hipError_t launch_paged_read(const PagedReadParams& p, int D, hipStream_t st) {
-  if (D == 128)
-    p.c.e4m3 ? launch_read_t<128, true>(p, st) : launch_read_t<128, false>(p, st);
-  else
-    p.c.e4m3 ? launch_read_t<64, true>(p, st) : launch_read_t<64, false>(p, st);
+  D == 128 ? launch_read_d<128>(p, st) : launch_read_d<64>(p, st);
   return hipGetLastError();
 }
 

@@ -151,14 +151,15 @@ struct SplitState {
   }
 };
 
-template <int D, bool E4M3, int MODE>
+template <int D, int FMT, int MODE>
 __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(PagedDecParams p) {
   constexpr int W = kPagedWaves;
   constexpr bool DENSE = MODE == kDense, TEAM = MODE == kTeam;
+  constexpr bool E4M3 = FMT == kCacheE4M3, BLOCK = FMT == kCacheBlock, BYTES = E4M3 || BLOCK;
   constexpr int KS = D / 32;             // k-steps of 32 over head_dim
   constexpr int NDB = D / 16;            // 16-row blocks of O^T
   constexpr int LD = D + 8;
-  constexpr int CPR = D / (E4M3 ? 16 : 8);   // 16-byte chunks per row of the cache
+  constexpr int CPR = D / (BYTES ? 16 : 8);   // 16-byte chunks per row of the cache
   constexpr int RPI = 64 / CPR;          // rows per load instruction
   constexpr int IPG = kPageRows / RPI;   // load instructions per 16-row group
   static_assert(IPG >= 1, "a load instruction stays within a group");
@@ -208,6 +209,7 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
   // length, or of a page whose entry is outside the pool).
   uint32_t off_lo = 0, off_hi = 0;
   int rows = 0;
+  uint32_t kscale = 0, vscale = 0;     // kCacheBlock: of the group's K and V, as bits of an fp32
   const int32_t* entry = p.table + (long)b * p.W;
   const unsigned gpp = p.c.page_size / kPageRows;
   const auto find_groups = [&](int g_top) {
@@ -222,6 +224,14 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
                               : 0;
     off_lo = (uint32_t)off;
     off_hi = (uint32_t)(off >> 32);
+    if constexpr (BLOCK) {
+      kscale = vscale = 0x3f800000;
+      if (rows) {
+        const int64_t at = ((int64_t)number * Hkv + hkv) * gpp + within;
+        kscale = block_scale_bits(p.c.kb[at]);
+        vscale = block_scale_bits(p.c.vb[at]);
+      }
+    }
   };
   find_groups(2 * t_hi - 1);
 
@@ -255,12 +265,14 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
   struct Place {
     uint64_t off0, off1;
     int rows0, rows1;
+    int lane;            // that holds the upper group (kCacheBlock)
+    uint32_t ks0, ks1, vs0, vs1;
   };
   int in = 0;                            // lane of the next tile's upper group
   // where tile t is, the one below the last asked for (kTeam: any below it); nowhere below t_end
   int top = t_hi - 1;                    // its lane 0 holds this tile (kTeam)
   const auto next_tile = [&](int t, int t_end) {
-    Place x = {0, 0, 0, 0};
+    Place x = {0, 0, 0, 0, 0, 0, 0, 0, 0};
     if (t < t_end) return x;
     if constexpr (TEAM) {
       if (top - t >= 32) {
@@ -278,8 +290,19 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
     x.off0 = (uint64_t)(uint32_t)__builtin_amdgcn_readlane(off_hi, in + 1) << 32 |
              (uint32_t)__builtin_amdgcn_readlane(off_lo, in + 1);
     x.rows0 = __builtin_amdgcn_readlane(rows, in + 1);
+    x.lane = in;
     in += 2;
     return x;
+  };
+  // A place's scales.  They are loaded behind its offsets, and read here once the place's turn has
+  // come (before the next lookup), so that its K and V loads do not wait for them.
+  const auto take_scales = [&](Place& x) {
+    if constexpr (BLOCK) {
+      x.ks1 = __builtin_amdgcn_readlane(kscale, x.lane);
+      x.vs1 = __builtin_amdgcn_readlane(vscale, x.lane);
+      x.ks0 = __builtin_amdgcn_readlane(kscale, x.lane + 1);
+      x.vs0 = __builtin_amdgcn_readlane(vscale, x.lane + 1);
+    }
   };
 
   uint32_t lane_off[IPG];
@@ -301,19 +324,20 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
   // A tile's rows to LDS.  One wavefront's LDS accesses complete in issue order, so K and V
   // tiles can follow each other in one slot without waits.
   bf16* mine = slot[w];
-  const auto to_lds = [&](const Tile& x) {
+  const auto to_lds = [&](const Tile& x, uint32_t scale0, uint32_t scale1) {
 #pragma unroll
     for (int i = 0; i < 2 * IPG; ++i) {
       const int r = i * RPI + lane / CPR, c = lane % CPR;
-      if constexpr (E4M3) {
+      if constexpr (BYTES) {
         const i32x4 raw = __builtin_bit_cast(i32x4, x[i]);
+        const float f = BLOCK ? __uint_as_float(i < IPG ? scale0 : scale1) : 1.f;
         i32x4 y[2];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
           y[k / 2][2 * (k % 2)] = __builtin_bit_cast(
-              int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[k], 1.f, false));
+              int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[k], f, false));
           y[k / 2][2 * (k % 2) + 1] = __builtin_bit_cast(
-              int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[k], 1.f, true));
+              int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[k], f, true));
         }
         store8(mine + r * LD + c * 16, __builtin_bit_cast(bf16x8, y[0]));
         store8(mine + r * LD + c * 16 + 8, __builtin_bit_cast(bf16x8, y[1]));
@@ -385,19 +409,20 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
   Place at = next_tile(TEAM ? t_hi - 1 - w : t_hi - 1, TEAM ? split_lo : t_lo);
   load_tile(p.c.k, at, true, kr);
   load_tile(p.c.v, at, true, vr);
+  take_scales(at);
 
   if constexpr (DENSE) {
     // every tile counts: K and V of the next one load while a tile is worked on.  (Columns
     // without a head have zero queries; what they hold is never stored.)
     for (int t = t_hi - 1; t >= t_lo; --t) {
       const Place next = next_tile(t - 1, t_lo);
-      to_lds(kr);
+      to_lds(kr, at.ks0, at.ks1);
       load_tile(p.c.k, next, true, kr);
       float s[8];
       const float mt = scores(at, s);
       raise(fmaxf(m, mt));
       const float shift = m == kNegInf ? 0.f : m;       // scores of -inf alone add 0
-      to_lds(vr);
+      to_lds(vr, at.vs0, at.vs1);
       load_tile(p.c.v, next, true, vr);
 #pragma unroll
       for (int r = 0; r < 8; ++r) s[r] = fast_exp2(__builtin_fmaf(s[r], scale2, -shift));
@@ -407,6 +432,7 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
       legal += here ? 1u : 0u;
       if (p.counters && here) hsum += tile_hash(b, h0 + col, 0, t);
       at = next;
+      take_scales(at);
     }
     cnt = legal;
     vfetch = vloads = legal;
@@ -424,7 +450,7 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
         lo_next = split_lo - p.unit;
       }
       const Place next = next_tile(t_next - w, max(lo_next, t_lo));
-      to_lds(kr);
+      to_lds(kr, at.ks0, at.ks1);
       load_tile(p.c.k, next, true, kr);
       float s[8];
       const float mt = scores(at, s), own = mt == kNegInf ? 0.f : mt;
@@ -434,7 +460,7 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
       const float all = rows_sum(ps);
       const bool here = at.rows0 + at.rows1 > 0;
       if (g == 0) tests[round & 1][w][col] = f32x2{mt, here ? all : -1.f};
-      to_lds(vr);
+      to_lds(vr, at.vs0, at.vs1);
       load_tile(p.c.v, next, true, vr);
       __syncthreads();
       bool mine = false;
@@ -463,6 +489,7 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
       t0 = t_next;
       split_lo = lo_next;
       at = next;
+      take_scales(at);
     }
     vfetch = legal;
   } else if (t_hi > t_lo) {
@@ -473,13 +500,14 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
     float s[8], sn[8];
     int left = (t_hi - 1) % p.unit + 1;      // tiles of the split from t down
     Place next = next_tile(t_hi - 2, t_lo);
-    to_lds(kr);
+    to_lds(kr, at.ks0, at.ks1);
     load_tile(p.c.k, next, true, kr);
     float mt = scores(at, s);
+    take_scales(next);
     vfetch = at.rows0 + at.rows1 > 0;
     for (int t = t_hi - 1; t >= t_lo; --t) {
       const Place after = next_tile(t - 2, t_lo);
-      to_lds(kr);                            // K of t - 1 (zeros past the run's first tile)
+      to_lds(kr, next.ks0, next.ks1);        // K of t - 1 (zeros past the run's first tile)
       load_tile(p.c.k, after, true, kr);
       const float mtn = scores(next, sn);
       const bool here = at.rows0 + at.rows1 > 0, there = next.rows0 + next.rows1 > 0;
@@ -489,7 +517,7 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
       const bool hint =
           there && (last || wave_any(head_valid && state.may_retain(mtn, run, thr2)));
       const bool any = wave_any(demand);
-      if (any) to_lds(vr);
+      if (any) to_lds(vr, at.vs0, at.vs1);
       load_tile(p.c.v, next, hint, vr);
       legal += here ? 1u : 0u;
       vfetch += hint ? 1u : 0u;
@@ -524,6 +552,7 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
       mt = mtn;
       at = next;
       next = after;
+      take_scales(next);
     }
   }
   l = rows_sum(l);
@@ -678,28 +707,38 @@ __global__ __launch_bounds__(kJoinThreads) void mala_paged_join_kernel(PagedDecP
 }
 
 // ------------------------------------------------------------------ launches
-template <int D, bool E4M3, int MODE>
+template <int D, int FMT, int MODE>
 void launch_t(const PagedDecParams& p, hipStream_t st) {
   const dim3 grid(paged_grid(p.nblk * p.c.Hkv, p.nchunk)), wg(kPagedWaves * 64);
-  hipLaunchKernelGGL((mala_paged_decode_kernel<D, E4M3, MODE>), grid, wg, 0, st, p);
+  hipLaunchKernelGGL((mala_paged_decode_kernel<D, FMT, MODE>), grid, wg, 0, st, p);
   if (p.nblk > p.B)
     hipLaunchKernelGGL(mala_paged_join_kernel<D>, dim3((unsigned)(p.B * p.Hq)), dim3(kJoinThreads), 0,
                        st, p);
 }
-template <int D, bool E4M3>
+template <int D, int FMT>
 void launch_e(const PagedDecParams& p, int mode, hipStream_t st) {
   if (mode == kDense)
-    launch_t<D, E4M3, kDense>(p, st);
+    launch_t<D, FMT, kDense>(p, st);
   else if (mode == kTeam)
-    launch_t<D, E4M3, kTeam>(p, st);
+    launch_t<D, FMT, kTeam>(p, st);
   else
-    launch_t<D, E4M3, kChain>(p, st);
+    launch_t<D, FMT, kChain>(p, st);
+}
+
+template <int D>
+void launch_d(const PagedDecParams& p, int mode, hipStream_t st) {
+  if (p.c.fmt == kCacheBlock)
+    launch_e<D, kCacheBlock>(p, mode, st);
+  else if (p.c.fmt == kCacheE4M3)
+    launch_e<D, kCacheE4M3>(p, mode, st);
+  else
+    launch_e<D, kCacheBf16>(p, mode, st);
 }
 
 }  // namespace
 
 hipError_t launch_paged_decode(PagedDecParams p, int D, int split_tokens, hipStream_t st) {
-  const PagedPlan x = paged_plan(p.B, p.Hq, p.c.Hkv, D, p.c.e4m3, p.max_len, split_tokens,
+  const PagedPlan x = paged_plan(p.B, p.Hq, p.c.Hkv, D, p.c.fmt != kCacheBf16, p.max_len, split_tokens,
                                  p.log2tau == kNegInf);
   p.target = x.target;
   p.ragged = x.ragged;
@@ -708,10 +747,7 @@ hipError_t launch_paged_decode(PagedDecParams p, int D, int split_tokens, hipStr
   p.nblk = x.blocks;
   p.nchunk = x.nchunk;
   p.sorted = p.B > 1 && (long)p.nblk * p.c.Hkv * p.nchunk > kNumCus;
-  if (D == 128)
-    p.c.e4m3 ? launch_e<128, true>(p, x.mode, st) : launch_e<128, false>(p, x.mode, st);
-  else
-    p.c.e4m3 ? launch_e<64, true>(p, x.mode, st) : launch_e<64, false>(p, x.mode, st);
+  D == 128 ? launch_d<128>(p, x.mode, st) : launch_d<64>(p, x.mode, st);
   return hipGetLastError();
 }
 

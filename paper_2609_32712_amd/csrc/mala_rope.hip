@@ -1,0 +1,39 @@
+// Rotary positions of queries and keys, and of their gradients (gfx950).
+//
+// Every row is read and written once, so HBM bounds a large call; an angle is computed once per
+// token and pair and kept for the heads that a workgroup takes.
+#include "mala_rope.h"
+
+namespace mala {
+
+namespace {
+
+template <int D, bool IN32, bool OUT32>
+__global__ __launch_bounds__(256) void mala_rope_kernel(RopeParams p) {
+  turn_rows<D, IN32, OUT32>(p, blockIdx.x * (256 / (D / 16)), blockIdx.y * p.per);
+}
+
+template <int D, bool IN32, bool OUT32>
+void launch_t(const RopeParams& p, hipStream_t st) {
+  constexpr unsigned kTokens = 256 / (D / 16);
+  const int heads = p.r[0].H + p.r[1].H;
+  const dim3 grid((p.B * p.T + kTokens - 1) / kTokens, (heads + p.per - 1) / p.per);
+  hipLaunchKernelGGL((mala_rope_kernel<D, IN32, OUT32>), grid, dim3(256), 0, st, p);
+}
+template <int D>
+void launch_d(const RopeParams& p, bool in32, bool out32, hipStream_t st) {
+  if (in32)
+    out32 ? launch_t<D, true, true>(p, st) : launch_t<D, true, false>(p, st);
+  else
+    out32 ? launch_t<D, false, true>(p, st) : launch_t<D, false, false>(p, st);
+}
+
+}  // namespace
+
+hipError_t launch_rope(RopeParams p, int D, bool in32, bool out32, hipStream_t st) {
+  p.per = rope_heads_per_group(p.B * p.T, p.r[0].H + p.r[1].H, D);
+  D == 128 ? launch_d<128>(p, in32, out32, st) : launch_d<64>(p, in32, out32, st);
+  return hipGetLastError();
+}
+
+}  // namespace mala
