@@ -527,10 +527,11 @@ int check_write(const void* k_new, const void* v_new, int64_t new_token_stride, 
     return fail(MALA_ERR_INVALID_ARG, "rows of k_new and v_new must be 16-byte aligned");
   if (new_token_stride > INT64_MAX / 8 / num_tokens || new_head_stride > INT64_MAX / 8 / cache->Hkv)
     return fail(MALA_ERR_UNSUPPORTED, "k_new stride too large");
-  // (a thread per 16 bytes of a row of the cache; of blocks, 256 per kBlockChunk tokens)
-  const int threads = p->c.fmt == mala::kCacheBlock ? 256 / mala::kBlockChunk
-                                                    : cache->D / (p->c.fmt == mala::kCacheBf16 ? 8 : 16);
-  if ((int64_t)num_tokens * threads > UINT32_MAX - 255)
+  // (a thread per 16 bytes of a row of the cache; of blocks, as the launch rule says)
+  const int64_t threads = p->c.fmt == mala::kCacheBlock
+                              ? 64 * mala::block_write_plan(num_tokens, cache->Hkv, false).waves
+                              : (int64_t)num_tokens * (cache->D / (p->c.fmt == mala::kCacheBf16 ? 8 : 16));
+  if (threads > UINT32_MAX - 255)
     return fail(MALA_ERR_UNSUPPORTED, "a launch of 2^32 threads or more (num_tokens %d)", num_tokens);
   p->k = (const char*)k_new;
   p->v = (const char*)v_new;
@@ -538,7 +539,7 @@ int check_write(const void* k_new, const void* v_new, int64_t new_token_stride, 
   p->head_stride = new_head_stride * 2;
   p->slots = slots;
   p->T = num_tokens;
-  p->chunk = 0;
+  p->chunk = p->heads = 0;
   return MALA_OK;
 }
 
@@ -699,9 +700,11 @@ int mala_paged_rope_write(const mala_rope_rows_t* q, const void* k_new, const vo
   if (q && (st = check_rows(q, "q", 1, num_tokens, cache->D, 2, 2, &p.q.r[0]))) return st;
   p.q.B = 1;
   p.q.T = num_tokens;
-  // a workgroup per rope_tokens(D) tokens, and per head at most; in one dimension
+  // a workgroup per rope_tokens(D) tokens, and per head at most, and those of a block-scaled write; in
+  // one dimension
   const double groups = ((double)num_tokens / mala::rope_tokens(cache->D) + 1) *
-                            (p.q.r[0].H + 2.0 * cache->Hkv) + num_tokens / mala::kBlockChunk + 2048;
+                            (p.q.r[0].H + 2.0 * cache->Hkv) +
+                        mala::block_write_plan(num_tokens, cache->Hkv, true).waves / 4.0 + 1;
   if (groups * 256 > UINT32_MAX) return fail(MALA_ERR_UNSUPPORTED, "a launch of 2^32 threads or more");
   const hipError_t e = mala::launch_paged_rope_write(p, cache->D, (hipStream_t)stream);
   return e == hipSuccess ? MALA_OK : hip_fail(e, "mala_paged_rope_write: kernel launch");

@@ -15,8 +15,6 @@ namespace mala {
 
 namespace {
 
-constexpr int kWindow = 63;    // tokens of a block lie at most so far apart
-
 // e of a block whose largest |value| is the bf16 with these bits (finite): 448 = 1.75 x 2^8.
 __device__ __forceinline__ int block_exponent(uint32_t bf16_bits) {
   return min(max((int)(((bf16_bits << 16) + 0x1fffffu) >> 23) - 127 - 8, kScaleMin), kScaleMax);
@@ -25,6 +23,7 @@ __device__ __forceinline__ float power_of_two(int e) {     // e in [-126, 127]
   return __uint_as_float((uint32_t)(e + 127) << 23);
 }
 
+typedef short s16x2 __attribute__((ext_vector_type(2)));
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ uint32_t max_u16x2(uint32_t a, uint32_t b) {
   return __builtin_bit_cast(uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2, a),
@@ -50,168 +49,187 @@ __device__ __forceinline__ int to_block4(float a, float b, float c, float d, flo
 __device__ __forceinline__ float bf16_lo(uint32_t u) { return __uint_as_float(u << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
 
-// The n-th set bit of mask.
-__device__ __forceinline__ int set_bit(uint64_t mask, int n) {
-  for (int i = 0; i < n; ++i) mask &= mask - 1;
-  return __builtin_ctzll(mask);
-}
-
-// Keys and values of the blocks whose first token (of this call) is among the chunk's tokens.
-// LPR lanes take a block of one head, all its rows in registers.
+// Keys and values of the blocks whose first token (of this call) is among the wavefront's chunk of
+// tokens, of some heads of K or of V.  No wavefront waits for another: each finds the rows of its
+// blocks from the slots around its tokens, by ballots and a lane exchange.  D / 16 lanes a row.
 template <int D, bool ROPE>
 struct BlockWriter {
-  static constexpr int LPR = D / 16, SUBS = 256 / LPR;
-  static constexpr int G = ROPE ? 256 / D : kBlockChunk;    // blocks at a time (their angles in LDS)
+  static constexpr int LPR = D / 16, RPI = 64 / LPR, NI = kPageRows / RPI;   // rows at a time, times
 
-  struct Shared {
-    int window[kBlockChunk + 2 * kWindow];
-    __attribute__((aligned(16))) int rows[kBlockChunk][16];   // token of each row, or -1
-    int block[kBlockChunk];
-    __attribute__((aligned(16))) f32x2 turns[ROPE ? G : 1][ROPE ? 16 : 1][ROPE ? D / 2 : 1];
-  };
-
-  static __device__ __forceinline__ void run(const PagedWriteParams& p, const Turn& turn, unsigned group,
-                                             Shared& sh) {
-    const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int t0 = (int)group * p.chunk, Hkv = p.c.Hkv;
+  // `at`: the wavefront's number among those of the keys and values
+  static __device__ __forceinline__ void run(const PagedWriteParams& p, const Turn& turn, unsigned at) {
+    const int lane = threadIdx.x & 63;
+    const int parts = (p.c.Hkv + p.heads - 1) / p.heads;      // of the heads, for K and for V
+    const unsigned chunk = at / (2 * parts);
+    const int part = at - chunk * 2 * parts, kind = part >= parts, h0 = (part - kind * parts) * p.heads;
+    const int64_t t0 = (int64_t)chunk * p.chunk;
+    if (t0 >= p.T) return;
     const int slots = (int)(p.c.num_pages * (unsigned)p.c.page_size);
-    // which tokens share a block
-    for (int j = tid; j < p.chunk + 2 * kWindow; j += 256) {
-      const int t = t0 - kWindow + j;
-      int s = t >= 0 && t < p.T ? p.slots[t] : -1;
-      sh.window[j] = s < slots ? s : -1;
-    }
-    __syncthreads();
-    for (int ci = w; ci < p.chunk; ci += 4) {
-      const int mine = sh.window[kWindow + ci], block = mine >> 4;
-      const int before = lane < kWindow ? sh.window[kWindow + ci - 1 - lane] : -1;
-      const int after = sh.window[kWindow + ci + lane];
-      const bool first = mine >= 0 && !wave_any(before >= 0 && before >> 4 == block);
-      if (lane < 16) sh.rows[ci][lane] = -1;
-      if (first && after >= 0 && after >> 4 == block) sh.rows[ci][after & 15] = t0 + ci + lane;
-      if (lane == 0) sh.block[ci] = first ? block : -1;
-    }
-    __syncthreads();
-    const uint64_t firsts =
-        __builtin_amdgcn_ballot_w64(lane < p.chunk && sh.block[lane < p.chunk ? lane : 0] >= 0);
-    const int n = __builtin_popcountll(firsts);
-    for (int g0 = 0; g0 < n; g0 += G) {
-      const int here = min(G, n - g0);
-      if constexpr (ROPE) {
-        const int pairs = turn.R / 2;
-        if (g0) __syncthreads();
-        for (int i = tid; i < here * 16 * pairs; i += 256) {
-          const int row = i / pairs, pair = i - row * pairs;
-          const int t = sh.rows[set_bit(firsts, g0 + row / 16)][row & 15];
-          if (t < 0) continue;
-          float c, s;
-          turn_of(turn.pos ? turn.pos[t] : t, turn.inv_freq[pair], turn.scale, turn.sin_scale, c, s);
-          sh.turns[row / 16][row & 15][pair] = f32x2{c, s};
+    const auto slot_of = [&](int64_t t) {
+      if (t < 0 || t >= p.T) return -1;
+      const int s = p.slots[t];
+      return s < slots && s >= 0 ? s : -1;
+    };
+    const int before = slot_of(t0 - 64 + lane), here = slot_of(t0 + lane);
+    const int after = p.chunk > 1 ? slot_of(t0 + 64 + lane) : -1;
+    uint64_t todo = __builtin_amdgcn_ballot_w64(here >= 0 && lane < p.chunk);
+    while (todo) {
+      const int ci = __builtin_ctzll(todo), first = __builtin_amdgcn_readlane(here, ci), block = first >> 4;
+      // (-1 >> 4 is no block's number.  Tokens of a block lie within 64: those before from lane ci + 1 on,
+      // those after below lane ci)
+      const uint64_t same = __builtin_amdgcn_ballot_w64(here >> 4 == block);
+      todo &= ~same;
+      if (__builtin_amdgcn_ballot_w64(before >> 4 == block) >> ci >> 1) continue;
+      const uint64_t more =
+          p.chunk > 1 ? __builtin_amdgcn_ballot_w64(after >> 4 == block) & ((1ull << ci) - 1) : 0;
+      // token of row r of the block, from t0 on, plus 1, in lane r < 16; 0 for none
+      int token;
+      if (!(same & (same - 1)) && !more) {
+        token = lane == (first & 15) ? ci + 1 : 0;
+      } else {
+        // (of tokens with the same slot, one's number arrives)
+        token = __builtin_amdgcn_ds_permute(4 * (here >> 4 == block ? here & 15 : 63), lane + 1);
+        if (more) {
+          const bool mine = (more >> lane) & 1;
+          const int late = __builtin_amdgcn_ds_permute(4 * (mine ? after & 15 : 63), 64 + lane + 1);
+          token = token ? token : late;
         }
-        __syncthreads();
       }
-      for (int u = tid / LPR; u < here * 2 * Hkv; u += SUBS) {
-        const int g = u / (2 * Hkv), kind = (u - g * 2 * Hkv) / Hkv, h = u - (2 * g + kind) * Hkv;
-        write_block(p, turn, sh, set_bit(firsts, g0 + g), g, kind, h);
-      }
+      write_block(p, turn, t0 - 1, token, (unsigned)block, kind, h0);
     }
   }
 
-  static __device__ __forceinline__ void write_block(const PagedWriteParams& p, const Turn& turn, Shared& sh,
-                                                     int ci, int g, int kind, int h) {
-    const int lr = threadIdx.x % LPR;
-    const unsigned per_page = (unsigned)p.c.page_size / kPageRows, block = sh.block[ci];
+  static __device__ __forceinline__ void write_block(const PagedWriteParams& p, const Turn& turn, int64_t base,
+                                                     int token, unsigned block, int kind, int h0) {
+    const int lane = threadIdx.x & 63, lr = lane % LPR;
+    const unsigned per_page = (unsigned)p.c.page_size / kPageRows;
     const unsigned page = block / per_page, within = block - page * per_page;
+    const bool anew = __builtin_amdgcn_readlane(token, 0) != 0;
+    int t[NI];
+#pragma unroll
+    for (int i = 0; i < NI; ++i) t[i] = __builtin_amdgcn_ds_bpermute(4 * (lane / LPR + i * RPI), token);
     const bool keys = ROPE && kind == 0;
     const Pieces pc = pieces_of(lr, keys ? turn.R : 0, keys ? turn.interleaved : 1);
-    const char* in = (kind ? p.v : p.k) + h * p.head_stride;
-    char* out = (kind ? p.c.v : p.c.k) + (int64_t)page * p.c.page_stride + h * p.c.head_stride +
-                (int64_t)(within * kPageRows) * p.c.token_stride;
-    uint8_t* scale = (kind ? p.c.vb : p.c.kb) + ((int64_t)page * p.c.Hkv + h) * per_page + within;
-    int t[16];
-#pragma unroll
-    for (int r = 0; r < 16; ++r) t[r] = sh.rows[ci][r];
-    const int held = t[0] >= 0 ? kScaleMin : min(max((int)*scale - 127, kScaleMin), kScaleMax);
-
-    i32x4 x[16][2];
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      x[r][0] = x[r][1] = i32x4{0, 0, 0, 0};
-      if (t[r] >= 0) {
-        const char* row = in + t[r] * p.token_stride;
-        x[r][0] = *reinterpret_cast<const i32x4*>(row + pc.first * 16);
-        x[r][1] = *reinterpret_cast<const i32x4*>(row + pc.second * 16);
-      }
-    }
+    float c[NI][8], s[NI][8];
     if (ROPE && pc.turned) {
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        if (t[r] < 0) continue;
-        float v[16], c[8], s[8];
+      for (int i = 0; i < NI; ++i)
+        if (t[i]) {
+          const int pos = turn.pos ? turn.pos[base + t[i]] : (int)(base + t[i]);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
+          for (int k = 0; k < 8; ++k)
+            turn_of(pos, turn.inv_freq[8 * lr + k], turn.scale, turn.sin_scale, c[i][k], s[i][k]);
+        }
+    }
+    for (int h = h0; h < min(h0 + p.heads, p.c.Hkv); ++h) {
+      const char* in = (kind ? p.v : p.k) + h * p.head_stride;
+      char* out = (kind ? p.c.v : p.c.k) + (int64_t)page * p.c.page_stride + h * p.c.head_stride +
+                  (int64_t)(within * kPageRows) * p.c.token_stride;
+      uint8_t* scale = (kind ? p.c.vb : p.c.kb) + ((int64_t)page * p.c.Hkv + h) * per_page + within;
+      int byte = 0;
+      if (!anew) byte = *scale;
+      i32x4 x[NI][2];
 #pragma unroll
-          for (int half = 0; half < 2; ++half) {
-            v[8 * half + 2 * i] = bf16_lo((uint32_t)x[r][half][i]);
-            v[8 * half + 2 * i + 1] = bf16_hi((uint32_t)x[r][half][i]);
+      for (int i = 0; i < NI; ++i) {
+        x[i][0] = x[i][1] = i32x4{0, 0, 0, 0};
+        if (t[i]) {
+          const char* row = in + (base + t[i]) * p.token_stride;
+          x[i][0] = *reinterpret_cast<const i32x4*>(row + pc.first * 16);
+          x[i][1] = *reinterpret_cast<const i32x4*>(row + pc.second * 16);
+        }
+      }
+      if (ROPE && pc.turned) {
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          float v[16];
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+#pragma unroll
+            for (int half = 0; half < 2; ++half) {
+              v[8 * half + 2 * k] = bf16_lo((uint32_t)x[i][half][k]);
+              v[8 * half + 2 * k + 1] = bf16_hi((uint32_t)x[i][half][k]);
+            }
           }
+          if (t[i]) turn_pieces(v, c[i], s[i], turn.interleaved);
+          x[i][0] = to_bf16x8(v);        // the key as it would be stored without a cache
+          x[i][1] = to_bf16x8(v + 8);
         }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const f32x2 a = sh.turns[g][r][8 * lr + i];
-          c[i] = a[0];
-          s[i] = a[1];
-        }
-        turn_pieces(v, c, s, turn.interleaved);
-        x[r][0] = to_bf16x8(v);        // the key as it would be stored without a cache
-        x[r][1] = to_bf16x8(v + 8);
       }
-    }
-    uint32_t most = 0;
+      // |bf16| compare as their bits; infinities and NaN, which do not count, are above all others
+      uint32_t bits = 0;
 #pragma unroll
-    for (int r = 0; r < 16; ++r)
+      for (int i = 0; i < NI; ++i)
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        most = max_finite(max_finite(most, (uint32_t)x[r][0][i]), (uint32_t)x[r][1][i]);
-    most = max(most & 0xffffu, most >> 16);
-    // over the LPR lanes of the block
-    most = max(most, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)most, 0xB1, 0xf, 0xf, true));   // lane ^ 1
-    most = max(most, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)most, 0x4E, 0xf, 0xf, true));   // lane ^ 2
-    if constexpr (LPR == 8)   // row_half_mirror: the other four of eight
-      most = max(most, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)most, 0x141, 0xf, 0xf, true));
-    const int e = max(held, block_exponent(most));
-    if (lr == 0) *scale = (uint8_t)(e + 127);
+        for (int k = 0; k < 4; ++k)
+          bits = max_u16x2(max_u16x2(bits, (uint32_t)x[i][0][k] & 0x7fff7fffu), (uint32_t)x[i][1][k] & 0x7fff7fffu);
+      int most = wave_max((int)max(bits & 0xffffu, bits >> 16));
+      const bool odd = most >= 0x7f80;
+      if (odd) {
+        bits = 0;
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            bits = max_finite(max_finite(bits, (uint32_t)x[i][0][k]), (uint32_t)x[i][1][k]);
+        most = wave_max((int)max(bits & 0xffffu, bits >> 16));
+      }
+      const int old = anew ? kScaleMin : min(max(__builtin_amdgcn_readfirstlane(byte) - 127, kScaleMin), kScaleMax);
+      const int e = max(old, block_exponent((uint32_t)most));
+      if (lane == 0) *scale = (uint8_t)(e + 127);
 
-    // (448 x 2^120 is no bf16 any more)
-    const float inv = power_of_two(-e), limit = e == kScaleMax ? 240.f : 448.f;
+      i32x4 y[NI];
+      if (odd || e == kScaleMax) {
+        // (448 x 2^120 is no bf16 any more)
+        const float inv = power_of_two(-e), limit = e == kScaleMax ? 240.f : 448.f;
 #pragma unroll
-    for (int r = 0; r < 16; ++r) {
-      if (t[r] < 0) continue;
-      i32x4 y;
+        for (int i = 0; i < NI; ++i)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t a = (uint32_t)x[r][i / 2][2 * (i % 2)], b = (uint32_t)x[r][i / 2][2 * (i % 2) + 1];
-        y[i] = to_block4(bf16_lo(a), bf16_hi(a), bf16_lo(b), bf16_hi(b), inv, limit);
+          for (int k = 0; k < 4; ++k) {
+            const uint32_t a = (uint32_t)x[i][k / 2][2 * (k % 2)], b = (uint32_t)x[i][k / 2][2 * (k % 2) + 1];
+            y[i][k] = to_block4(bf16_lo(a), bf16_hi(a), bf16_lo(b), bf16_hi(b), inv, limit);
+          }
+      } else {
+        // the instruction divides by the scale and rounds once, to nearest even (checked for every
+        // bf16 and e); it does not saturate, and here nothing is above 448
+        const float f = power_of_two(e);
+#pragma unroll
+        for (int i = 0; i < NI; ++i)
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const uint32_t a = (uint32_t)x[i][k / 2][2 * (k % 2)], b = (uint32_t)x[i][k / 2][2 * (k % 2) + 1];
+            s16x2 r = {0, 0};
+            r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf16x2, a), f, false);
+            r = __builtin_amdgcn_cvt_scalef32_pk_fp8_bf16(r, __builtin_bit_cast(bf16x2, b), f, true);
+            y[i][k] = __builtin_bit_cast(int, r);
+          }
       }
-      char* row = out + r * p.c.token_stride;
-      *reinterpret_cast<i32x2*>(row + pc.first * 8) = i32x2{y[0], y[1]};
-      *reinterpret_cast<i32x2*>(row + pc.second * 8) = i32x2{y[2], y[3]};
-    }
-    // a larger scale than the block had: its other rows
-    if (t[0] < 0 && e > held) {
-      const float less = power_of_two(max(held - e, -100));
 #pragma unroll
-      for (int r = 0; r < 16; ++r) {
-        if (t[r] >= 0) continue;
-        i32x4* row = reinterpret_cast<i32x4*>(out + r * p.c.token_stride + 16 * lr);
-        i32x4 y = *row;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(y[i], false);
-          const f32x2 b = __builtin_amdgcn_cvt_pk_f32_fp8(y[i], true);
-          y[i] = to_block4(a[0], a[1], b[0], b[1], less, 448.f);
+      for (int i = 0; i < NI; ++i) {
+        if (!t[i]) continue;
+        char* row = out + (lane / LPR + i * RPI) * p.c.token_stride;
+        if (ROPE && pc.second != pc.first + 1) {
+          *reinterpret_cast<i32x2*>(row + pc.first * 8) = i32x2{y[i][0], y[i][1]};
+          *reinterpret_cast<i32x2*>(row + pc.second * 8) = i32x2{y[i][2], y[i][3]};
+        } else {
+          *reinterpret_cast<i32x4*>(row + pc.first * 8) = y[i];
         }
-        *row = y;
+      }
+      // a larger scale than the block had: its other rows
+      if (!anew && e > old) {
+        const float less = power_of_two(max(old - e, -100));
+#pragma unroll
+        for (int i = 0; i < NI; ++i) {
+          if (t[i]) continue;
+          i32x4* row = reinterpret_cast<i32x4*>(out + (lane / LPR + i * RPI) * p.c.token_stride + 16 * lr);
+          i32x4 z = *row;
+#pragma unroll
+          for (int k = 0; k < 4; ++k) {
+            const f32x2 a = __builtin_amdgcn_cvt_pk_f32_fp8(z[k], false);
+            const f32x2 b = __builtin_amdgcn_cvt_pk_f32_fp8(z[k], true);
+            z[k] = to_block4(a[0], a[1], b[0], b[1], less, 448.f);
+          }
+          *row = z;
+        }
       }
     }
   }
@@ -219,16 +237,14 @@ struct BlockWriter {
 
 template <int D>
 __global__ __launch_bounds__(256) void mala_paged_block_write_kernel(PagedWriteParams p) {
-  __shared__ typename BlockWriter<D, false>::Shared sh;
-  BlockWriter<D, false>::run(p, Turn{}, blockIdx.x, sh);
+  BlockWriter<D, false>::run(p, Turn{}, blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
 }
 
 // Keys and values into a block-scaled cache by the first workgroups, queries by the others.
 template <int D>
 __global__ __launch_bounds__(256) void mala_paged_block_rope_kernel(PagedRopeWriteParams p) {
-  __shared__ typename BlockWriter<D, true>::Shared sh;
   if (blockIdx.x < p.kv_groups) {
-    BlockWriter<D, true>::run(p.w, p.q.turn, blockIdx.x, sh);
+    BlockWriter<D, true>::run(p.w, p.q.turn, blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
   } else {
     const unsigned nx = (p.q.T + rope_tokens(D) - 1) / rope_tokens(D), i = blockIdx.x - p.kv_groups;
     turn_rows<D, false, false>(p.q, i % nx * rope_tokens(D), (int)(i / nx) * p.q.per);
@@ -252,7 +268,7 @@ __global__ __launch_bounds__(256) void mala_paged_rope_write_kernel(PagedRopeWri
   const int slot = w.slots[t], lr = threadIdx.x % LPR;
   if (slot < 0 || (unsigned)slot >= w.c.num_pages * P) return;
   const unsigned page = slot / P, row = slot - page * P;
-  const int kind = blockIdx.x / nx % 2, h0 = blockIdx.x / nx / 2 * w.chunk;
+  const int kind = blockIdx.x / nx % 2, h0 = blockIdx.x / nx / 2 * w.heads;
   const Pieces pc = pieces_of(lr, kind ? 0 : turn.R, turn.interleaved);
   float c[8], s[8];
   if (pc.turned) {
@@ -261,7 +277,7 @@ __global__ __launch_bounds__(256) void mala_paged_rope_write_kernel(PagedRopeWri
     for (int k = 0; k < 8; ++k)
       turn_of(pos, turn.inv_freq[8 * lr + k], turn.scale, turn.sin_scale, c[k], s[k]);
   }
-  for (int h = h0; h < min(h0 + w.chunk, w.c.Hkv); ++h) {
+  for (int h = h0; h < min(h0 + w.heads, w.c.Hkv); ++h) {
     const char* x = (kind ? w.v : w.k) + t * w.token_stride + h * w.head_stride;
     char* out = (kind ? w.c.v : w.c.k) + page * w.c.page_stride + h * w.c.head_stride + row * w.c.token_stride;
     float v[16];
@@ -291,9 +307,16 @@ __global__ __launch_bounds__(256) void mala_paged_rope_write_kernel(PagedRopeWri
 
 }  // namespace
 
+// Workgroups (of four wavefronts) of the keys and values
+static unsigned block_write_groups(PagedWriteParams& p, bool rope) {
+  const BlockWritePlan x = block_write_plan(p.T, p.c.Hkv, rope);
+  p.chunk = x.chunk;
+  p.heads = x.heads;
+  return (unsigned)((x.waves + 3) / 4);
+}
+
 hipError_t launch_paged_block_write(PagedWriteParams p, int D, hipStream_t st) {
-  p.chunk = block_write_chunk(p.T);
-  const dim3 grid((unsigned)((p.T + p.chunk - 1) / p.chunk));
+  const dim3 grid(block_write_groups(p, false));
   if (D == 128)
     hipLaunchKernelGGL(mala_paged_block_write_kernel<128>, grid, dim3(256), 0, st, p);
   else
@@ -310,13 +333,12 @@ static void launch_rope_write_t(PagedRopeWriteParams& p, hipStream_t st) {
     q_groups = nx * ((p.q.r[0].H + p.q.per - 1) / p.q.per);
   }
   if (p.w.c.fmt == kCacheBlock) {
-    p.w.chunk = block_write_chunk(p.w.T);
-    p.kv_groups = (p.w.T + p.w.chunk - 1) / p.w.chunk;
+    p.kv_groups = block_write_groups(p.w, true);
     hipLaunchKernelGGL(mala_paged_block_rope_kernel<D>, dim3(p.kv_groups + q_groups), dim3(256), 0, st, p);
     return;
   }
-  p.w.chunk = rope_heads_per_group(p.w.T, p.w.c.Hkv, D);        // heads at a time
-  p.kv_groups = nx * 2 * ((p.w.c.Hkv + p.w.chunk - 1) / p.w.chunk);
+  p.w.heads = rope_heads_per_group(p.w.T, p.w.c.Hkv, D);
+  p.kv_groups = nx * 2 * ((p.w.c.Hkv + p.w.heads - 1) / p.w.heads);
   if (p.w.c.fmt == kCacheE4M3)
     hipLaunchKernelGGL((mala_paged_rope_write_kernel<D, true>), dim3(p.kv_groups + q_groups), dim3(256), 0, st, p);
   else

@@ -19,8 +19,21 @@ inline int rope_heads_per_group(unsigned tokens, int heads, int D) {
   return (int)((heads + slices - 1) / slices);
 }
 
-// Tokens that a workgroup of the block-scaled write looks at.
-constexpr int kBlockChunk = 32;
-inline int block_write_chunk(int T) { return std::clamp(T / 1024, 1, kBlockChunk); }
+// A wavefront of the block-scaled write takes the blocks that begin among `chunk` tokens, of `heads`
+// heads of K or of V.
+constexpr int kBlockChunk = 16;
+struct BlockWritePlan {
+  int chunk, heads;
+  int64_t waves;
+};
+inline BlockWritePlan block_write_plan(int T, int Hkv, bool rope) {
+  BlockWritePlan x;
+  x.chunk = std::clamp(T / 256, 1, kBlockChunk);
+  const int64_t chunks = ((int64_t)T + x.chunk - 1) / x.chunk;
+  const int64_t parts = std::clamp<int64_t>(4 * 4 * kNumCus / chunks, 1, Hkv);
+  x.heads = (int)((Hkv + parts - 1) / parts);
+  x.waves = chunks * 2 * ((Hkv + x.heads - 1) / x.heads);
+  return x;
+}
 
 }  // namespace mala

@@ -564,7 +564,7 @@ def test_serving_run(D, P, tokens):
             got_o = fw["o"][:, cq[i]:cq[i + 1]].double().cpu().numpy()
             # P as two bf16 terms (2^-16), and the scores' sums as above
             vmax = float(np.abs(rows(hv, r)).max())
-            smax = scale * float(np.abs(qp.float().cpu()).sum(-1).max()) * float(np.abs(rows(hk, r)).max())
+            smax = scale * float(qp.float().abs().sum(-1).max()) * float(np.abs(rows(hk, r)).max())
             assert np.abs(got_o - want).max() <= (2.0 ** -14 + (2 * D + 600) * pu.U24 * (smax + 1)) * vmax
     used = sum(pu.pages_of(int(n), P) for n in lens.cpu())
     assert int(state[1]) + used == N
