@@ -52,7 +52,7 @@ __device__ __forceinline__ float bf16_hi(uint32_t u) { return __uint_as_float(u 
 // Keys and values of the blocks whose first token (of this call) is among the wavefront's chunk of
 // tokens, of some heads of K or of V.  No wavefront waits for another: each finds the rows of its
 // blocks from the slots around its tokens, by ballots and a lane exchange.  D / 16 lanes a row.
-template <int D, bool ROPE>
+template <int D, bool ROPE, bool INTER>
 struct BlockWriter {
   static constexpr int LPR = D / 16, RPI = 64 / LPR, NI = kPageRows / RPI;   // rows at a time, times
 
@@ -109,17 +109,14 @@ struct BlockWriter {
 #pragma unroll
     for (int i = 0; i < NI; ++i) t[i] = __builtin_amdgcn_ds_bpermute(4 * (lane / LPR + i * RPI), token);
     const bool keys = ROPE && kind == 0;
-    const Pieces pc = pieces_of(lr, keys ? turn.R : 0, keys ? turn.interleaved : 1);
+    const Pieces<D, 8, INTER> pc(lr, turn.R);
+    // (rows that stay as they are: 16 elements of a row side by side)
+    const int first = keys ? pc.at[0] : 2 * lr, second = keys ? pc.at[1] : 2 * lr + 1;
     float c[NI][8], s[NI][8];
-    if (ROPE && pc.turned) {
+    if (keys) {
 #pragma unroll
       for (int i = 0; i < NI; ++i)
-        if (t[i]) {
-          const int pos = turn.pos ? turn.pos[base + t[i]] : (int)(base + t[i]);
-#pragma unroll
-          for (int k = 0; k < 8; ++k)
-            turn_of(pos, turn.inv_freq[8 * lr + k], turn.scale, turn.sin_scale, c[i][k], s[i][k]);
-        }
+        if (t[i]) pc.angles(turn, turn.pos ? turn.pos[base + t[i]] : (int)(base + t[i]), c[i], s[i]);
     }
     for (int h = h0; h < min(h0 + p.heads, p.c.Hkv); ++h) {
       const char* in = (kind ? p.v : p.k) + h * p.head_stride;
@@ -134,25 +131,23 @@ struct BlockWriter {
         x[i][0] = x[i][1] = i32x4{0, 0, 0, 0};
         if (t[i]) {
           const char* row = in + (base + t[i]) * p.token_stride;
-          x[i][0] = *reinterpret_cast<const i32x4*>(row + pc.first * 16);
-          x[i][1] = *reinterpret_cast<const i32x4*>(row + pc.second * 16);
+          x[i][0] = *reinterpret_cast<const i32x4*>(row + first * 16);
+          x[i][1] = *reinterpret_cast<const i32x4*>(row + second * 16);
         }
       }
-      if (ROPE && pc.turned) {
+      if (keys) {
 #pragma unroll
         for (int i = 0; i < NI; ++i) {
-          float v[16];
+          float v[2][8];
 #pragma unroll
-          for (int k = 0; k < 4; ++k) {
+          for (int n = 0; n < 2; ++n)
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              v[8 * half + 2 * k] = bf16_lo((uint32_t)x[i][half][k]);
-              v[8 * half + 2 * k + 1] = bf16_hi((uint32_t)x[i][half][k]);
-            }
-          }
-          if (t[i]) turn_pieces(v, c[i], s[i], turn.interleaved);
-          x[i][0] = to_bf16x8(v);        // the key as it would be stored without a cache
-          x[i][1] = to_bf16x8(v + 8);
+            for (int k = 0; k < 4; ++k) unpack((uint32_t)x[i][n][k], v[n] + 2 * k);
+          if (t[i]) pc.apply(v, c[i], s[i]);
+#pragma unroll
+          for (int n = 0; n < 2; ++n)    // the key as it would be stored without a cache
+#pragma unroll
+            for (int k = 0; k < 4; ++k) x[i][n][k] = pack(v[n] + 2 * k);
         }
       }
       // |bf16| compare as their bits; infinities and NaN, which do not count, are above all others
@@ -207,11 +202,11 @@ struct BlockWriter {
       for (int i = 0; i < NI; ++i) {
         if (!t[i]) continue;
         char* row = out + (lane / LPR + i * RPI) * p.c.token_stride;
-        if (ROPE && pc.second != pc.first + 1) {
-          *reinterpret_cast<i32x2*>(row + pc.first * 8) = i32x2{y[i][0], y[i][1]};
-          *reinterpret_cast<i32x2*>(row + pc.second * 8) = i32x2{y[i][2], y[i][3]};
+        if (keys) {
+          *reinterpret_cast<i32x2*>(row + first * 8) = i32x2{y[i][0], y[i][1]};
+          *reinterpret_cast<i32x2*>(row + second * 8) = i32x2{y[i][2], y[i][3]};
         } else {
-          *reinterpret_cast<i32x4*>(row + pc.first * 8) = y[i];
+          *reinterpret_cast<i32x4*>(row + first * 8) = y[i];
         }
       }
       // a larger scale than the block had: its other rows
@@ -237,28 +232,28 @@ struct BlockWriter {
 
 template <int D>
 __global__ __launch_bounds__(256) void mala_paged_block_write_kernel(PagedWriteParams p) {
-  BlockWriter<D, false>::run(p, Turn{}, blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+  BlockWriter<D, false, false>::run(p, Turn{}, blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
 }
 
 // Keys and values into a block-scaled cache by the first workgroups, queries by the others.
-template <int D>
+template <int D, bool INTER>
 __global__ __launch_bounds__(256) void mala_paged_block_rope_kernel(PagedRopeWriteParams p) {
   if (blockIdx.x < p.kv_groups) {
-    BlockWriter<D, true>::run(p.w, p.q.turn, blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
+    BlockWriter<D, true, INTER>::run(p.w, p.q.turn, blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6));
   } else {
     const unsigned nx = (p.q.T + rope_tokens(D) - 1) / rope_tokens(D), i = blockIdx.x - p.kv_groups;
-    turn_rows<D, false, false>(p.q, i % nx * rope_tokens(D), (int)(i / nx) * p.q.per);
+    turn_rows<D, false, false, INTER, false>(p.q, i % nx * rope_tokens(D), (int)(i / nx) * p.q.per);
   }
 }
 
 // The same for a cache of bf16, or of e4m3 with a scale per head: every row is its own.
-template <int D, bool E4M3>
+template <int D, bool E4M3, bool INTER>
 __global__ __launch_bounds__(256) void mala_paged_rope_write_kernel(PagedRopeWriteParams p) {
   constexpr int LPR = D / 16, TOK = rope_tokens(D);
   const unsigned nx = (p.q.T + TOK - 1) / TOK;
   if (blockIdx.x >= p.kv_groups) {
     const unsigned i = blockIdx.x - p.kv_groups;
-    turn_rows<D, false, false>(p.q, i % nx * TOK, (int)(i / nx) * p.q.per);
+    turn_rows<D, false, false, INTER, false>(p.q, i % nx * TOK, (int)(i / nx) * p.q.per);
     return;
   }
   const PagedWriteParams& w = p.w;
@@ -269,27 +264,23 @@ __global__ __launch_bounds__(256) void mala_paged_rope_write_kernel(PagedRopeWri
   if (slot < 0 || (unsigned)slot >= w.c.num_pages * P) return;
   const unsigned page = slot / P, row = slot - page * P;
   const int kind = blockIdx.x / nx % 2, h0 = blockIdx.x / nx / 2 * w.heads;
-  const Pieces pc = pieces_of(lr, kind ? 0 : turn.R, turn.interleaved);
+  const Pieces<D, 8, INTER> pc(lr, turn.R);
   float c[8], s[8];
-  if (pc.turned) {
-    const int pos = turn.pos ? turn.pos[t] : (int)t;
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-      turn_of(pos, turn.inv_freq[8 * lr + k], turn.scale, turn.sin_scale, c[k], s[k]);
-  }
+  if (!kind) pc.angles(turn, turn.pos ? turn.pos[t] : (int)t, c, s);
   for (int h = h0; h < min(h0 + w.heads, w.c.Hkv); ++h) {
     const char* x = (kind ? w.v : w.k) + t * w.token_stride + h * w.head_stride;
     char* out = (kind ? w.c.v : w.c.k) + page * w.c.page_stride + h * w.c.head_stride + row * w.c.token_stride;
-    float v[16];
-    load_piece<false>(x + pc.first * 16, v);
-    load_piece<false>(x + pc.second * 16, v + 8);
-    if (pc.turned) turn_pieces(v, c, s, turn.interleaved);
+    float v[2][8];
+    load_piece<false>(x + pc.at[0] * 16, v[0]);
+    load_piece<false>(x + pc.at[1] * 16, v[1]);
+    if (!kind) pc.apply(v, c, s);
     const float* scales = kind ? w.c.vs : w.c.ks;
     const float scale = E4M3 && scales ? scales[h] : 1.f;
 #pragma unroll
-    for (int half = 0; half < 2; ++half) {
-      const int piece = half ? pc.second : pc.first;
-      const i32x4 y = to_bf16x8(v + 8 * half);     // (a value as it is, a rotated key rounded)
+    for (int n = 0; n < 2; ++n) {
+      i32x4 y;                           // (a value as it is, a rotated key rounded)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) y[k] = pack(v[n] + 2 * k);
       if constexpr (E4M3) {
         int e[2];
 #pragma unroll
@@ -297,9 +288,9 @@ __global__ __launch_bounds__(256) void mala_paged_rope_write_kernel(PagedRopeWri
           const uint32_t a = (uint32_t)y[2 * i], b = (uint32_t)y[2 * i + 1];
           e[i] = to_e4m3x4(bf16_lo(a) / scale, bf16_hi(a) / scale, bf16_lo(b) / scale, bf16_hi(b) / scale);
         }
-        *reinterpret_cast<i32x2*>(out + piece * 8) = i32x2{e[0], e[1]};
+        *reinterpret_cast<i32x2*>(out + pc.at[n] * 8) = i32x2{e[0], e[1]};
       } else {
-        *reinterpret_cast<i32x4*>(out + piece * 16) = y;
+        *reinterpret_cast<i32x4*>(out + pc.at[n] * 16) = y;
       }
     }
   }
@@ -324,7 +315,7 @@ hipError_t launch_paged_block_write(PagedWriteParams p, int D, hipStream_t st) {
   return hipGetLastError();
 }
 
-template <int D>
+template <int D, bool INTER>
 static void launch_rope_write_t(PagedRopeWriteParams& p, hipStream_t st) {
   const unsigned nx = (p.q.T + rope_tokens(D) - 1) / rope_tokens(D);
   unsigned q_groups = 0;
@@ -334,19 +325,25 @@ static void launch_rope_write_t(PagedRopeWriteParams& p, hipStream_t st) {
   }
   if (p.w.c.fmt == kCacheBlock) {
     p.kv_groups = block_write_groups(p.w, true);
-    hipLaunchKernelGGL(mala_paged_block_rope_kernel<D>, dim3(p.kv_groups + q_groups), dim3(256), 0, st, p);
-    return;
+  } else {
+    p.w.heads = rope_heads_per_group(p.w.T, p.w.c.Hkv, D);
+    p.kv_groups = nx * 2 * ((p.w.c.Hkv + p.w.heads - 1) / p.w.heads);
   }
-  p.w.heads = rope_heads_per_group(p.w.T, p.w.c.Hkv, D);
-  p.kv_groups = nx * 2 * ((p.w.c.Hkv + p.w.heads - 1) / p.w.heads);
-  if (p.w.c.fmt == kCacheE4M3)
-    hipLaunchKernelGGL((mala_paged_rope_write_kernel<D, true>), dim3(p.kv_groups + q_groups), dim3(256), 0, st, p);
+  const dim3 grid(p.kv_groups + q_groups);
+  if (p.w.c.fmt == kCacheBlock)
+    hipLaunchKernelGGL((mala_paged_block_rope_kernel<D, INTER>), grid, dim3(256), 0, st, p);
+  else if (p.w.c.fmt == kCacheE4M3)
+    hipLaunchKernelGGL((mala_paged_rope_write_kernel<D, true, INTER>), grid, dim3(256), 0, st, p);
   else
-    hipLaunchKernelGGL((mala_paged_rope_write_kernel<D, false>), dim3(p.kv_groups + q_groups), dim3(256), 0, st, p);
+    hipLaunchKernelGGL((mala_paged_rope_write_kernel<D, false, INTER>), grid, dim3(256), 0, st, p);
+}
+template <int D>
+static void launch_rope_write_d(PagedRopeWriteParams& p, hipStream_t st) {
+  p.q.turn.interleaved ? launch_rope_write_t<D, true>(p, st) : launch_rope_write_t<D, false>(p, st);
 }
 
 hipError_t launch_paged_rope_write(PagedRopeWriteParams p, int D, hipStream_t st) {
-  D == 128 ? launch_rope_write_t<128>(p, st) : launch_rope_write_t<64>(p, st);
+  D == 128 ? launch_rope_write_d<128>(p, st) : launch_rope_write_d<64>(p, st);
   return hipGetLastError();
 }
 

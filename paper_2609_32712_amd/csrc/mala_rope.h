@@ -86,98 +86,135 @@ __device__ __forceinline__ void turn_pair(float& a, float& b, float c, float s) 
   b = __builtin_fmaf(b, c, as);
 }
 
-// A lane owns 16 elements of a row, two pieces of 8 which hold both elements of 8 pairs: pairs
-// 8 piece .. + 7 where the lane's number is below R / 16.
+// The 16 elements of a row that a lane owns (D / 16 lanes a row): pieces of E elements, so that each
+// is loaded and stored at once and neighbouring lanes' pieces lie side by side.  Pieces 2 i and 2 i + 1
+// hold both elements of E pairs (half), or each piece E / 2 pairs (interleaved: INTER).
+template <int D, int E, bool INTER>
 struct Pieces {
-  int first, second;     // numbers of the two pieces
-  bool turned;
-};
-__device__ __forceinline__ Pieces pieces_of(int lane_of_row, int R, int interleaved) {
-  Pieces x = {2 * lane_of_row, 2 * lane_of_row + 1, 16 * lane_of_row < R};
-  if (x.turned && !interleaved) {
-    x.first = lane_of_row;
-    x.second = lane_of_row + R / 16;
-  }
-  return x;
-}
-// x: the two pieces' elements, in order; c, s of the lane's 8 pairs
-__device__ __forceinline__ void turn_pieces(float (&x)[16], const float (&c)[8], const float (&s)[8],
-                                            int interleaved) {
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    if (interleaved)
-      turn_pair(x[2 * i], x[2 * i + 1], c[i], s[i]);
-    else
-      turn_pair(x[i], x[8 + i], c[i], s[i]);
-  }
-}
+  static constexpr int LPR = D / 16, N = 16 / E, HALF = D / (2 * E);
+  int at[N];             // their numbers in the row
+  bool turned[N];
 
-// Eight elements at p, bf16 or fp32.
-template <bool F32>
-__device__ __forceinline__ void load_piece(const char* p, float* x) {
-  if constexpr (F32) {
-    const f32x4 a = *reinterpret_cast<const f32x4*>(p), b = *reinterpret_cast<const f32x4*>(p + 16);
+  __device__ __forceinline__ Pieces(int lane_of_row, int R) {
+    const int pairs = R / (2 * E);       // pieces that hold first elements (half)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[i] = a[i];
-      x[4 + i] = b[i];
-    }
-  } else {
-    const i32x4 a = *reinterpret_cast<const i32x4*>(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      x[2 * i] = __uint_as_float((uint32_t)a[i] << 16);
-      x[2 * i + 1] = __uint_as_float((uint32_t)a[i] & 0xffff0000u);
+    for (int i = 0; i < N / 2; ++i) {
+      const int n = i * LPR + lane_of_row;
+      if constexpr (INTER) {
+        at[2 * i] = n;
+        at[2 * i + 1] = n + HALF;
+        turned[2 * i] = n * E < R;
+        turned[2 * i + 1] = (n + HALF) * E < R;
+      } else {
+        turned[2 * i] = turned[2 * i + 1] = n < pairs;
+        at[2 * i] = n < pairs ? n : n + pairs;
+        at[2 * i + 1] = n < pairs ? n + pairs : n + HALF;
+      }
     }
   }
-}
-__device__ __forceinline__ i32x4 to_bf16x8(const float* x) {
-  i32x4 y;
+  // Pairs that piece n is the (first) piece of, and the number of the first of them.
+  static constexpr int pairs_of(int n) { return INTER ? E / 2 : n % 2 ? 0 : E; }
+  __device__ __forceinline__ int first_pair(int n) const { return at[n] * (INTER ? E / 2 : E); }
+
+  // cos and sin of the lane's eight pairs, as far as they are turned
+  __device__ __forceinline__ void angles(const Turn& turn, int pos, float (&c)[8], float (&s)[8]) const {
 #pragma unroll
-  for (int i = 0; i < 4; ++i)
-    y[i] = __builtin_bit_cast(int, __builtin_convertvector((f32x2{x[2 * i], x[2 * i + 1]}), bf16x2));
-  return y;
+    for (int n = 0; n < N; ++n)
+      if (turned[n])
+#pragma unroll
+        for (int k = 0; k < pairs_of(n); ++k)
+          turn_of(pos, turn.inv_freq[first_pair(n) + k], turn.scale, turn.sin_scale, c[n * (E / 2) + k],
+                  s[n * (E / 2) + k]);
+  }
+  __device__ __forceinline__ void apply(float (&x)[N][E], const float (&c)[8], const float (&s)[8]) const {
+#pragma unroll
+    for (int n = 0; n < N; ++n)
+      if (turned[n])
+#pragma unroll
+        for (int k = 0; k < pairs_of(n); ++k) {
+          const int slot = n * (E / 2) + k;
+          if constexpr (INTER)
+            turn_pair(x[n][2 * k], x[n][2 * k + 1], c[slot], s[slot]);
+          else
+            turn_pair(x[n][k], x[n + 1][k], c[slot], s[slot]);
+        }
+  }
+};
+
+// A piece's elements at p, bf16 (4 or 8) or fp32 (4).
+__device__ __forceinline__ void unpack(uint32_t u, float* x) {
+  x[0] = __uint_as_float(u << 16);
+  x[1] = __uint_as_float(u & 0xffff0000u);
 }
-template <bool F32>
-__device__ __forceinline__ void store_piece(char* p, const float* x) {
+__device__ __forceinline__ int pack(const float* x) {
+  return __builtin_bit_cast(int, __builtin_convertvector((f32x2{x[0], x[1]}), bf16x2));
+}
+template <class T, bool ONCE>
+__device__ __forceinline__ T load_as(const char* p) {
+  if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const T*>(p));
+  return *reinterpret_cast<const T*>(p);
+}
+template <bool F32, bool ONCE = false, int E>
+__device__ __forceinline__ void load_piece(const char* p, float (&x)[E]) {
   if constexpr (F32) {
-    *reinterpret_cast<f32x4*>(p) = f32x4{x[0], x[1], x[2], x[3]};
-    *reinterpret_cast<f32x4*>(p + 16) = f32x4{x[4], x[5], x[6], x[7]};
+    f32x4 a[E / 4];
+#pragma unroll
+    for (int i = 0; i < E / 4; ++i) a[i] = load_as<f32x4, ONCE>(p + 16 * i);
+#pragma unroll
+    for (int i = 0; i < E; ++i) x[i] = a[i / 4][i % 4];
+  } else if constexpr (E == 4) {
+    const i32x2 a = load_as<i32x2, ONCE>(p);
+    unpack((uint32_t)a[0], x);
+    unpack((uint32_t)a[1], x + 2);
   } else {
-    *reinterpret_cast<i32x4*>(p) = to_bf16x8(x);
+    const i32x4 a = load_as<i32x4, ONCE>(p);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) unpack((uint32_t)a[i], x + 2 * i);
+  }
+}
+template <bool F32, int E>
+__device__ __forceinline__ void store_piece(char* p, const float (&x)[E]) {
+  static_assert(E == 4 || !F32, "16 bytes at most");
+  if constexpr (F32) {
+    const f32x4 a = {x[0], x[1], x[2], x[3]};
+    __builtin_nontemporal_store(a, reinterpret_cast<f32x4*>(p));
+  } else if constexpr (E == 4) {
+    const i32x2 a = {pack(x), pack(x + 2)};
+    __builtin_nontemporal_store(a, reinterpret_cast<i32x2*>(p));
+  } else {
+    const i32x4 a = {pack(x), pack(x + 2), pack(x + 4), pack(x + 6)};
+    __builtin_nontemporal_store(a, reinterpret_cast<i32x4*>(p));
   }
 }
 
 // Rows of the heads [h0, h0 + per) of 256 / (D / 16) tokens from number `first` on (of all
 // batches'), by a workgroup of 256 threads: D / 16 lanes a row, a thread keeps its token and with
-// it the angles.
-template <int D, bool IN32, bool OUT32>
+// it the angles.  ONCE: x is loaded past the caches.
+template <int D, bool IN32, bool OUT32, bool INTER, bool ONCE>
 __device__ __forceinline__ void turn_rows(const RopeParams& p, unsigned first, int h0) {
-  constexpr int LPR = D / 16, IN = IN32 ? 4 : 2, OUT = OUT32 ? 4 : 2;
+  // (whole pieces at a store: half lines stored at a time cost more than half lines loaded: 16000
+  // tokens' gradients, fp32 to bf16, 86 us in pieces of 8, 89 of 4)
+  constexpr int LPR = D / 16, E = OUT32 ? 4 : 8, N = 16 / E;
+  constexpr int IN = E * (IN32 ? 4 : 2), OUT = E * (OUT32 ? 4 : 2);     // bytes of a piece
   const unsigned i = first + threadIdx.x / LPR;
   if (i >= p.B * p.T) return;
-  const int lr = threadIdx.x % LPR;
   const unsigned b = i / p.T, t = i - b * p.T;
-  const Pieces pc = pieces_of(lr, p.turn.R, p.turn.interleaved);
+  const Pieces<D, E, INTER> pc(threadIdx.x % LPR, p.turn.R);
   float c[8], s[8];
-  if (pc.turned) {
-    const int pos = p.turn.pos ? p.turn.pos[b * p.turn.pos_b + t] : (int)t;
-#pragma unroll
-    for (int k = 0; k < 8; ++k)
-      turn_of(pos, p.turn.inv_freq[8 * lr + k], p.turn.scale, p.turn.sin_scale, c[k], s[k]);
-  }
+  pc.angles(p.turn, p.turn.pos ? p.turn.pos[b * p.turn.pos_b + t] : (int)t, c, s);
   const int heads = p.r[0].H + p.r[1].H, h1 = min(h0 + p.per, heads);
   for (int h = h0; h < h1; ++h) {
-    const RopeRows& r = p.r[h >= p.r[0].H];
-    const int hr = h >= p.r[0].H ? h - p.r[0].H : h;
-    const char* x = r.x + b * r.xb + hr * r.xh + t * r.xt;
-    char* out = r.out + b * r.ob + hr * r.oh + t * r.ot;
-    float v[16];
-    load_piece<IN32>(x + pc.first * 8 * IN, v);
-    load_piece<IN32>(x + pc.second * 8 * IN, v + 8);
-    if (pc.turned) turn_pieces(v, c, s, p.turn.interleaved);
-    store_piece<OUT32>(out + pc.first * 8 * OUT, v);
-    store_piece<OUT32>(out + pc.second * 8 * OUT, v + 8);
+    const bool second = h >= p.r[0].H;
+    const int hr = second ? h - p.r[0].H : h;
+    const auto of = [&](auto RopeRows::* f) { return second ? p.r[1].*f : p.r[0].*f; };
+    const char* x = of(&RopeRows::x) + hr * of(&RopeRows::xh) + (b * of(&RopeRows::xb) + t * of(&RopeRows::xt));
+    char* out = of(&RopeRows::out) + hr * of(&RopeRows::oh) + (b * of(&RopeRows::ob) + t * of(&RopeRows::ot));
+    float v[N][E];
+#pragma unroll
+    for (int n = 0; n < N; ++n) load_piece<IN32, ONCE>(x + pc.at[n] * IN, v[n]);
+    pc.apply(v, c, s);
+#pragma unroll
+    for (int n = 0; n < N; ++n) store_piece<OUT32>(out + pc.at[n] * OUT, v[n]);
   }
 }
 

@@ -8,17 +8,25 @@ namespace mala {
 
 namespace {
 
-template <int D, bool IN32, bool OUT32>
+template <int D, bool IN32, bool OUT32, bool INTER, bool ONCE>
 __global__ __launch_bounds__(256) void mala_rope_kernel(RopeParams p) {
-  turn_rows<D, IN32, OUT32>(p, blockIdx.x * (256 / (D / 16)), blockIdx.y * p.per);
+  turn_rows<D, IN32, OUT32, INTER, ONCE>(p, blockIdx.x * rope_tokens(D), blockIdx.y * p.per);
 }
 
+template <int D, bool IN32, bool OUT32, bool INTER>
+void launch_l(const RopeParams& p, hipStream_t st) {
+  const int heads = p.r[0].H + p.r[1].H;
+  const dim3 grid((p.B * p.T + rope_tokens(D) - 1) / rope_tokens(D), (heads + p.per - 1) / p.per);
+  if constexpr (D == 128)
+    if (rope_loads_once(p.B * p.T, heads, D, p.turn.R, IN32 ? 4 : 2)) {
+      hipLaunchKernelGGL((mala_rope_kernel<D, IN32, OUT32, INTER, true>), grid, dim3(256), 0, st, p);
+      return;
+    }
+  hipLaunchKernelGGL((mala_rope_kernel<D, IN32, OUT32, INTER, false>), grid, dim3(256), 0, st, p);
+}
 template <int D, bool IN32, bool OUT32>
 void launch_t(const RopeParams& p, hipStream_t st) {
-  constexpr unsigned kTokens = 256 / (D / 16);
-  const int heads = p.r[0].H + p.r[1].H;
-  const dim3 grid((p.B * p.T + kTokens - 1) / kTokens, (heads + p.per - 1) / p.per);
-  hipLaunchKernelGGL((mala_rope_kernel<D, IN32, OUT32>), grid, dim3(256), 0, st, p);
+  p.turn.interleaved ? launch_l<D, IN32, OUT32, true>(p, st) : launch_l<D, IN32, OUT32, false>(p, st);
 }
 template <int D>
 void launch_d(const RopeParams& p, bool in32, bool out32, hipStream_t st) {
