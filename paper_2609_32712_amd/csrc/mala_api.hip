@@ -529,7 +529,7 @@ int check_write(const void* k_new, const void* v_new, int64_t new_token_stride, 
     return fail(MALA_ERR_UNSUPPORTED, "k_new stride too large");
   // (a thread per 16 bytes of a row of the cache; of blocks, as the launch rule says)
   const int64_t threads = p->c.fmt == mala::kCacheBlock
-                              ? 64 * mala::block_write_plan(num_tokens, cache->Hkv, false).waves
+                              ? 256 * mala::block_write_plan(num_tokens, cache->Hkv, false).groups
                               : (int64_t)num_tokens * (cache->D / (p->c.fmt == mala::kCacheBf16 ? 8 : 16));
   if (threads > UINT32_MAX - 255)
     return fail(MALA_ERR_UNSUPPORTED, "a launch of 2^32 threads or more (num_tokens %d)", num_tokens);
@@ -539,7 +539,7 @@ int check_write(const void* k_new, const void* v_new, int64_t new_token_stride, 
   p->head_stride = new_head_stride * 2;
   p->slots = slots;
   p->T = num_tokens;
-  p->chunk = p->heads = 0;
+  p->chunk = p->units = 0;
   return MALA_OK;
 }
 
@@ -704,7 +704,7 @@ int mala_paged_rope_write(const mala_rope_rows_t* q, const void* k_new, const vo
   // one dimension
   const double groups = ((double)num_tokens / mala::rope_tokens(cache->D) + 1) *
                             (p.q.r[0].H + 2.0 * cache->Hkv) +
-                        mala::block_write_plan(num_tokens, cache->Hkv, true).waves / 4.0 + 1;
+                        (double)mala::block_write_plan(num_tokens, cache->Hkv, true).groups;
   if (groups * 256 > UINT32_MAX) return fail(MALA_ERR_UNSUPPORTED, "a launch of 2^32 threads or more");
   const hipError_t e = mala::launch_paged_rope_write(p, cache->D, (hipStream_t)stream);
   return e == hipSuccess ? MALA_OK : hip_fail(e, "mala_paged_rope_write: kernel launch");

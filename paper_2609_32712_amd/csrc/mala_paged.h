@@ -53,7 +53,7 @@ struct PagedWriteParams {
   int64_t token_stride, head_stride;
   const int32_t* slots;
   int T;
-  int chunk, heads;     // tokens and heads at a time, set by the launch
+  int chunk, units;     // tokens and heads at a time (see block_write_plan), set by the launch
 };
 
 struct PagedReadParams {

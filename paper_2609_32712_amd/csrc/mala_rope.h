@@ -34,6 +34,7 @@ struct RopeParams {
   Turn turn;
   unsigned B, T;
   int per;                 // heads per workgroup
+  bool heads_first;        // order of the workgroups
 };
 
 struct PagedRopeWriteParams {
@@ -141,7 +142,6 @@ struct Pieces {
   }
 };
 
-// A piece's elements at p, bf16 (4 or 8) or fp32 (4).
 __device__ __forceinline__ void unpack(uint32_t u, float* x) {
   x[0] = __uint_as_float(u << 16);
   x[1] = __uint_as_float(u & 0xffff0000u);
@@ -149,41 +149,61 @@ __device__ __forceinline__ void unpack(uint32_t u, float* x) {
 __device__ __forceinline__ int pack(const float* x) {
   return __builtin_bit_cast(int, __builtin_convertvector((f32x2{x[0], x[1]}), bf16x2));
 }
-template <class T, bool ONCE>
-__device__ __forceinline__ T load_as(const char* p) {
-  if constexpr (ONCE) return __builtin_nontemporal_load(reinterpret_cast<const T*>(p));
-  return *reinterpret_cast<const T*>(p);
-}
-template <bool F32, bool ONCE = false, int E>
-__device__ __forceinline__ void load_piece(const char* p, float (&x)[E]) {
-  if constexpr (F32) {
-    f32x4 a[E / 4];
-#pragma unroll
-    for (int i = 0; i < E / 4; ++i) a[i] = load_as<f32x4, ONCE>(p + 16 * i);
-#pragma unroll
-    for (int i = 0; i < E; ++i) x[i] = a[i / 4][i % 4];
-  } else if constexpr (E == 4) {
-    const i32x2 a = load_as<i32x2, ONCE>(p);
-    unpack((uint32_t)a[0], x);
-    unpack((uint32_t)a[1], x + 2);
-  } else {
-    const i32x4 a = load_as<i32x4, ONCE>(p);
-#pragma unroll
-    for (int i = 0; i < 4; ++i) unpack((uint32_t)a[i], x + 2 * i);
-  }
-}
+
+// A piece of E elements as it lies in memory, bf16 or fp32: 8, 16 or 32 bytes.
 template <bool F32, int E>
-__device__ __forceinline__ void store_piece(char* p, const float (&x)[E]) {
-  static_assert(E == 4 || !F32, "16 bytes at most");
-  if constexpr (F32) {
-    const f32x4 a = {x[0], x[1], x[2], x[3]};
-    __builtin_nontemporal_store(a, reinterpret_cast<f32x4*>(p));
-  } else if constexpr (E == 4) {
-    const i32x2 a = {pack(x), pack(x + 2)};
-    __builtin_nontemporal_store(a, reinterpret_cast<i32x2*>(p));
-  } else {
-    const i32x4 a = {pack(x), pack(x + 2), pack(x + 4), pack(x + 6)};
-    __builtin_nontemporal_store(a, reinterpret_cast<i32x4*>(p));
+struct RawPiece {
+  static constexpr int WORDS = E * (F32 ? 4 : 2) / 4;
+  int d[WORDS];
+
+  // ONCE: past the caches
+  template <bool ONCE>
+  __device__ __forceinline__ void load(const char* p) {
+    typedef int vec __attribute__((ext_vector_type(WORDS < 4 ? WORDS : 4)));
+#pragma unroll
+    for (int i = 0; i < WORDS; i += 4) {
+      const vec* at = reinterpret_cast<const vec*>(p + 4 * i);
+      const vec x = ONCE ? __builtin_nontemporal_load(at) : *at;
+#pragma unroll
+      for (int k = 0; k < 4 && k < WORDS; ++k) d[i + k] = x[k];
+    }
+  }
+  __device__ __forceinline__ void store(char* p) const {
+    typedef int vec __attribute__((ext_vector_type(WORDS < 4 ? WORDS : 4)));
+#pragma unroll
+    for (int i = 0; i < WORDS; i += 4) {
+      vec x;
+#pragma unroll
+      for (int k = 0; k < 4 && k < WORDS; ++k) x[k] = d[i + k];
+      __builtin_nontemporal_store(x, reinterpret_cast<vec*>(p + 4 * i));
+    }
+  }
+  __device__ __forceinline__ void get(float (&x)[E]) const {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) {
+      if constexpr (F32)
+        x[i] = __int_as_float(d[i]);
+      else
+        unpack((uint32_t)d[i], x + 2 * i);
+    }
+  }
+  __device__ __forceinline__ void set(const float (&x)[E]) {
+#pragma unroll
+    for (int i = 0; i < WORDS; ++i) {
+      if constexpr (F32)
+        d[i] = __float_as_int(x[i]);
+      else
+        d[i] = pack(x + 2 * i);
+    }
+  }
+};
+// Exchanges a with lane `with`'s b where `first`, b with its a where not; with itself: nothing.
+template <class Raw>
+__device__ __forceinline__ void swap_pieces(Raw& a, Raw& b, int with, bool first) {
+#pragma unroll
+  for (int i = 0; i < Raw::WORDS; ++i) {
+    const int got = __builtin_amdgcn_ds_bpermute(4 * with, first ? b.d[i] : a.d[i]);
+    (first ? b.d[i] : a.d[i]) = got;
   }
 }
 
@@ -202,6 +222,15 @@ __device__ __forceinline__ void turn_rows(const RopeParams& p, unsigned first, i
   const Pieces<D, E, INTER> pc(threadIdx.x % LPR, p.turn.R);
   float c[8], s[8];
   pc.angles(p.turn, p.turn.pos ? p.turn.pos[b * p.turn.pos_b + t] : (int)t, c, s);
+  // Where up to half of each head turns, the two halves of a turned pair come from one line: lanes then
+  // load and store pieces lane and lane + LPR, whole lines, and swap one of them for the one they turn.
+  const bool lines = !INTER && E == 8 && 2 * p.turn.R <= D;
+  const int lr = threadIdx.x % LPR, lane = threadIdx.x & 63, half = p.turn.R / 16;
+  const bool low = lr < half;
+  const int with = low ? lane + half : lr < 2 * half ? lane - half : lane;
+  int at[N];
+#pragma unroll
+  for (int n = 0; n < N; ++n) at[n] = lines ? lr + n * LPR : pc.at[n];
   const int heads = p.r[0].H + p.r[1].H, h1 = min(h0 + p.per, heads);
   for (int h = h0; h < h1; ++h) {
     const bool second = h >= p.r[0].H;
@@ -209,12 +238,20 @@ __device__ __forceinline__ void turn_rows(const RopeParams& p, unsigned first, i
     const auto of = [&](auto RopeRows::* f) { return second ? p.r[1].*f : p.r[0].*f; };
     const char* x = of(&RopeRows::x) + hr * of(&RopeRows::xh) + (b * of(&RopeRows::xb) + t * of(&RopeRows::xt));
     char* out = of(&RopeRows::out) + hr * of(&RopeRows::oh) + (b * of(&RopeRows::ob) + t * of(&RopeRows::ot));
+    RawPiece<IN32, E> in[N];
+    RawPiece<OUT32, E> y[N];
     float v[N][E];
 #pragma unroll
-    for (int n = 0; n < N; ++n) load_piece<IN32, ONCE>(x + pc.at[n] * IN, v[n]);
+    for (int n = 0; n < N; ++n) in[n].template load<ONCE>(x + at[n] * IN);
+    if (lines) swap_pieces(in[0], in[1], with, low);
+#pragma unroll
+    for (int n = 0; n < N; ++n) in[n].get(v[n]);
     pc.apply(v, c, s);
 #pragma unroll
-    for (int n = 0; n < N; ++n) store_piece<OUT32>(out + pc.at[n] * OUT, v[n]);
+    for (int n = 0; n < N; ++n) y[n].set(v[n]);
+    if (lines) swap_pieces(y[0], y[1], with, low);
+#pragma unroll
+    for (int n = 0; n < N; ++n) y[n].store(out + at[n] * OUT);
   }
 }
 
