@@ -533,15 +533,15 @@ def mala_paged_update(lens, new_lens, block_table, free_ring, free_state, lens_o
 
 def _new_rows(k_new, v_new, slots, c):
     """The checks of the rows that a write takes; (T, token stride, head stride)."""
-    Hkv, T, D = _shape(k_new, "k_new", 3)
+    Hkv, T, D = shape = _shape(k_new, "k_new", 3)
     _shape(v_new, "v_new", 3)
-    if k_new.dtype != torch.bfloat16 or v_new.dtype != torch.bfloat16:
+    if k_new.dtype is not torch.bfloat16 or v_new.dtype is not torch.bfloat16:
         raise TypeError("k_new and v_new must have dtype %s, got %s and %s"
                         % (torch.bfloat16, k_new.dtype, v_new.dtype))
     if Hkv != c.Hkv or D != c.D:
         raise ValueError("k_new must have shape %s, got %s" % ((c.Hkv, T, c.D), (Hkv, T, D)))
     st = k_new.stride()
-    if v_new.shape != k_new.shape or (v_new.stride() != st and T):
+    if v_new.shape != shape or (v_new.stride() != st and T):
         raise ValueError("v_new must have the shape and strides of k_new")
     if st[2] != 1 and T:
         raise ValueError("the rows of k_new must be contiguous")
@@ -563,13 +563,13 @@ def mala_paged_write(k_new, v_new, slots, cache, stream=None):
             v_new.data_ptr(), token_stride, head_stride, slots.data_ptr(), c._ref, T)
 
 
-def _rope_rows(x, out, name, shape, dtypes, device):
+def _rope_rows(x, out, name, shape, t_in, t_out, device):
     """The bytes of a mala_rope_rows_t of x and out [(B,) H, T, D], rows contiguous."""
     if not isinstance(out, torch.Tensor) or out.shape != shape:
         raise ValueError("%s_out must have shape %s" % (name, tuple(shape)))
-    if (x.dtype, out.dtype) != dtypes:
-        raise TypeError("%s and %s_out must have dtypes %s, got %s"
-                        % (name, name, dtypes, (x.dtype, out.dtype)))
+    if x.dtype is not t_in or out.dtype is not t_out:
+        raise TypeError("%s and %s_out must have dtypes %s and %s, got %s and %s"
+                        % (name, name, t_in, t_out, x.dtype, out.dtype))
     if x.get_device() != device or out.get_device() != device or device < 0:
         raise TypeError("%s and %s_out must be CUDA (HIP) tensors on the device of the others"
                         % (name, name))
@@ -577,20 +577,20 @@ def _rope_rows(x, out, name, shape, dtypes, device):
     if (a[-1] != 1 or b[-1] != 1) and x.numel():
         raise ValueError("the rows of %s and %s_out must be contiguous" % (name, name))
     if len(shape) == 3:
-        a, b = (0, *a), (0, *b)
-    return _ROPE_ROWS.pack(x.data_ptr(), out.data_ptr(), a[0], a[1], a[2], b[0], b[1], b[2], shape[-3])
+        return _ROPE_ROWS.pack(x.data_ptr(), out.data_ptr(), 0, a[0], a[1], 0, b[0], b[1], shape[0])
+    return _ROPE_ROWS.pack(x.data_ptr(), out.data_ptr(), a[0], a[1], a[2], b[0], b[1], b[2], shape[1])
 
 
 def _rope_turn(positions, inv_freq, layout, scale, B, T, device):
     """The bytes of a mala_rope_t; positions [T], [B, T] or None."""
-    _args(device, (inv_freq, "inv_freq", torch.float64, _shape(inv_freq, "inv_freq", 1)))
-    at, stride = None, 0
-    if positions is not None:
-        if isinstance(positions, torch.Tensor) and positions.dim() == 2:
-            stride = T
-        _args(device, (positions, "positions", torch.int32, (B, T) if stride else (T,)))
-        at = positions.data_ptr()
-    return _ROPE.pack(at or 0, stride, inv_freq.data_ptr(), 2 * inv_freq.shape[0], layout, scale)
+    (n,) = shape = _shape(inv_freq, "inv_freq", 1)
+    if positions is None:
+        _args(device, (inv_freq, "inv_freq", torch.float64, shape))
+        return _ROPE.pack(0, 0, inv_freq.data_ptr(), 2 * n, layout, scale)
+    each = isinstance(positions, torch.Tensor) and positions.dim() == 2
+    _args(device, (inv_freq, "inv_freq", torch.float64, shape),
+          (positions, "positions", torch.int32, (B, T) if each else (T,)))
+    return _ROPE.pack(positions.data_ptr(), T if each else 0, inv_freq.data_ptr(), 2 * n, layout, scale)
 
 
 def mala_rope(q, k, q_out, k_out, positions, inv_freq, layout=ROPE_HALF, scale=1.0, inverse=False,
@@ -603,22 +603,23 @@ def mala_rope(q, k, q_out, k_out, positions, inv_freq, layout=ROPE_HALF, scale=1
     if not isinstance(q, torch.Tensor) or q.dim() not in (3, 4):
         raise ValueError("q must be a [B, H, T, D] or [H, T, D] tensor")
     shape, dev = q.shape, _device(q, "q")
-    B, T, D = shape[0] if len(shape) == 4 else 1, shape[-2], shape[-1]
+    *batch, _, T, D = shape
     if not isinstance(q_out, torch.Tensor) or q.dtype not in _OUT or q_out.dtype not in _OUT:
         raise TypeError("q and q_out must be tensors of dtype %s" % (_OUT,))
-    dtypes = q.dtype, q_out.dtype
-    rows, more = _rope_rows(q, q_out, "q", shape, dtypes, dev), None
+    t_in, t_out = q.dtype, q_out.dtype
+    rows, more = _rope_rows(q, q_out, "q", shape, t_in, t_out, dev), None
     if k is not None:
-        if not isinstance(k, torch.Tensor) or k.dim() != len(shape) or (B, T, D) != (
-                k.shape[0] if len(shape) == 4 else 1, k.shape[-2], k.shape[-1]):
+        other = k.shape if isinstance(k, torch.Tensor) else ()
+        if len(other) != len(shape) or other[-2:] != shape[-2:] or other[:-3] != shape[:-3]:
             raise ValueError("k must have the batch, tokens and head size of q")
-        more = _rope_rows(k, k_out, "k", k.shape, dtypes, dev)
+        more = _rope_rows(k, k_out, "k", other, t_in, t_out, dev)
     elif k_out is not None:
         raise ValueError("k_out without k")
+    B = batch[0] if batch else 1
     turn = _rope_turn(positions, inv_freq, layout, scale, B, T, dev)
     _launch(dev, stream, (_lib or load_library()).mala_rope, rows, more, turn, B, T, D,
-            OUT_BF16 if dtypes[0] is torch.bfloat16 else OUT_F32,
-            OUT_BF16 if dtypes[1] is torch.bfloat16 else OUT_F32, 1 if inverse else 0)
+            OUT_BF16 if t_in is torch.bfloat16 else OUT_F32,
+            OUT_BF16 if t_out is torch.bfloat16 else OUT_F32, 1 if inverse else 0)
 
 
 def mala_paged_rope_write(q, q_out, k_new, v_new, positions, slots, cache, inv_freq, layout=ROPE_HALF,
@@ -633,7 +634,7 @@ def mala_paged_rope_write(q, q_out, k_new, v_new, positions, slots, cache, inv_f
         shape = _shape(q, "q", 3)
         if shape[1] != T or shape[2] != c.D:
             raise ValueError("q must have %d tokens of %d, got shape %s" % (T, c.D, tuple(shape)))
-        rows = _rope_rows(q, q_out, "q", shape, (torch.bfloat16, torch.bfloat16), c.device)
+        rows = _rope_rows(q, q_out, "q", shape, torch.bfloat16, torch.bfloat16, c.device)
     elif q_out is not None:
         raise ValueError("q_out without q")
     turn = _rope_turn(positions, inv_freq, layout, scale, 1, T, c.device)

@@ -255,13 +255,14 @@ __global__ __launch_bounds__(256) void mala_paged_write_kernel(PagedWriteParams 
 }
 
 // ------------------------------------------------------------------ pages to packed rows
-// A workgroup takes kReadRows consecutive packed rows (of every head).  HBM-bound.
-constexpr int kReadRows = 4;
-template <int D, int FMT>
+// A workgroup takes ROWS consecutive packed rows (of every head).  HBM-bound.  Rows of bytes are read
+// 8 at a time, half lines, by ordinary loads: past the caches each half fetched its line again (10 caches
+// of up to 10000 rows, 8 heads, 62.4 / 59.9 us; 32 of up to 8000, 2 heads, 41.2 / 29.8).
+template <int D, int FMT, int ROWS>
 __global__ __launch_bounds__(256) void mala_paged_read_kernel(PagedReadParams p) {
   constexpr int CPR = D / 8;             // pieces of 8 values per row
   __shared__ int s_seq;
-  const int tid = threadIdx.x, row0 = blockIdx.x * kReadRows, Hkv = p.c.Hkv;
+  const int tid = threadIdx.x, row0 = blockIdx.x * ROWS, Hkv = p.c.Hkv;
   const unsigned P = p.c.page_size;
   if (tid == 0) s_seq = 0;
   __syncthreads();
@@ -271,8 +272,8 @@ __global__ __launch_bounds__(256) void mala_paged_read_kernel(PagedReadParams p)
   __syncthreads();
   const int seq0 = max(s_seq - 1, 0);
   // a thread keeps its piece of the row and its row, and goes on by heads
-  constexpr int HEADS = 256 / (CPR * kReadRows);   // heads at a time
-  const int c = tid % CPR, row = row0 + tid / CPR % kReadRows;
+  constexpr int HEADS = 256 / (CPR * ROWS);   // heads at a time
+  const int c = tid % CPR, row = row0 + tid / CPR % ROWS;
   int b = seq0;
   while (b < p.S && p.cu[b + 1] <= row) ++b;
   if (b >= p.S || row >= p.total) return;
@@ -283,27 +284,30 @@ __global__ __launch_bounds__(256) void mala_paged_read_kernel(PagedReadParams p)
   const bool there = (unsigned)number < (unsigned)p.c.num_pages;
   const long at = there ? (long)number * p.c.page_stride + off * p.c.token_stride : 0;
 #pragma unroll 4
-  for (int h = tid / (CPR * kReadRows); h < Hkv; h += HEADS) {
+  for (int h = tid / (CPR * ROWS); h < Hkv; h += HEADS) {
     const long dst = (((long)h * p.total + row) * D + c * 8) * 2;
     if constexpr (FMT != kCacheBf16) {
       const long src = at + h * p.c.head_stride + c * 8;
       i32x2 a = {0, 0}, v = a;
       if (there) {
-        a = load_once<i32x2>(p.c.k + src);
-        v = load_once<i32x2>(p.c.v + src);
+        a = *reinterpret_cast<const i32x2*>(p.c.k + src);
+        v = *reinterpret_cast<const i32x2*>(p.c.v + src);
       }
       const auto put = [&](char* out, const i32x2& x, float s) {
-        bf16x8 y;
+        i32x4 y;
 #pragma unroll
         for (int j = 0; j < 2; ++j) {
-          const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(x[j], false);
-          const f32x2 hi = __builtin_amdgcn_cvt_pk_f32_fp8(x[j], true);
-          y[4 * j] = (bf16)(lo[0] * s);
-          y[4 * j + 1] = (bf16)(lo[1] * s);
-          y[4 * j + 2] = (bf16)(hi[0] * s);
-          y[4 * j + 3] = (bf16)(hi[1] * s);
+          if constexpr (FMT == kCacheBlock) {      // (by a power of two: exact)
+            y[2 * j] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[j], s, false));
+            y[2 * j + 1] = __builtin_bit_cast(int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(x[j], s, true));
+          } else {
+            const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(x[j], false);
+            const f32x2 hi = __builtin_amdgcn_cvt_pk_f32_fp8(x[j], true);
+            y[2 * j] = __builtin_bit_cast(int, bf16x2{(bf16)(lo[0] * s), (bf16)(lo[1] * s)});
+            y[2 * j + 1] = __builtin_bit_cast(int, bf16x2{(bf16)(hi[0] * s), (bf16)(hi[1] * s)});
+          }
         }
-        store_once(out + dst, __builtin_bit_cast(i32x4, y));
+        store_once(out + dst, y);
       };
       float ks = 1.f, vs = 1.f;
       if constexpr (FMT == kCacheBlock) {
@@ -360,12 +364,21 @@ hipError_t launch_paged_write(const PagedWriteParams& p, int D, hipStream_t st) 
   return hipGetLastError();
 }
 
+template <int D, int FMT, int ROWS>
+static void launch_read_r(const PagedReadParams& p, hipStream_t st) {
+  const unsigned grid = (unsigned)(((long)p.total + ROWS - 1) / ROWS);
+  hipLaunchKernelGGL((mala_paged_read_kernel<D, FMT, ROWS>), dim3(grid), dim3(256), 0, st, p);
+}
+// Rows of a workgroup: eight of a large batch, and where the threads of four would be more than there
+// are heads for.  us per call of four / eight: 2000 rows of 8 heads 3.8 / 4.4, 8000 9.9 / 9.9, 10 caches
+// of up to 10000 62.4 / 59.9, 32 of up to 8000 with 2 heads 42.1 / 29.8.
 template <int D, int FMT>
 static void launch_read_t(const PagedReadParams& p, hipStream_t st) {
-  const unsigned grid = (unsigned)(((long)p.total + kReadRows - 1) / kReadRows);
-  hipLaunchKernelGGL((mala_paged_read_kernel<D, FMT>), dim3(grid), dim3(256), 0, st, p);
+  if (FMT != kCacheBf16 && (p.total >= 16384 || p.c.Hkv * (D / 8) < 64))
+    launch_read_r<D, FMT, FMT == kCacheBf16 ? 4 : 8>(p, st);
+  else
+    launch_read_r<D, FMT, 4>(p, st);
 }
-
 template <int D>
 static void launch_read_d(const PagedReadParams& p, hipStream_t st) {
   if (p.c.fmt == kCacheBlock)

@@ -45,8 +45,8 @@ inline bool rope_loads_once(unsigned tokens, int heads, int D, int R, int size) 
 // few tokens to a workgroup (one behind the other), large ones fewer workgroups that find no block's
 // first token; with whole chunks a workgroup per some heads, or where keys are turned, angles
 // computed for as many of them as possible.  us per call with 2 / 4 / 16 workgroups per CU: writes of
-// 20000 tokens of 8 heads 22.3 / 22.3 / 20.7, of 1000 decodes 4.6 / 4.8 / 6.3; turned 16000 tokens with
-// 32 heads' queries 71.3 / 71.2 / 77.0, 512 decodes 5.7 / 7.1 / 7.1.
+// 20000 tokens of 8 heads 22.3 / 22.3 / 20.7, of 2000 6.9 / 5.6 / 5.3, of 1000 decodes 5.1 / 4.8 / 6.3; turned
+// 16000 tokens with 32 heads' queries 71.3 / 71.2 / 77.0, 512 decodes 5.7 / 7.1 / 7.1.
 constexpr int kBlockChunk = 16;
 struct BlockWritePlan {
   int chunk, units;
@@ -57,7 +57,7 @@ inline BlockWritePlan block_write_plan(int T, int Hkv, bool rope) {
   BlockWritePlan x;
   x.chunk = std::clamp(T / kNumCus, 1, kBlockChunk);
   const int64_t chunks = ((int64_t)T + x.chunk - 1) / x.chunk;
-  const int64_t want = (x.chunk < kBlockChunk ? 2 : rope ? 4 : 16) * kNumCus;
+  const int64_t want = (x.chunk == kBlockChunk ? (rope ? 4 : 16) : rope ? 2 : 4) * kNumCus;
   const int64_t parts = std::clamp<int64_t>(want / chunks, 1, (2 * (int64_t)Hkv + 3) / 4);
   x.units = (int)((2 * (int64_t)Hkv + 4 * parts - 1) / (4 * parts));
   x.groups = chunks * block_write_parts(Hkv, x.units);
