@@ -396,12 +396,13 @@ __global__ __launch_bounds__(256) void mala_paged_block_write_kernel(PagedWriteP
   BlockWriter<D, false, false>(p, turn).run(blockIdx.x, none);
 }
 
-// Keys and values into a block-scaled cache by the first workgroups, queries by the others.  (In turns
-// they gain nothing: 16000 tokens, 32 + 8 heads, 72.0 us, in turns 75.5.)
+// Keys and values into a block-scaled cache by the first workgroups, queries by the others: two heads
+// at a time, since the first kind's registers leave room for half as many wavefronts (16000 tokens,
+// 32 + 8 heads, 73.2 / 69.5 us).  In turns, or the queries first, they take longer (75.5, 75.9).
 template <int D, bool INTER>
 __device__ __forceinline__ void turn_queries(const PagedRopeWriteParams& p) {
   const unsigned nx = (p.q.T + rope_tokens(D) - 1) / rope_tokens(D), i = blockIdx.x - p.kv_groups;
-  turn_rows<D, false, false, INTER, false>(p.q, i % nx * rope_tokens(D), (int)(i / nx) * p.q.per);
+    turn_rows<D, false, false, INTER, false, 2>(p.q, i % nx * rope_tokens(D), (int)(i / nx) * p.q.per);
 }
 
 template <int D, bool INTER>

@@ -209,8 +209,9 @@ __device__ __forceinline__ void swap_pieces(Raw& a, Raw& b, int with, bool first
 
 // Rows of the heads [h0, h0 + per) of 256 / (D / 16) tokens from number `first` on (of all
 // batches'), by a workgroup of 256 threads: D / 16 lanes a row, a thread keeps its token and with
-// it the angles.  ONCE: x is loaded past the caches.
-template <int D, bool IN32, bool OUT32, bool INTER, bool ONCE>
+// it the angles.  ONCE: x is loaded past the caches.  HEADS: heads whose rows are loaded at a time.  (In
+// place: a row is read by the lanes that write it, before they do.)
+template <int D, bool IN32, bool OUT32, bool INTER, bool ONCE, int HEADS>
 __device__ __forceinline__ void turn_rows(const RopeParams& p, unsigned first, int h0) {
   // (whole pieces at a store: half lines stored at a time cost more than half lines loaded: 16000
   // tokens' gradients, fp32 to bf16, 86 us in pieces of 8, 89 of 4)
@@ -232,26 +233,35 @@ __device__ __forceinline__ void turn_rows(const RopeParams& p, unsigned first, i
 #pragma unroll
   for (int n = 0; n < N; ++n) at[n] = lines ? lr + n * LPR : pc.at[n];
   const int heads = p.r[0].H + p.r[1].H, h1 = min(h0 + p.per, heads);
-  for (int h = h0; h < h1; ++h) {
-    const bool second = h >= p.r[0].H;
-    const int hr = second ? h - p.r[0].H : h;
-    const auto of = [&](auto RopeRows::* f) { return second ? p.r[1].*f : p.r[0].*f; };
-    const char* x = of(&RopeRows::x) + hr * of(&RopeRows::xh) + (b * of(&RopeRows::xb) + t * of(&RopeRows::xt));
-    char* out = of(&RopeRows::out) + hr * of(&RopeRows::oh) + (b * of(&RopeRows::ob) + t * of(&RopeRows::ot));
-    RawPiece<IN32, E> in[N];
-    RawPiece<OUT32, E> y[N];
-    float v[N][E];
+  const auto of = [&](int h, auto RopeRows::* f) { return h >= p.r[0].H ? p.r[1].*f : p.r[0].*f; };
+  for (int h = h0; h < h1; h += HEADS) {
+    RawPiece<IN32, E> in[HEADS][N];
 #pragma unroll
-    for (int n = 0; n < N; ++n) in[n].template load<ONCE>(x + at[n] * IN);
-    if (lines) swap_pieces(in[0], in[1], with, low);
+    for (int k = 0; k < HEADS; ++k) {
+      const int g = min(h + k, h1 - 1), hr = g >= p.r[0].H ? g - p.r[0].H : g;
+      const char* x = of(g, &RopeRows::x) + hr * of(g, &RopeRows::xh) +
+                      (b * of(g, &RopeRows::xb) + t * of(g, &RopeRows::xt));
 #pragma unroll
-    for (int n = 0; n < N; ++n) in[n].get(v[n]);
-    pc.apply(v, c, s);
+      for (int n = 0; n < N; ++n) in[k][n].template load<ONCE>(x + at[n] * IN);
+    }
 #pragma unroll
-    for (int n = 0; n < N; ++n) y[n].set(v[n]);
-    if (lines) swap_pieces(y[0], y[1], with, low);
+    for (int k = 0; k < HEADS; ++k) {
+      const int g = h + k, hr = g >= p.r[0].H ? g - p.r[0].H : g;
+      if (g >= h1) break;
+      RawPiece<OUT32, E> y[N];
+      float v[N][E];
+      if (lines) swap_pieces(in[k][0], in[k][1], with, low);
 #pragma unroll
-    for (int n = 0; n < N; ++n) y[n].store(out + at[n] * OUT);
+      for (int n = 0; n < N; ++n) in[k][n].get(v[n]);
+      pc.apply(v, c, s);
+#pragma unroll
+      for (int n = 0; n < N; ++n) y[n].set(v[n]);
+      if (lines) swap_pieces(y[0], y[1], with, low);
+      char* out = of(g, &RopeRows::out) + hr * of(g, &RopeRows::oh) +
+                  (b * of(g, &RopeRows::ob) + t * of(g, &RopeRows::ot));
+#pragma unroll
+      for (int n = 0; n < N; ++n) y[n].store(out + at[n] * OUT);
+    }
   }
 }
 

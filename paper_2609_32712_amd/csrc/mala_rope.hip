@@ -13,9 +13,9 @@ __global__ __launch_bounds__(256) void mala_rope_kernel(RopeParams p) {
     // consecutive workgroups: the tokens of some heads, or (heads_first) the heads of some tokens
   const unsigned slices = gridDim.y, i = blockIdx.x + blockIdx.y * gridDim.x;
   if (p.heads_first)
-    turn_rows<D, IN32, OUT32, INTER, ONCE>(p, i / slices * rope_tokens(D), i % slices * p.per);
+    turn_rows<D, IN32, OUT32, INTER, ONCE, 1>(p, i / slices * rope_tokens(D), i % slices * p.per);
   else
-    turn_rows<D, IN32, OUT32, INTER, ONCE>(p, blockIdx.x * rope_tokens(D), blockIdx.y * p.per);
+    turn_rows<D, IN32, OUT32, INTER, ONCE, 1>(p, blockIdx.x * rope_tokens(D), blockIdx.y * p.per);
 }
 
 template <int D, bool IN32, bool OUT32, bool INTER>
