@@ -495,6 +495,12 @@ int check_cache(const mala_paged_cache_t* c, mala::PagedCache* out) {
     return fail(MALA_ERR_UNSUPPORTED, "16 rows of the cache span 2^31 bytes");
   if ((uintptr_t)c->k_pages % 16 || (uintptr_t)c->v_pages % 16)
     return fail(MALA_ERR_INVALID_ARG, "k_pages or v_pages not 16-byte aligned");
+  if (block) {
+    const uintptr_t a = (uintptr_t)c->k_block_scale, b = (uintptr_t)c->v_block_scale;
+    const uintptr_t n = (uintptr_t)c->num_pages * c->Hkv * (c->page_size / mala::kPageRows);
+    if (a < b + n && b < a + n)
+      return fail(MALA_ERR_INVALID_ARG, "k_block_scale and v_block_scale share memory");
+  }
   if (out) {
     out->k = (char*)c->k_pages;
     out->v = (char*)c->v_pages;

@@ -90,7 +90,7 @@ def test_rope_nulls_and_nothing_to_do():
 def _block_cache(**kw):
     a = dict(k_pages=256, v_pages=512, k_scale=None, v_scale=None, page_stride=4 * 32 * 128,
              head_stride=32 * 128, token_stride=128, num_pages=10, page_size=32, Hkv=4, D=128,
-             dtype=mala.CACHE_E4M3_BLOCK, k_block_scale=64, v_block_scale=64)
+             dtype=mala.CACHE_E4M3_BLOCK, k_block_scale=64, v_block_scale=1 << 16)
     a.update(kw)
     return mala._PagedCacheStruct(**a)
 
@@ -98,7 +98,8 @@ def _block_cache(**kw):
 @pytest.mark.parametrize("kw,want", [
     (dict(k_block_scale=None), BAD), (dict(v_block_scale=None), BAD), (dict(k_scale=64), BAD),
     (dict(v_scale=64), BAD), (dict(dtype=3), BAD), (dict(token_stride=136), BAD), (dict(D=96), UNSUP),
-    (dict(page_size=24), UNSUP), (dict(k_pages=264), BAD), (dict(num_pages=1 << 27), UNSUP)])
+    (dict(page_size=24), UNSUP), (dict(k_pages=264), BAD), (dict(num_pages=1 << 27), UNSUP),
+    (dict(v_block_scale=64), BAD), (dict(v_block_scale=64 + 79), BAD), (dict(k_block_scale=(1 << 16) + 79), BAD)])
 def test_block_caches_are_refused(kw, want):
     lib, c = mala.load_library(), ctypes.byref(_block_cache(**kw))
     _refused(lib.mala_paged_write(256, 512, 512, 128, 16, c, 4, None), want)
