@@ -145,6 +145,7 @@ def _check(status):
 
 
 _OUT = (torch.float32, torch.bfloat16)
+_OUT_CODES = {torch.float32: OUT_F32, torch.bfloat16: OUT_BF16}
 
 
 def _spec(t, name, dtype, shape, optional=False):
@@ -573,24 +574,33 @@ def _rope_rows(x, out, name, shape, t_in, t_out, device):
     if x.get_device() != device or out.get_device() != device or device < 0:
         raise TypeError("%s and %s_out must be CUDA (HIP) tensors on the device of the others"
                         % (name, name))
-    a, b = x.stride(), out.stride()
-    if (a[-1] != 1 or b[-1] != 1) and x.numel():
-        raise ValueError("the rows of %s and %s_out must be contiguous" % (name, name))
     if len(shape) == 3:
-        return _ROPE_ROWS.pack(x.data_ptr(), out.data_ptr(), 0, a[0], a[1], 0, b[0], b[1], shape[0])
-    return _ROPE_ROWS.pack(x.data_ptr(), out.data_ptr(), a[0], a[1], a[2], b[0], b[1], b[2], shape[1])
+        (xh, xt, xd), (oh, ot, od) = x.stride(), out.stride()
+        xb = ob = 0
+    else:
+        (xb, xh, xt, xd), (ob, oh, ot, od) = x.stride(), out.stride()
+    if (xd != 1 or od != 1) and x.numel():
+        raise ValueError("the rows of %s and %s_out must be contiguous" % (name, name))
+    return _ROPE_ROWS.pack(x.data_ptr(), out.data_ptr(), xb, xh, xt, ob, oh, ot, shape[-3])
 
 
 def _rope_turn(positions, inv_freq, layout, scale, B, T, device):
     """The bytes of a mala_rope_t; positions [T], [B, T] or None."""
-    (n,) = shape = _shape(inv_freq, "inv_freq", 1)
-    if positions is None:
-        _args(device, (inv_freq, "inv_freq", torch.float64, shape))
-        return _ROPE.pack(0, 0, inv_freq.data_ptr(), 2 * n, layout, scale)
-    each = isinstance(positions, torch.Tensor) and positions.dim() == 2
-    _args(device, (inv_freq, "inv_freq", torch.float64, shape),
-          (positions, "positions", torch.int32, (B, T) if each else (T,)))
-    return _ROPE.pack(positions.data_ptr(), T if each else 0, inv_freq.data_ptr(), 2 * n, layout, scale)
+    # (as _args: one quick look where everything is right)
+    if not (type(inv_freq) is torch.Tensor and inv_freq.dtype is torch.float64 and inv_freq.dim() == 1
+            and inv_freq.get_device() == device and inv_freq.is_contiguous()):
+        _args(device, (inv_freq, "inv_freq", torch.float64, _shape(inv_freq, "inv_freq", 1)))
+    at, stride = 0, 0
+    if positions is not None:
+        shape = (T,)
+        if isinstance(positions, torch.Tensor) and positions.dim() == 2:
+            shape, stride = (B, T), T
+        if not (type(positions) is torch.Tensor and positions.dtype is torch.int32
+                and positions.shape == shape and positions.get_device() == device
+                and positions.is_contiguous()):
+            _args(device, (positions, "positions", torch.int32, shape))
+        at = positions.data_ptr()
+    return _ROPE.pack(at, stride, inv_freq.data_ptr(), 2 * inv_freq.numel(), layout, scale)
 
 
 def mala_rope(q, k, q_out, k_out, positions, inv_freq, layout=ROPE_HALF, scale=1.0, inverse=False,
@@ -600,26 +610,29 @@ def mala_rope(q, k, q_out, k_out, positions, inv_freq, layout=ROPE_HALF, scale=1
     positions: int32 [T] or [B, T], None for 0 .. T - 1; inv_freq: float64 [rotary_dim / 2] on the
     device (rope_frequencies); scale: of the turned part; inverse: the transposed rotation, which
     takes the gradients of q_out and k_out to those of q and k."""
-    if not isinstance(q, torch.Tensor) or q.dim() not in (3, 4):
+    shape = q.shape if isinstance(q, torch.Tensor) else ()
+    if len(shape) == 4:
+        B, _, T, D = shape
+    elif len(shape) == 3:
+        B, (_, T, D) = 1, shape
+    else:
         raise ValueError("q must be a [B, H, T, D] or [H, T, D] tensor")
-    shape, dev = q.shape, _device(q, "q")
-    *batch, _, T, D = shape
-    if not isinstance(q_out, torch.Tensor) or q.dtype not in _OUT or q_out.dtype not in _OUT:
+    dev = q.get_device()
+    t_in, t_out = q.dtype, getattr(q_out, "dtype", None)
+    codes = _OUT_CODES.get(t_in), _OUT_CODES.get(t_out)
+    if None in codes:
         raise TypeError("q and q_out must be tensors of dtype %s" % (_OUT,))
-    t_in, t_out = q.dtype, q_out.dtype
     rows, more = _rope_rows(q, q_out, "q", shape, t_in, t_out, dev), None
     if k is not None:
         other = k.shape if isinstance(k, torch.Tensor) else ()
-        if len(other) != len(shape) or other[-2:] != shape[-2:] or other[:-3] != shape[:-3]:
+        if len(other) != len(shape) or other[-2:] != (T, D) or (len(shape) == 4 and other[0] != B):
             raise ValueError("k must have the batch, tokens and head size of q")
         more = _rope_rows(k, k_out, "k", other, t_in, t_out, dev)
     elif k_out is not None:
         raise ValueError("k_out without k")
-    B = batch[0] if batch else 1
     turn = _rope_turn(positions, inv_freq, layout, scale, B, T, dev)
-    _launch(dev, stream, (_lib or load_library()).mala_rope, rows, more, turn, B, T, D,
-            OUT_BF16 if t_in is torch.bfloat16 else OUT_F32,
-            OUT_BF16 if t_out is torch.bfloat16 else OUT_F32, 1 if inverse else 0)
+    _launch(dev, stream, (_lib or load_library()).mala_rope, rows, more, turn, B, T, D, *codes,
+            1 if inverse else 0)
 
 
 def mala_paged_rope_write(q, q_out, k_new, v_new, positions, slots, cache, inv_freq, layout=ROPE_HALF,

@@ -134,6 +134,9 @@ def test_broadcast_input_and_no_tokens():
     for shape in ((0, 3, 5, 64), (2, 3, 0, 64)):
         e = torch.empty(shape, dtype=BF16, device="cuda")
         assert mala.rope(e, e, None, f)["k"].shape == shape
+        for pos in (shape[2:3], (shape[0], shape[2])):
+            pos = torch.zeros(pos, dtype=torch.int32, device="cuda")
+            assert mala.rope(e, None, pos, f)["q"].shape == shape
 
 
 def test_infinities_and_nan_stay_in_their_pairs():
