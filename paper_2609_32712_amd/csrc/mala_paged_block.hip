@@ -7,8 +7,9 @@
 // to nearest even as the new ones.  Scales are powers of two so that this second rounding is exact
 // but where a value leaves the normal range, and so that value x scale is a bf16.
 //
-// What bounds it: HBM (2 bytes read and 1 written per value); small calls the chain slots -> rows
-// -> stores.
+// What bounds it: HBM (2 bytes read and 1 written per value): 20000 tokens of 8 heads 20 us, 5.8 TB/s;
+// 16000 turned ones with 32 heads' queries 67 us, 5.4 TB/s; small calls the chain slots -> scale ->
+// stores (64 decodes 3.5 us, turned and with their queries 4.5).
 #include "mala_rope.h"
 
 namespace mala {
