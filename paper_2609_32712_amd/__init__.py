@@ -535,21 +535,26 @@ def mala_paged_update(lens, new_lens, block_table, free_ring, free_state, lens_o
 def _new_rows(k_new, v_new, slots, c):
     """The checks of the rows that a write takes; (T, token stride, head stride)."""
     Hkv, T, D = shape = _shape(k_new, "k_new", 3)
-    _shape(v_new, "v_new", 3)
+    if not isinstance(v_new, torch.Tensor) or v_new.dim() != 3:
+        _dims(v_new, "v_new", 3)
     if k_new.dtype is not torch.bfloat16 or v_new.dtype is not torch.bfloat16:
         raise TypeError("k_new and v_new must have dtype %s, got %s and %s"
                         % (torch.bfloat16, k_new.dtype, v_new.dtype))
     if Hkv != c.Hkv or D != c.D:
         raise ValueError("k_new must have shape %s, got %s" % ((c.Hkv, T, c.D), (Hkv, T, D)))
-    st = k_new.stride()
+    st = head_stride, token_stride, unit = k_new.stride()
     if v_new.shape != shape or (v_new.stride() != st and T):
         raise ValueError("v_new must have the shape and strides of k_new")
-    if st[2] != 1 and T:
+    if unit != 1 and T:
         raise ValueError("the rows of k_new must be contiguous")
-    if k_new.get_device() != c.device or v_new.get_device() != c.device:
+    device = c.device
+    if k_new.get_device() != device or v_new.get_device() != device:
         raise TypeError("k_new and v_new must be CUDA (HIP) tensors on the device of the cache")
-    _args(c.device, (slots, "slots", torch.int32, (T,)))
-    return T, st[1] if T > 1 else D, st[0] if Hkv > 1 else D
+    # (as _args: one quick look where everything is right)
+    if not (type(slots) is torch.Tensor and slots.dtype is torch.int32 and slots.shape == (T,)
+            and slots.get_device() == device and slots.is_contiguous()):
+        _args(device, (slots, "slots", torch.int32, (T,)))
+    return T, token_stride if T > 1 else D, head_stride if Hkv > 1 else D
 
 
 def mala_paged_write(k_new, v_new, slots, cache, stream=None):
