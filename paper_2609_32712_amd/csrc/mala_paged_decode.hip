@@ -155,6 +155,30 @@ struct SplitState {
   }
 };
 
+// Where a tile's pieces of 8 values lie in LDS: rows D + 16 apart, and within a row (SWAP: of 128 bytes
+// in the cache, where a lane has two neighbouring pieces to store) the even pieces in front of the odd
+// ones, these in pairs swapped.  K reads (a phase takes rows 0-3 and 12-15 of one piece with 4-11 of
+// the next), transposed V reads and stores (128 bytes at a time) then find no two lanes on one bank.
+// With rows D + 8 apart and the pieces in order LDS was busy 384 instead of 192 cycles per tile of
+// bytes; us per call before / now: 48 ragged caches of up to 8192 tokens 71.5 / 70.0, 16 of 8192 with 64
+// heads on 2 27.5 / 26.9.
+template <int D, bool SWAP>
+struct Layout {
+  static constexpr int LD = D == 128 ? D + 16 : D + 8;    // (D = 64: a wavefront per SIMD less, 52 / 60 us)
+  // element of piece n of a row
+  static __device__ __forceinline__ constexpr int at(int n) {
+    return 8 * (!SWAP ? n : n % 2 ? D / 16 + (n / 2 ^ 1) : n / 2);
+  }
+  // piece 4 kk + g: k_lane(g) + k_step(kk)
+  static __device__ __forceinline__ int k_lane(int g) { return at(g); }
+  static constexpr int k_step(int kk) { return SWAP ? 16 * kk : 32 * kk; }
+  // values 16 db + 4 j .. + 3: v_lane(j, db odd?) + v_step(db)
+  static __device__ __forceinline__ int v_lane(int j, int odd) {
+    return SWAP ? (j >> 1 ? D / 2 + (odd ? -8 : 8) : 0) + 4 * (j & 1) : 4 * j;
+  }
+  static constexpr int v_step(int db) { return SWAP ? 8 * db : 16 * db; }
+};
+
 template <int D, int FMT, int MODE>
 __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(PagedDecParams p) {
   constexpr int W = kPagedWaves;
@@ -162,7 +186,8 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
   constexpr bool E4M3 = FMT == kCacheE4M3, BLOCK = FMT == kCacheBlock, BYTES = E4M3 || BLOCK;
   constexpr int KS = D / 32;             // k-steps of 32 over head_dim
   constexpr int NDB = D / 16;            // 16-row blocks of O^T
-  constexpr int LD = D + 8;
+  using Lay = Layout<D, FMT != kCacheBf16 && D == 128>;
+  constexpr int LD = Lay::LD;
   constexpr int CPR = D / (BYTES ? 16 : 8);   // 16-byte chunks per row of the cache
   constexpr int RPI = 64 / CPR;          // rows per load instruction
   constexpr int IPG = kPageRows / RPI;   // load instructions per 16-row group
@@ -343,13 +368,15 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
           y[k / 2][2 * (k % 2) + 1] = __builtin_bit_cast(
               int, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(raw[k], f, true));
         }
-        store8(mine + r * LD + c * 16, __builtin_bit_cast(bf16x8, y[0]));
-        store8(mine + r * LD + c * 16 + 8, __builtin_bit_cast(bf16x8, y[1]));
+        store8(mine + r * LD + Lay::at(2 * c), __builtin_bit_cast(bf16x8, y[0]));
+        store8(mine + r * LD + Lay::at(2 * c + 1), __builtin_bit_cast(bf16x8, y[1]));
       } else {
         store8(mine + r * LD + c * 8, x[i]);
       }
     }
   };
+
+  const int k_lane = Lay::k_lane(g), v_even = Lay::v_lane(col & 3, 0), v_odd = Lay::v_lane(col & 3, 1);
 
   // Products of the K tile in LDS with this lane's head (before scale2): s[0..3] keys 4 g + r,
   // s[4..7] keys 16 + 4 g + r; keys that are not there -inf.  Returns the scaled maximum.
@@ -357,8 +384,8 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
     f32x4 s0 = {0.f, 0.f, 0.f, 0.f}, s1 = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
     for (int kk = 0; kk < KS; ++kk) {
-      s0 = mfma16(load8(mine + col * LD + 32 * kk + 8 * g), qreg[kk], s0);
-      s1 = mfma16(load8(mine + (16 + col) * LD + 32 * kk + 8 * g), qreg[kk], s1);
+      s0 = mfma16(load8(mine + col * LD + k_lane + Lay::k_step(kk)), qreg[kk], s0);
+      s1 = mfma16(load8(mine + (16 + col) * LD + k_lane + Lay::k_step(kk)), qreg[kk], s1);
     }
 #pragma unroll
     for (int r = 0; r < 4; ++r) {
@@ -398,7 +425,7 @@ __global__ __launch_bounds__(kPagedWaves * 64, 2) void mala_paged_decode_kernel(
     const bf16x8 ph = take_bf16x8(x), pl = take_bf16x8(x), pr = take_bf16x8(x);
 #pragma unroll
     for (int db = 0; db < NDB; ++db) {
-      const bf16* vrow = mine + (4 * g + (col >> 2)) * LD + 16 * db + 4 * (col & 3);
+      const bf16* vrow = mine + (4 * g + (col >> 2)) * LD + (db % 2 ? v_odd : v_even) + Lay::v_step(db);
       const bf16x8 a = cat(lds_read_tr(vrow), lds_read_tr(vrow + 16 * LD));
       acc[db] = mfma16(a, ph, acc[db]);
       acc[db] = mfma16(a, pl, acc[db]);
