@@ -68,26 +68,32 @@ __device__ __forceinline__ Share share_of(const PagedDecParams& p, int at) {
     const int nb = lane < here ? paged_blocks_of(t, per_block) : 0;
     const int end = wave_scan(nb), all = __builtin_amdgcn_readlane(end, 63);
     if (at < before + all) {
-      // even runs within a sequence; its blocks take the places [from, from + nb) of these 64
-      // sequences' blocks, the longest runs first
-      const int tpw = paged_run_tiles(t, max(nb, 1), unit, W);
-      int from = end - nb;
+      // even runs within a sequence.  Its blocks but the last, which are full, take the places [from, from +
+      // nb - 1) of these 64 sequences' blocks, its last one, of what is left of it, the place `last`:
+      // the blocks of the most tiles first
+      const int tpw = paged_run_tiles(t, max(nb, 1), unit, W), full = W * tpw;
+      int from = end - nb, last = end - 1;
       if (p.sorted && __builtin_amdgcn_ballot_w64(lane < here && tpw > 4)) {
-        const int cls = paged_run_class(tpw, per_block, W);
+        const int cls = paged_run_class(full, per_block, 1);
+        const int cls_last = paged_run_class(t - (nb - 1) * full, per_block, 1);
         int base = 0;
 #pragma unroll
         for (int c = kPagedClasses - 1; c >= 0; --c) {
-          const int e = wave_scan(cls == c ? nb : 0);
-          if (cls == c) from = base + e - nb;
+          const int n = nb == 0 ? 0 : (cls == c ? nb - 1 : 0) + (cls_last == c ? 1 : 0);
+          const int e = wave_scan(n), at_c = base + e - n;
+          if (cls == c) from = at_c;
+          if (cls_last == c) last = base + e - 1;
           base += __builtin_amdgcn_readlane(e, 63);
         }
       }
       const int place = at - before;
-      const int i = __builtin_ctzll(__builtin_amdgcn_ballot_w64(from <= place && place < from + nb));
+      const bool mine = lane < here && ((from <= place && place < from + nb - 1) || place == last);
+      const int i = __builtin_ctzll(__builtin_amdgcn_ballot_w64(mine));
       s.b = b0 + i;
       s.blocks = __builtin_amdgcn_readlane(nb, i);
       s.first = before + __builtin_amdgcn_readlane(end, i) - s.blocks;
-      s.blk = place - __builtin_amdgcn_readlane(from, i);
+      s.blk = place == __builtin_amdgcn_readlane(last, i) ? s.blocks - 1
+                                                           : place - __builtin_amdgcn_readlane(from, i);
       s.tpw = __builtin_amdgcn_readlane(tpw, i);
       s.n = min(max(p.lens[s.b], 0), p.max_len);
       return s;
