@@ -83,6 +83,7 @@ struct BlockWriter {
   unsigned within = 0, page = 0;
   int t[NI];
   bool anew = false;
+  int pos_here = 0, pos_after = 0;         // positions of the 64 tokens from t0 on, and of the next
 
   __device__ __forceinline__ BlockWriter(const PagedWriteParams& p, const Turn& turn)
       : p(p), turn(turn), lane(threadIdx.x & 63), w(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)),
@@ -95,20 +96,23 @@ struct BlockWriter {
     const int64_t t0 = (int64_t)chunk * p.chunk;
     base = t0 - 1;
     const int slots = (int)(p.c.num_pages * (unsigned)p.c.page_size);
-    const auto slot_of = [&](int64_t n) {
-      if (n < 0 || n >= p.T) return -1;
-      const int s = p.slots[n];
-      return s < slots && s >= 0 ? s : -1;
-    };
-    // A chunk of one token, most likely alone: its rows and angles are fetched beside the slots.
+    const auto load_slot = [&](int64_t n) { return n >= 0 && n < p.T ? p.slots[n] : -1; };
+    const auto in_pool = [&](int s) { return s < slots && s >= 0 ? s : -1; };
+    // The slots of the tokens around, and their positions.  A chunk of one token, most likely alone: its
+    // rows and angles are fetched beside the slots.
+    int before = load_slot(t0 - 64 + lane), here = load_slot(t0 + lane), after = -1;
+    if constexpr (ROPE) pos_here = pos_of(t0 + lane);
     i32x4 early[2];
-    if (p.chunk == 1) load_one(1, min(u_lo + w * RPI + lane / LPR, u_hi - 1), early);
-    if constexpr (ROPE)
-      if (p.chunk == 1) {
-        table(turns.at[0], 1, 1);
-      }
-    const int before = slot_of(t0 - 64 + lane), here = slot_of(t0 + lane);
-    const int after = p.chunk > 1 ? slot_of(t0 + 64 + lane) : -1;
+    if (p.chunk == 1) {
+      load_one(1, min(u_lo + w * RPI + lane / LPR, u_hi - 1), early);
+      if constexpr (ROPE) table(turns.at[0], 1, 1);
+    } else {
+      after = load_slot(t0 + 64 + lane);
+      if constexpr (ROPE) pos_after = pos_of(t0 + 64 + lane);
+    }
+    before = in_pool(before);
+    here = in_pool(here);
+    after = in_pool(after);
     uint64_t todo = __builtin_amdgcn_ballot_w64(here >= 0 && lane < p.chunk), ones = 0;
     int tables = 0;
     while (todo) {                        // (the same for the workgroup's wavefronts)
@@ -193,16 +197,21 @@ struct BlockWriter {
   // (rows that stay as they are: 16 elements of a row side by side)
   __device__ __forceinline__ int piece(int u, int n) const { return ROPE && !kind_of(u) ? pc.at[n] : 2 * lr + n; }
 
-  // cos and sin of the first `rows` tokens of lanes 0, 1, .., by the workgroup
+  __device__ __forceinline__ int pos_of(int64_t n) const {
+    return n >= p.T ? 0 : turn.pos ? turn.pos[n] : (int)n;
+  }
+  // cos and sin of the first `rows` tokens of lanes 0, 1, .., by the workgroup.  (Lanes are asked by all
+  // lanes: one that is switched off would answer 0.)
   __device__ __forceinline__ void table(f32x2* to, int token, int rows) const {
-    const int pairs = turn.R / 2;
-    for (int i = threadIdx.x; i < rows * pairs; i += 256) {
-      const int row = i / pairs, pair = i - row * pairs;
-      const int n = __builtin_amdgcn_ds_bpermute(4 * row, token);
-      if (!n) continue;
+    const int pairs = turn.R / 2, own = 4 * ((token - 1) & 63);
+    const int near = __builtin_amdgcn_ds_bpermute(own, pos_here), far = __builtin_amdgcn_ds_bpermute(own, pos_after);
+    const int own_pos = token > 64 ? far : near;
+    for (int i0 = 0; i0 < rows * pairs; i0 += 256) {
+      const int i = i0 + (int)threadIdx.x, row = min(i / pairs, rows - 1), pair = i - row * pairs;
+      const int n = __builtin_amdgcn_ds_bpermute(4 * row, token), pos = __builtin_amdgcn_ds_bpermute(4 * row, own_pos);
+      if (!n || i >= rows * pairs) continue;
       float c, s;
-      turn_of(turn.pos ? turn.pos[base + n] : (int)(base + n), turn.inv_freq[pair], turn.scale, turn.sin_scale, c,
-              s);
+      turn_of(pos, turn.inv_freq[pair], turn.scale, turn.sin_scale, c, s);
       to[row * ROW + pair] = f32x2{c, s};
     }
   }

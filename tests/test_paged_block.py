@@ -256,6 +256,24 @@ def test_rope_write_is_rope_and_write(Hkv, D, P, layout, order, kind):
                 assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
 
 
+@pytest.mark.parametrize("R", [16, 48, 64])
+@pytest.mark.parametrize("T", [300, 1300, 2400, 3900, 4700])
+def test_rope_write_of_many_decodes(T, R):
+    # tokens alone in their blocks, one to sixteen of them to a workgroup: angles of as many rows
+    rng = np.random.default_rng(T)
+    f, _ = mala.rope_frequencies(R, device="cuda")
+    pos = torch.from_numpy(rng.integers(0, 100000, T)).int().cuda()
+    slots = rng.permutation(T) * 16 + rng.integers(0, 16, T)
+    slots[rng.random(T) < 0.05] = -1
+    kn, vn = new_rows(torch.from_numpy(rng.standard_normal((2, 2, T, 64))).to(BF16), "tokens")
+    caches = [bu.block_cache(mala, T, 2, 16, 64, fill=0x75) for _ in range(2)]
+    sep = mala.rope(kn, None, pos, f)["q"]
+    mala.mala_paged_write(sep, vn.contiguous(), cuda(slots), caches[0][0])
+    mala.mala_paged_rope_write(None, None, kn, vn, pos, cuda(slots), caches[1][0], f)
+    for a, b in zip(caches[0][1:], caches[1][1:]):
+        assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+
+
 # ------------------------------------------------------------------ reads
 def test_read_of_every_byte_and_scale_is_exact():
     # 256 bytes x 256 scales: e4m3 x 2^e as a bf16, no rounding (bytes outside the range: its ends)
