@@ -9,7 +9,7 @@
 //
 // What bounds it: HBM (2 bytes read and 1 written per value): 20000 tokens of 8 heads 20 us, 5.8 TB/s;
 // 16000 turned ones with 32 heads' queries 67 us, 5.4 TB/s; small calls the chain slots -> scale ->
-// stores (64 decodes 3.5 us, turned and with their queries 4.5).
+// stores (64 decodes 3.5 us, turned and with their queries 4.3).
 #include "mala_rope.h"
 
 namespace mala {

@@ -19,7 +19,7 @@
 //
 // Blocks of 16 rows with a scale 2^e (kCacheBlock) are these 16-row groups; the conversion to bf16
 // applies the scale, exactly.  They take as long as e4m3 with a scale per head (16 caches of 100000
-// tokens 499 us, 6.6 TB/s; 48 ragged ones of up to 8192 75).
+// tokens 498 us, 6.6 TB/s; 48 ragged ones of up to 8192 75).
 #include "mala_device.h"
 #include "mala_kernels.h"
 #include "mala_paged.h"
