@@ -331,9 +331,9 @@ typedef struct {
 
 /* Rows to turn: D contiguous elements at element b x batch_stride + h x head_stride + t x
  * token_stride of x, and of out for the result; pointers 16-byte aligned, strides multiples of 16
- * bytes (those of out at least D; of an axis of one entry, any).  out is x with the same strides
- * (in place), or memory between whose first and last byte none of x lies.  Outputs share no row with
- * each other or with the other tensor's x. */
+ * bytes (of an axis of one entry, any); rows of out share no memory with each other.  out is x with the
+ * same strides (in place), or memory between whose first and last byte none of x lies.  Outputs share
+ * no row with each other or with the other tensor's x. */
 typedef struct {
   const void* x;
   void* out;

@@ -13,6 +13,7 @@
 #include "mala_kernels.h"
 #include "mala_paged.h"
 #include "mala_rope.h"
+#include "mala_rows.h"
 
 namespace {
 
@@ -550,12 +551,6 @@ int check_write(const void* k_new, const void* v_new, int64_t new_token_stride, 
 }
 
 // ---------------------------------------------------------------- rotary positions
-int64_t extent(const int64_t stride[3], const int64_t n[3], int64_t row) {
-  int64_t bytes = row;
-  for (int i = 0; i < 3; ++i) bytes += stride[i] * (n[i] - 1);
-  return bytes;
-}
-
 // One tensor's rows, B x heads x T of them (all above 0).
 int check_rows(const mala_rope_rows_t* r, const char* name, int B, int T, int D, int in_size, int out_size,
                mala::RopeRows* out) {
@@ -576,16 +571,18 @@ int check_rows(const mala_rope_rows_t* r, const char* name, int B, int T, int D,
     constexpr int64_t kMost = (int64_t)1 << 60;
     if (in[i] > kMost / in_size / n[i] || to[i] > kMost / out_size / n[i])
       return fail(MALA_ERR_UNSUPPORTED, "stride of %s too large", name);
-    // rows of an output that share memory would be written by several threads
-    if (n[i] > 1 && to[i] < D)
-      return fail(MALA_ERR_INVALID_ARG, "rows of the output of %s overlap", name);
     in_b[i] = in[i] * in_size;
     to_b[i] = to[i] * out_size;
   }
+  // rows of an output that share memory would be written by several threads
+  const mala::Rows x = {(uintptr_t)r->x, (int64_t)D * in_size, {in_b[0], in_b[1], in_b[2]}, {n[0], n[1], n[2]}};
+  const mala::Rows y = {(uintptr_t)r->out, (int64_t)D * out_size, {to_b[0], to_b[1], to_b[2]}, {n[0], n[1], n[2]}};
+  const mala::Shared shared = mala::rows_overlap(y);
+  if (shared == mala::kShare) return fail(MALA_ERR_INVALID_ARG, "rows of the output of %s overlap", name);
+  if (shared) return fail(MALA_ERR_UNSUPPORTED, "the rows of the output of %s cannot be told apart", name);
   bool same = r->x == r->out && in_size == out_size;
   for (int i = 0; i < 3; ++i) same = same && in[i] == to[i];
-  const uintptr_t a = (uintptr_t)r->x, b = (uintptr_t)r->out;
-  if (!same && a < b + extent(to_b, n, (int64_t)D * out_size) && b < a + extent(in_b, n, (int64_t)D * in_size))
+  if (!same && x.base < y.base + y.extent() && y.base < x.base + x.extent())
     return fail(MALA_ERR_INVALID_ARG, "the output of %s meets its input without being it", name);
   *out = {(const char*)r->x, (char*)r->out, in_b[0], in_b[1], in_b[2], to_b[0], to_b[1], to_b[2], r->heads};
   return MALA_OK;

@@ -1,0 +1,93 @@
+"""Rows that share memory (CPU): the host's answer (csrc/mala_rows.h, compiled here) against a look at
+every pair of rows, and the calls that have to refuse such outputs."""
+import itertools
+import random
+import shutil
+import subprocess
+
+import pytest
+
+import paper_2609_32712_amd as mala
+from paper_2609_32712_amd import build as libbuild
+from test_rope_block_abi import BAD, _refused, _rope, _rows
+
+CXX = shutil.which("g++")
+needs_cxx = pytest.mark.skipif(CXX is None, reason="needs g++")
+
+PROGRAM = r"""
+#include <cstdio>
+#include "mala_rows.h"
+using namespace mala;
+static bool get(Rows& r) {
+  long b, w, s[3], n[3];
+  if (std::scanf("%ld %ld %ld %ld %ld %ld %ld %ld", &b, &w, s, s + 1, s + 2, n, n + 1, n + 2) != 8) return false;
+  r = {(uintptr_t)b, w, {s[0], s[1], s[2]}, {n[0], n[1], n[2]}};
+  return true;
+}
+int main() {
+  Rows r;
+  while (get(r)) std::printf("%d\n", (int)rows_overlap(r));
+}
+"""
+
+
+def _ask(tmp_path, program, lines):
+    src, exe = tmp_path / "rows.cc", tmp_path / "rows"
+    src.write_text(program)
+    subprocess.run([CXX, "-std=c++17", "-O1", "-Wall", "-Werror", "-fsanitize=undefined",
+                    "-fno-sanitize-recover", "-I" + libbuild.CSRC, str(src), "-o", str(exe)], check=True)
+    out = subprocess.run([str(exe)], input="\n".join(" ".join(map(str, x)) for x in lines), text=True,
+                         capture_output=True, check=True).stdout.split()
+    assert len(out) == len(lines)
+    return [int(x) for x in out]
+
+
+def _places(r):
+    base, _, s, n = r[0], r[1], r[2:5], r[5:8]
+    return [base + sum(i * a for i, a in zip(at, s)) for at in itertools.product(*map(range, n))]
+
+
+def _random(rng):
+    w = 16 * rng.choice([1, 2, 8])
+    nested = rng.random() < 0.4
+    n = [rng.randint(1, 6) for _ in range(3)]
+    s = [16 * rng.randint(0, 30) for _ in range(3)]
+    if nested:
+        step = w
+        for i in rng.sample(range(3), 3):
+            s[i] = step + 16 * rng.choice([0, 0, 1, 5]) * rng.randint(0, 1)
+            step = s[i] * n[i]
+    return [16 * rng.randint(0, 60), w] + s + n
+
+
+@needs_cxx
+def test_own_rows(tmp_path):
+    rng = random.Random(1)
+    rows = [_random(rng) for _ in range(4000)]
+    want = []
+    for r in rows:
+        at = sorted(_places(r))
+        want.append(int(any(b - a < r[1] for a, b in zip(at, at[1:]))))
+    assert 800 < sum(want) < 3200
+    assert _ask(tmp_path, PROGRAM, rows) == want
+    # large ones: rows side by side in every order, 16 bytes short of it, and strides that do not nest
+    cases = [([0, 256, 256 * 40, 256, 256 * 40 * 70000, 70000, 40, 100], 0),
+             ([0, 256, 256 * 70000, 256, 256 * 40 * 70000, 40, 70000, 100], 0),
+             ([0, 256, 256 * 40 - 16, 256, 256 * 40 * 70000, 70000, 40, 100], 1),
+             ([0, 256, 256, 256, 1 << 40, 2, 2, 1], 1), ([0, 256, 256, 256, 1 << 40, 1, 2, 1], 0),
+             ([0, 256, 3 * 256, 2 * 256, 1 << 40, 2, 2, 2], 0), ([0, 256, 3 * 256, 2 * 256, 1 << 40, 3, 4, 2], 1),
+             ([0, 256, 0, 256, 1024, 1, 4, 1], 0), ([0, 256, 0, 256, 1024, 2, 4, 1], 1),
+             ([0, 256, 1 << 59, 1 << 58, 1 << 50, 2, 2, 2], 0),
+             # (strides no memory has, and more steps than are taken: not told, and refused)
+             ([0, 256, 1 << 60, 3 << 59, 1 << 58, 2, 2, 4], 2),
+             ([0, 32, 16 * 100003, 16 * 99991, 1 << 45, 90000, 90000, 1], 2)]
+    assert _ask(tmp_path, PROGRAM, [c for c, _ in cases]) == [x for _, x in cases]
+
+
+@pytest.mark.parametrize("kw", [dict(oh=128, ot=128), dict(ob=1024, ot=1024), dict(oh=128, ot=256, ob=2048),
+                                dict(oh=128, ot=504, ob=4096), dict(ob=128, oh=1024, ot=192)])
+def test_rows_of_an_output_that_overlap_are_refused(kw):
+    # (two, four tokens of four heads of 128 elements)
+    _refused(_rope(q=_rows(**kw)), BAD)
+    _refused(_rope(k=_rows(**kw)), BAD)
+    assert b"rows of the output of k overlap" in mala.load_library().mala_last_error()
