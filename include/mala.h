@@ -333,7 +333,7 @@ typedef struct {
  * token_stride of x, and of out for the result; pointers 16-byte aligned, strides multiples of 16
  * bytes (of an axis of one entry, any); rows of out share no memory with each other.  out is x with the
  * same strides (in place), or memory between whose first and last byte none of x lies.  Outputs share
- * no row with each other or with the other tensor's x. */
+ * no memory with each other or with the other tensor's x, between whose rows they may lie. */
 typedef struct {
   const void* x;
   void* out;

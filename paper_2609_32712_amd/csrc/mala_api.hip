@@ -551,9 +551,21 @@ int check_write(const void* k_new, const void* v_new, int64_t new_token_stride, 
 }
 
 // ---------------------------------------------------------------- rotary positions
+// Rows that a launch reads or writes in any order beside those that it writes.
+int check_apart(const mala::Rows& written, const char* name, const mala::Rows& other, const char* what) {
+  const mala::Shared shared = mala::rows_meet(written, other);
+  if (shared == mala::kShare)
+    return fail(MALA_ERR_INVALID_ARG, "the output of %s shares memory with %s", name, what);
+  if (shared) return fail(MALA_ERR_UNSUPPORTED, "the output of %s and %s cannot be told apart", name, what);
+  return MALA_OK;
+}
+
 // One tensor's rows, B x heads x T of them (all above 0).
+struct TurnedRows {
+  mala::Rows x, out;
+};
 int check_rows(const mala_rope_rows_t* r, const char* name, int B, int T, int D, int in_size, int out_size,
-               mala::RopeRows* out) {
+               mala::RopeRows* out, TurnedRows* rows) {
   if (!r->x || !r->out) return fail(MALA_ERR_INVALID_ARG, "null x or out of %s", name);
   if (r->heads <= 0) return fail(MALA_ERR_INVALID_ARG, "non-positive heads of %s", name);
   if (r->heads > 65535) return fail(MALA_ERR_UNSUPPORTED, "%d heads of %s", r->heads, name);
@@ -584,6 +596,7 @@ int check_rows(const mala_rope_rows_t* r, const char* name, int B, int T, int D,
   for (int i = 0; i < 3; ++i) same = same && in[i] == to[i];
   if (!same && x.base < y.base + y.extent() && y.base < x.base + x.extent())
     return fail(MALA_ERR_INVALID_ARG, "the output of %s meets its input without being it", name);
+  *rows = {x, y};
   *out = {(const char*)r->x, (char*)r->out, in_b[0], in_b[1], in_b[2], to_b[0], to_b[1], to_b[2], r->heads};
   return MALA_OK;
 }
@@ -683,8 +696,15 @@ int mala_rope(const mala_rope_rows_t* q, const mala_rope_rows_t* k, const mala_r
   if (!st) st = check_dtype(out_dtype, "out_dtype");
   if (st || !B || !T) return st;
   const int in_size = in_dtype == MALA_OUT_BF16 ? 2 : 4, out_size = out_dtype == MALA_OUT_BF16 ? 2 : 4;
-  if ((st = check_rows(q, "q", B, T, D, in_size, out_size, &p.r[0]))) return st;
-  if (k && (st = check_rows(k, "k", B, T, D, in_size, out_size, &p.r[1]))) return st;
+  TurnedRows qr, kr;
+  if ((st = check_rows(q, "q", B, T, D, in_size, out_size, &p.r[0], &qr))) return st;
+  if (k) {
+    if ((st = check_rows(k, "k", B, T, D, in_size, out_size, &p.r[1], &kr))) return st;
+    st = check_apart(qr.out, "q", kr.out, "the output of k");
+    if (!st) st = check_apart(qr.out, "q", kr.x, "k");
+    if (!st) st = check_apart(kr.out, "k", qr.x, "q");
+    if (st) return st;
+  }
   p.B = B;
   p.T = T;
   const hipError_t e = mala::launch_rope(p, D, in_size == 4, out_size == 4, (hipStream_t)stream);
@@ -700,7 +720,8 @@ int mala_paged_rope_write(const mala_rope_rows_t* q, const void* k_new, const vo
   int st = check_write(k_new, v_new, new_token_stride, new_head_stride, slots, cache, num_tokens, &p.w);
   if (!st) st = check_turn(rope, 1, num_tokens, cache->D, 0, &p.q.turn);
   if (st || !num_tokens) return st;
-  if (q && (st = check_rows(q, "q", 1, num_tokens, cache->D, 2, 2, &p.q.r[0]))) return st;
+  TurnedRows qr;
+  if (q && (st = check_rows(q, "q", 1, num_tokens, cache->D, 2, 2, &p.q.r[0], &qr))) return st;
   p.q.B = 1;
   p.q.T = num_tokens;
   // a workgroup per rope_tokens(D) tokens, and per head at most, and those of a block-scaled write; in

@@ -91,4 +91,15 @@ inline Shared rows_overlap(const Rows& r) {
   return m.find(0, -r.width, r.width, true);
 }
 
+// Whether a row of one and a row of the other share a byte.
+inline Shared rows_meet(const Rows& x, const Rows& y) {
+  if (x.base >= y.base + y.extent() || y.base >= x.base + x.extent()) return kApart;
+  Meeting m;
+  for (int a = 0; a < 3; ++a) {
+    m.axis(x.stride[a], 0, x.n[a] - 1);
+    m.axis(y.stride[a], 1 - y.n[a], 0);
+  }
+  return m.find((int64_t)(x.base - y.base), -x.width, y.width, false);
+}
+
 }  // namespace mala

@@ -6,6 +6,7 @@ import shutil
 import subprocess
 
 import pytest
+import torch
 
 import paper_2609_32712_amd as mala
 from paper_2609_32712_amd import build as libbuild
@@ -24,19 +25,22 @@ static bool get(Rows& r) {
   r = {(uintptr_t)b, w, {s[0], s[1], s[2]}, {n[0], n[1], n[2]}};
   return true;
 }
-int main() {
-  Rows r;
-  while (get(r)) std::printf("%d\n", (int)rows_overlap(r));
+int main(int argc, char**) {
+  Rows r, s;
+  if (argc > 1)
+    while (get(r) && get(s)) std::printf("%d\n", (int)rows_meet(r, s));
+  else
+    while (get(r)) std::printf("%d\n", (int)rows_overlap(r));
 }
 """
 
 
-def _ask(tmp_path, program, lines):
+def _ask(tmp_path, lines, *args):
     src, exe = tmp_path / "rows.cc", tmp_path / "rows"
-    src.write_text(program)
+    src.write_text(PROGRAM)
     subprocess.run([CXX, "-std=c++17", "-O1", "-Wall", "-Werror", "-fsanitize=undefined",
                     "-fno-sanitize-recover", "-I" + libbuild.CSRC, str(src), "-o", str(exe)], check=True)
-    out = subprocess.run([str(exe)], input="\n".join(" ".join(map(str, x)) for x in lines), text=True,
+    out = subprocess.run([str(exe), *args], input="\n".join(" ".join(map(str, x)) for x in lines), text=True,
                          capture_output=True, check=True).stdout.split()
     assert len(out) == len(lines)
     return [int(x) for x in out]
@@ -69,7 +73,7 @@ def test_own_rows(tmp_path):
         at = sorted(_places(r))
         want.append(int(any(b - a < r[1] for a, b in zip(at, at[1:]))))
     assert 800 < sum(want) < 3200
-    assert _ask(tmp_path, PROGRAM, rows) == want
+    assert _ask(tmp_path, rows) == want
     # large ones: rows side by side in every order, 16 bytes short of it, and strides that do not nest
     cases = [([0, 256, 256 * 40, 256, 256 * 40 * 70000, 70000, 40, 100], 0),
              ([0, 256, 256 * 70000, 256, 256 * 40 * 70000, 40, 70000, 100], 0),
@@ -81,7 +85,41 @@ def test_own_rows(tmp_path):
              # (strides no memory has, and more steps than are taken: not told, and refused)
              ([0, 256, 1 << 60, 3 << 59, 1 << 58, 2, 2, 4], 2),
              ([0, 32, 16 * 100003, 16 * 99991, 1 << 45, 90000, 90000, 1], 2)]
-    assert _ask(tmp_path, PROGRAM, [c for c, _ in cases]) == [x for _, x in cases]
+    assert _ask(tmp_path, [c for c, _ in cases]) == [x for _, x in cases]
+
+
+@needs_cxx
+def test_rows_of_two_tensors(tmp_path):
+    rng = random.Random(2)
+    pairs, want = [], []
+    for _ in range(4000):
+        x, y = _random(rng), _random(rng)
+        if rng.random() < 0.3:           # slices of one tensor: the same strides
+            y[2:5] = x[2:5]
+        pairs.append(x + y)
+        want.append(int(any(-x[1] < a - b < y[1] for a, b in itertools.product(_places(x), _places(y)))))
+    assert 800 < sum(want) < 3600
+    assert _ask(tmp_path, pairs, "two") == want
+    # queries, keys and values of one projection of 32 + 8 + 8 heads, and 16 bytes too far
+    row = 48 * 256
+    q = [1 << 20, 256, 0, 256, row, 1, 32, 1 << 20]
+    k = [(1 << 20) + 32 * 256, 256, 0, 256, row, 1, 8, 1 << 20]
+    far = [k[0] - 16] + k[1:]
+    batches = [q[:2] + [row << 10] + q[3:5] + [9, 32, 1 << 10], k[:2] + [row << 10] + k[3:5] + [9, 8, 1 << 10]]
+    assert _ask(tmp_path, [q + k, k + q, q + far, far + q, batches[0] + batches[1]], "two") == [0, 0, 1, 1, 0]
+
+
+def test_outputs_that_share_rows_are_refused():
+    # (rows of 256 bytes, 2 x 4 x 4 of them, 8 KB to a batch; in is 1 << 20, out 1 << 30)
+    at = 1 << 21
+    for q, k in ((dict(), dict(x=at)),                                     # one output for both
+                 (dict(), dict(x=at, out=(1 << 30) + 240)),
+                 (dict(ot=2048, ob=8192), dict(x=at, out=(1 << 30) + 768, ot=2048, ob=8192, oh=256)),
+                 (dict(), dict(x=1 << 30, out=at)),                        # keys read where queries are written
+                 (dict(x=at), dict(x=1 << 22, out=at)),                    # and the other way round
+                 (dict(out=1 << 20), dict(x=1 << 20, out=at))):            # queries turned in place are the keys
+        _refused(_rope(q=_rows(**q), k=_rows(**k)), BAD)
+        assert b"shares memory with" in mala.load_library().mala_last_error()
 
 
 @pytest.mark.parametrize("kw", [dict(oh=128, ot=128), dict(ob=1024, ot=1024), dict(oh=128, ot=256, ob=2048),
@@ -91,3 +129,21 @@ def test_rows_of_an_output_that_overlap_are_refused(kw):
     _refused(_rope(q=_rows(**kw)), BAD)
     _refused(_rope(k=_rows(**kw)), BAD)
     assert b"rows of the output of k overlap" in mala.load_library().mala_last_error()
+
+
+@pytest.mark.gpu
+def test_outputs_side_by_side_are_taken():
+    # queries and keys into slices of one tensor, of heads in turns, and of batches inside tokens
+    f, _ = mala.rope_frequencies(128, device="cuda")
+    q, k = (torch.randn((3, h, 50, 128), device="cuda").bfloat16() for h in (4, 2))
+    want = mala.rope(q, k, None, f)
+    one = torch.zeros((50, 3, 9, 128), dtype=torch.bfloat16, device="cuda")
+    heads = one.permute(1, 2, 0, 3)
+    for qo, ko in ((heads[:, :4], heads[:, 4:6]), (heads[:, :8:2], heads[:, 1:4:2]), (heads[:, 5:], heads[:, 1:3])):
+        one.zero_()
+        mala.mala_rope(q, k, qo, ko, None, f)
+        assert torch.equal(qo, want["q"]) and torch.equal(ko, want["k"])
+        assert int((one != 0).any(-1).sum()) == 50 * 3 * 6
+    for qo, ko in ((heads[:, :4], heads[:, 3:5]), (heads[:, :4], heads[:, 0:4:2])):
+        with pytest.raises(mala.MalaError):
+            mala.mala_rope(q, k, qo, ko, None, f)
