@@ -467,8 +467,8 @@ int mala_paged_write(const void* k_new, const void* v_new, int64_t new_token_str
  * The keys and values of a step into the cache and its queries rotated, in one launch: the keys turn
  * as mala_rope turns them (the same bits, a bf16 each), and go to their slots with the values as by
  * mala_paged_write; the queries' rows (bf16, of num_tokens tokens; q may be NULL) turn from q->x to
- * q->out (batch strides are not used).  rope: one position per token.  What mala_rope,
- * mala_paged_write and the cache's type ask for holds here.
+ * q->out (batch strides are not used), which shares no memory with k_new or v_new.  rope: one position
+ * per token.  What mala_rope, mala_paged_write and the cache's type ask for holds here.
  */
 int mala_paged_rope_write(const mala_rope_rows_t* q, const void* k_new, const void* v_new,
                           int64_t new_token_stride, int64_t new_head_stride, const int32_t* slots,

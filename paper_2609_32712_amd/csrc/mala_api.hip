@@ -721,7 +721,15 @@ int mala_paged_rope_write(const mala_rope_rows_t* q, const void* k_new, const vo
   if (!st) st = check_turn(rope, 1, num_tokens, cache->D, 0, &p.q.turn);
   if (st || !num_tokens) return st;
   TurnedRows qr;
-  if (q && (st = check_rows(q, "q", 1, num_tokens, cache->D, 2, 2, &p.q.r[0], &qr))) return st;
+  if (q) {
+    if ((st = check_rows(q, "q", 1, num_tokens, cache->D, 2, 2, &p.q.r[0], &qr))) return st;
+    const int64_t n[2] = {cache->Hkv, num_tokens};
+    mala::Rows rows = {(uintptr_t)k_new, (int64_t)cache->D * 2, {0, n[0] > 1 ? p.w.head_stride : 0,
+                       n[1] > 1 ? p.w.token_stride : 0}, {1, n[0], n[1]}};
+    if ((st = check_apart(qr.out, "q", rows, "k_new"))) return st;
+    rows.base = (uintptr_t)v_new;
+    if ((st = check_apart(qr.out, "q", rows, "v_new"))) return st;
+  }
   p.q.B = 1;
   p.q.T = num_tokens;
   // a workgroup per rope_tokens(D) tokens, and per head at most, and those of a block-scaled write; in

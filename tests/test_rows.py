@@ -1,5 +1,6 @@
 """Rows that share memory (CPU): the host's answer (csrc/mala_rows.h, compiled here) against a look at
 every pair of rows, and the calls that have to refuse such outputs."""
+import ctypes
 import itertools
 import random
 import shutil
@@ -10,7 +11,7 @@ import torch
 
 import paper_2609_32712_amd as mala
 from paper_2609_32712_amd import build as libbuild
-from test_rope_block_abi import BAD, _refused, _rope, _rows
+from test_rope_block_abi import BAD, _block_cache, _refused, _rope, _rows, _turn
 
 CXX = shutil.which("g++")
 needs_cxx = pytest.mark.skipif(CXX is None, reason="needs g++")
@@ -129,6 +130,20 @@ def test_rows_of_an_output_that_overlap_are_refused(kw):
     _refused(_rope(q=_rows(**kw)), BAD)
     _refused(_rope(k=_rows(**kw)), BAD)
     assert b"rows of the output of k overlap" in mala.load_library().mala_last_error()
+
+
+def test_queries_into_new_rows_are_refused():
+    # (queries of 4 heads, 8 tokens of 1024 elements; new rows of 4 heads 1024 elements apart too)
+    for dtype in (mala.CACHE_BF16, mala.CACHE_E4M3, mala.CACHE_E4M3_BLOCK):
+        cache = ctypes.byref(_block_cache(dtype=dtype, page_stride=8 * 32 * 128, v_block_scale=1 << 40,
+                                          k_block_scale=1 << 41))
+        lib = mala.load_library()
+        for k, v, x, out in ((1 << 30, 1 << 32, 1 << 20, 1 << 30), (1 << 32, 1 << 30, 1 << 20, 1 << 30),
+                             (1 << 32, (1 << 30) + 7 * 2048 + 768, 1 << 20, 1 << 30),
+                             (1 << 30, 1 << 32, (1 << 30) - 256, (1 << 30) - 256)):
+            _refused(lib.mala_paged_rope_write(_rows(x=x, out=out), k, v, 1024, 128, 16, _turn(), cache, 8, None),
+                     BAD)
+            assert b"the output of q shares memory with" in lib.mala_last_error()
 
 
 @pytest.mark.gpu
