@@ -383,9 +383,9 @@ enum { MALA_SCALE_BLOCK = 16 };
  * k_scale, v_scale: fp32 [Hkv] device arrays of a MALA_CACHE_E4M3, NULL for scales of 1 (and for
  * the others).  k_block_scale, v_block_scale: [num_pages, Hkv, page_size / MALA_SCALE_BLOCK] device
  * arrays of a MALA_CACHE_E4M3_BLOCK, e + 127 a byte (OCP e8m0), e in [-117, 120] (bytes outside are
- * read as the nearer end); not read for the other types, and of no shared memory.  Value x scale is a
- * bf16 exactly.  Who copies a page copies its scales with it.  The struct itself is host memory, read
- * during the call. */
+ * read as the nearer end); not read for the other types, and of memory that neither the other nor
+ * a row of the pages has.  Value x scale is a bf16 exactly.  Who copies a page copies its scales with
+ * it.  The struct itself is host memory, read during the call. */
 typedef struct {
   void* k_pages;
   void* v_pages;

@@ -520,6 +520,24 @@ int check_cache(const mala_paged_cache_t* c, mala::PagedCache* out) {
   return MALA_OK;
 }
 
+// A write's block scales lie in no row of the pages: others would be rows and scales at once.
+int check_scales_apart(const mala::PagedCache& c, int D) {
+  if (c.fmt != mala::kCacheBlock) return MALA_OK;
+  const mala::Rows pages = {(uintptr_t)c.k, D, {c.page_stride, c.head_stride, c.token_stride},
+                            {c.num_pages, c.Hkv, c.page_size}};
+  for (const char* rows : {c.k, c.v})
+    for (const uint8_t* scales : {c.kb, c.vb}) {
+      const mala::Rows x = {(uintptr_t)scales, (int64_t)c.num_pages * c.Hkv * (c.page_size / mala::kPageRows),
+                            {0, 0, 0}, {1, 1, 1}};
+      mala::Rows y = pages;
+      y.base = (uintptr_t)rows;
+      const mala::Shared shared = mala::rows_meet(x, y);
+      if (shared == mala::kShare) return fail(MALA_ERR_INVALID_ARG, "block scales share memory with the pages");
+      if (shared) return fail(MALA_ERR_UNSUPPORTED, "block scales and pages cannot be told apart");
+    }
+  return MALA_OK;
+}
+
 // The arguments of a write, and its kernel form (nothing past the cache where there is no token).
 int check_write(const void* k_new, const void* v_new, int64_t new_token_stride, int64_t new_head_stride,
                 const int32_t* slots, const mala_paged_cache_t* cache, int num_tokens,
@@ -679,8 +697,9 @@ int mala_paged_write(const void* k_new, const void* v_new, int64_t new_token_str
                      const mala_paged_cache_t* cache, int num_tokens, void* stream) {
   g_err[0] = 0;
   mala::PagedWriteParams p;
-  const int st = check_write(k_new, v_new, new_token_stride, new_head_stride, slots, cache, num_tokens, &p);
+  int st = check_write(k_new, v_new, new_token_stride, new_head_stride, slots, cache, num_tokens, &p);
   if (st || !num_tokens) return st;
+  if ((st = check_scales_apart(p.c, cache->D))) return st;
   const hipError_t e = mala::launch_paged_write(p, cache->D, (hipStream_t)stream);
   return e == hipSuccess ? MALA_OK : hip_fail(e, "mala_paged_write: kernel launch");
 }
@@ -730,6 +749,7 @@ int mala_paged_rope_write(const mala_rope_rows_t* q, const void* k_new, const vo
     rows.base = (uintptr_t)v_new;
     if ((st = check_apart(qr.out, "q", rows, "v_new"))) return st;
   }
+  if ((st = check_scales_apart(p.w.c, cache->D))) return st;
   p.q.B = 1;
   p.q.T = num_tokens;
   // a workgroup per rope_tokens(D) tokens, and per head at most, and those of a block-scaled write; in

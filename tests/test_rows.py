@@ -146,6 +146,48 @@ def test_queries_into_new_rows_are_refused():
             assert b"the output of q shares memory with" in lib.mala_last_error()
 
 
+def test_block_scales_among_the_pages_are_refused():
+    # (10 pages of 4 heads of 32 rows of 128 bytes, 160 KB of K and of V; 80 bytes of scales each)
+    lib, k, v, far = mala.load_library(), 1 << 30, 1 << 32, 1 << 40
+    rows = dict(k_pages=k, v_pages=v, page_stride=4 * 32 * 128)
+    wide = dict(k_pages=k, v_pages=k + 128, token_stride=256, head_stride=32 * 256, page_stride=4 * 32 * 256 + 64)
+    for pages, bad in ((rows, (k, v, k + 77, v + 10 * 16384 - 1, k - 79)), (wide, (k, k + 4 * 32 * 256 - 1, k + 200))):
+        for at in bad:
+            for scales in (dict(k_block_scale=at, v_block_scale=far), dict(k_block_scale=far, v_block_scale=at)):
+                c = ctypes.byref(_block_cache(**pages, **scales))
+                _refused(lib.mala_paged_write(1 << 20, 1 << 22, 512, 128, 16, c, 4, None), BAD)
+                assert b"block scales share memory with the pages" in lib.mala_last_error()
+                _refused(lib.mala_paged_rope_write(None, 1 << 20, 1 << 22, 512, 128, 16, _turn(), c, 4, None), BAD)
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("P", [16, 32])
+def test_block_scales_between_and_behind_pages_are_taken(P):
+    # pages and scales in one allocation: the scales behind the last page, and in a gap behind each
+    # head's rows that nothing else uses
+    import block_util as bu
+    N, Hkv, D, T = 6, 2, 64, 40
+    n = N * Hkv * (P // 16)
+    x = torch.randn((2, Hkv, T, D), device="cuda").bfloat16()
+    slots = torch.arange(T, dtype=torch.int32, device="cuda")
+    want = bu.block_cache(mala, N, Hkv, P, D)
+    mala.mala_paged_write(x[0], x[1], slots, want[0])
+    for gap in (0, 64):                  # (bytes behind a head's rows)
+        head = P * D + gap
+        one = torch.zeros(2 * N * Hkv * head + 2 * n, dtype=torch.uint8, device="cuda")
+        k, v = (one[i * N * Hkv * head:(i + 1) * N * Hkv * head].view(N, Hkv, head)[..., :P * D]
+                .view(N, Hkv, P, D).view(torch.float8_e4m3fn) for i in range(2))
+        at = [2 * N * Hkv * head, 2 * N * Hkv * head + n] if not gap else [P * D, head + P * D]
+        ks, vs = (one[a:a + n].view(N, Hkv, P // 16).view(torch.float8_e8m0fnu) for a in at)
+        mala.mala_paged_write(x[0], x[1], slots, mala.PagedCache(k, v, ks, vs))
+        for a, b in zip((k, v, ks, vs), want[1:]):
+            assert torch.equal(a.view(torch.uint8), b.view(torch.uint8))
+        if gap:
+            bad = one[P * D - 1:P * D - 1 + n].view(N, Hkv, P // 16).view(torch.float8_e8m0fnu)
+            with pytest.raises(mala.MalaError, match="share memory with the pages"):
+                mala.mala_paged_write(x[0], x[1], slots, mala.PagedCache(k, v, vs, bad))
+
+
 @pytest.mark.gpu
 def test_outputs_side_by_side_are_taken():
     # queries and keys into slices of one tensor, of heads in turns, and of batches inside tokens
