@@ -586,7 +586,10 @@ def _rope_rows(x, out, name, shape, t_in, t_out, device):
         (xb, xh, xt, xd), (ob, oh, ot, od) = x.stride(), out.stride()
     if (xd != 1 or od != 1) and x.numel():
         raise ValueError("the rows of %s and %s_out must be contiguous" % (name, name))
-    return _ROPE_ROWS.pack(x.data_ptr(), out.data_ptr(), xb, xh, xt, ob, oh, ot, shape[-3])
+    heads = shape[-3]
+    if heads > 0x7fffffff:
+        raise ValueError("the heads of %s (%d) do not fit 32 bits" % (name, heads))
+    return _ROPE_ROWS.pack(x.data_ptr(), out.data_ptr(), xb, xh, xt, ob, oh, ot, heads)
 
 
 def _rope_turn(positions, inv_freq, layout, scale, B, T, device):
@@ -605,7 +608,17 @@ def _rope_turn(positions, inv_freq, layout, scale, B, T, device):
                 and positions.is_contiguous()):
             _args(device, (positions, "positions", torch.int32, shape))
         at = positions.data_ptr()
-    return _ROPE.pack(at, stride, inv_freq.data_ptr(), 2 * inv_freq.numel(), layout, scale)
+    try:
+        return _ROPE.pack(at, stride, inv_freq.data_ptr(), 2 * inv_freq.numel(), layout, scale)
+    except (struct.error, OverflowError):
+        pass
+    if not hasattr(layout, "__index__"):
+        raise TypeError("layout must be ROPE_HALF or ROPE_INTERLEAVED, got %r" % (layout,))
+    if not hasattr(scale, "__float__") and not hasattr(scale, "__index__"):
+        raise TypeError("scale must be a number, got %r" % (scale,))
+    _int32(layout, "layout")
+    _int32(2 * inv_freq.numel(), "rotary_dim")
+    raise ValueError("scale (%s) does not fit 32 bits" % (scale,))
 
 
 def mala_rope(q, k, q_out, k_out, positions, inv_freq, layout=ROPE_HALF, scale=1.0, inverse=False,
