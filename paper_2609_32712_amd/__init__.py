@@ -529,12 +529,14 @@ def mala_paged_update(lens, new_lens, block_table, free_ring, free_state, lens_o
             new_lens.data_ptr(), block_table.data_ptr(), free_ring.data_ptr(),
             free_state.data_ptr(), lens_out.data_ptr(), cu_seqlens.data_ptr(), slots.data_ptr(),
             _addr(positions), free_state_out.data_ptr(), R, W, _int32(page_size, "page_size"),
-            _int32(num_pages, "num_pages"), C, T)
+            _int32(num_pages, "num_pages"), _int32(C, "ring_size"), _int32(T, "max_tokens"))
 
 
 def _new_rows(k_new, v_new, slots, c):
     """The checks of the rows that a write takes; (T, token stride, head stride)."""
     Hkv, T, D = shape = _shape(k_new, "k_new", 3)
+    if T > 0x7fffffff:
+        raise ValueError("the tokens of k_new (%d) do not fit 32 bits" % T)
     if not isinstance(v_new, torch.Tensor) or v_new.dim() != 3:
         _dims(v_new, "v_new", 3)
     if k_new.dtype is not torch.bfloat16 or v_new.dtype is not torch.bfloat16:

@@ -43,3 +43,25 @@ def test_calls(err, kw):
     many = torch.ones((1, 1, 64), dtype=torch.bfloat16, device="cuda").expand(1 << 31, 1, 64)
     with pytest.raises(ValueError, match="32 bits"):
         mala.mala_rope(many, None, many, None, None, f)
+
+
+@pytest.mark.gpu
+def test_more_tokens_than_32_bits_hold_are_refused():
+    # (the low 32 bits of their number were passed on: 2^32 + 3 tokens wrote three)
+    import block_util as bu
+    T = (1 << 32) + 3
+    if torch.cuda.mem_get_info()[0] < 5 * T:
+        pytest.skip("needs 20 GB of GPU memory")
+    f, _ = mala.rope_frequencies(64, device="cuda")
+    cache, k, v, ks, vs = bu.block_cache(mala, 2, 1, 16, 64)
+    x = torch.ones((1, 1, 64), dtype=torch.bfloat16, device="cuda").expand(1, T, 64)
+    slots = torch.empty(T, dtype=torch.int32, device="cuda")
+    slots[:3] = torch.arange(3)
+    with pytest.raises(ValueError, match="32 bits"):
+        mala.mala_paged_write(x, x, slots, cache)
+    with pytest.raises(ValueError, match="32 bits"):
+        mala.mala_paged_rope_write(None, None, x, x, None, slots, cache, f)
+    one = lambda n: torch.zeros(n, dtype=torch.int32, device="cuda")
+    with pytest.raises(ValueError, match="32 bits"):
+        mala.mala_paged_update(one(1), one(1), one((1, 4)), one(4), one(2), one(1), one(2), slots, slots, one(4), 16, 4)
+    assert not k.view(torch.uint8).any() and not ks.view(torch.uint8).any()
