@@ -456,8 +456,9 @@ int mala_paged_update(const int32_t* lens, const int32_t* new_lens, int32_t* blo
  *   new scale.  Values are rounded to nearest even; infinities become the largest value (448 x 2^e; 240
  *   x 2^120), NaN stays NaN.  Neither the pages nor the scales need a value before a block's row 0 has
  *   been written; after that its other rows mean nothing until they are.  The tokens of one block in
- *   a call (slots of it) lie within 64 consecutive tokens; two calls that run at the same time write
- *   to different blocks.
+ *   a call (slots of it) lie within 64 consecutive tokens, as mala_paged_update packs them; two calls
+ *   that run at the same time write to different blocks.  A block of which this is not so holds no
+ *   defined rows and scale afterwards; others are not touched.
  */
 int mala_paged_write(const void* k_new, const void* v_new, int64_t new_token_stride,
                      int64_t new_head_stride, const int32_t* slots,

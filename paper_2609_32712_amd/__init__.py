@@ -564,7 +564,8 @@ def mala_paged_write(k_new, v_new, slots, cache, stream=None):
     transposed slices of a [T, 2, Hkv, D] projection); slots: int32 [T].
 
     Of a cache with scales of blocks, the tokens of one block have to lie within 64 consecutive
-    tokens (as paged_update packs them); the block's scale is found or raised as they come."""
+    tokens (as paged_update packs them; a block whose tokens lie farther apart holds no defined rows
+    afterwards); the block's scale is found or raised as they come."""
     c = _cache(cache)
     T, token_stride, head_stride = _new_rows(k_new, v_new, slots, c)
     _launch(c.device, stream, (_lib or load_library()).mala_paged_write, k_new.data_ptr(),
@@ -817,7 +818,9 @@ def rope_frequencies(rotary_dim, base=10000.0, factor=1.0, scaling="none", origi
     factor^(rotary_dim / (rotary_dim - 2)), which leaves the fastest as it is and takes the slowest
     to 1 / factor.  "yarn": by parts, after the turns that a frequency makes over original_len
     tokens: from beta_fast turns on as they are, up to beta_slow over factor, linear in the turns
-    between; scale 0.1 ln(factor) + 1."""
+    between; scale 0.1 ln(factor) + 1.  This is the ramp of the method's formula.  Code that goes by a
+    pair's number between two (rounded) ends instead gives other frequencies between them: a model
+    that was trained with that needs those as its inv_freq."""
     if rotary_dim <= 0 or rotary_dim % 2:
         raise ValueError("rotary_dim (%s) must be positive and even" % rotary_dim)
     if not (base > 0 and math.isfinite(base)) or not (factor > 0 and math.isfinite(factor)):

@@ -412,7 +412,7 @@ __global__ __launch_bounds__(256) void mala_paged_block_write_kernel(PagedWriteP
 template <int D, bool INTER>
 __device__ __forceinline__ void turn_queries(const PagedRopeWriteParams& p) {
   const unsigned nx = (p.q.T + rope_tokens(D) - 1) / rope_tokens(D), i = blockIdx.x - p.kv_groups;
-    turn_rows<D, false, false, INTER, false, 2>(p.q, i % nx * rope_tokens(D), (int)(i / nx) * p.q.per);
+  turn_rows<D, false, false, INTER, false, 2>(p.q, i % nx * rope_tokens(D), (int)(i / nx) * p.q.per);
 }
 
 template <int D, bool INTER>
@@ -425,7 +425,9 @@ __global__ __launch_bounds__(256) void mala_paged_block_rope_kernel(PagedRopeWri
   }
 }
 
-// The same for a cache of bf16, or of e4m3 with a scale per head: every row is its own.
+// The same for a cache of bf16, or of e4m3 with a scale per head: every row is its own.  HBM-bound: 16000
+// tokens, 32 + 8 heads, bf16 75 us, 5.3 TB/s, e4m3 79, 4.6 (a division per value, 8 bytes to a store);
+// 64 tokens 3.3 and 3.9.
 template <int D, bool E4M3, bool INTER>
 __global__ __launch_bounds__(256) void mala_paged_rope_write_kernel(PagedRopeWriteParams p) {
   constexpr int LPR = D / 16, TOK = rope_tokens(D);

@@ -49,7 +49,8 @@ struct PagedRopeWriteParams {
 // whole number counts: as fp32 it would lose log2(pos) bits.  Both products are taken to twice 53
 // bits (a product and its exact remainder), so that what is left of a quarter turn is right to
 // 2^-53 of the quarter turn at any position, and then rounded to fp32 once.  sin and cos of up to
-// pi / 4 are their Taylor sums (the terms left out are below 2^-32).
+// pi / 4 are their Taylor sums: the first terms left out are x^11 / 11! (2^-29 at pi / 4, a 32nd of half a
+// step of 1) and x^12 / 12! (2^-33); with all roundings the sums are within 0.9 x 2^-24 of sin and cos.
 __device__ __forceinline__ void turn_of(int pos, double inv_freq, float scale, float sin_scale,
                                         float& c, float& s) {
 #pragma clang fp contract(off)

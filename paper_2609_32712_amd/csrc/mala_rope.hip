@@ -12,7 +12,7 @@ namespace {
 
 template <int D, bool IN32, bool OUT32, bool INTER, bool ONCE>
 __global__ __launch_bounds__(256) void mala_rope_kernel(RopeParams p) {
-    // consecutive workgroups: the tokens of some heads, or (heads_first) the heads of some tokens
+  // consecutive workgroups: the tokens of some heads, or (heads_first) the heads of some tokens
   const unsigned slices = gridDim.y, i = blockIdx.x + blockIdx.y * gridDim.x;
   if (p.heads_first)
     turn_rows<D, IN32, OUT32, INTER, ONCE, 1>(p, i / slices * rope_tokens(D), i % slices * p.per);
