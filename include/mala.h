@@ -69,7 +69,9 @@ typedef enum {
                                 forward/backward K/V slice of 2^32 bytes or more, a page
                                 size that is not a multiple of 16, or a pool, table or
                                 grid of 2^31 tokens, entries or workgroups or more, a
-                                rotary_dim that is not a multiple of 16 */
+                                rotary_dim that is not a multiple of 16, outputs of strides
+                                that take too long to be told apart (none of a tensor's
+                                or its slices') */
   MALA_ERR_WORKSPACE = -3,   /* workspace NULL or smaller than the *_workspace_size query */
   MALA_ERR_HIP = -4          /* a HIP launch/runtime call failed; see mala_last_error() */
 } mala_status;

@@ -110,6 +110,33 @@ def test_rows_of_two_tensors(tmp_path):
     assert _ask(tmp_path, [q + k, k + q, q + far, far + q, batches[0] + batches[1]], "two") == [0, 0, 1, 1, 0]
 
 
+@needs_cxx
+def test_large_tensors_and_their_slices_are_told_apart(tmp_path):
+    # axes of any size in any order, padded or not; two slices of the heads, and of every other head
+    rng = random.Random(3)
+    own, pairs, want = [], [], []
+    for _ in range(3000):
+        w = rng.choice([128, 256, 512])
+        heads = rng.randint(2, 300)
+        n = {"b": int(2 ** rng.uniform(0, 12)), "h": heads, "t": int(2 ** rng.uniform(0, 21))}
+        step, stride = w, {}
+        for axis in rng.sample("bht", 3):
+            stride[axis] = step + 16 * rng.choice([0, 0, 0, 1, 7, 64])
+            step = stride[axis] * n[axis]
+        rows = lambda first, count, every=1: [(1 << 20) + first * stride["h"], w, stride["b"], every * stride["h"],
+                                              stride["t"], n["b"], count, n["t"]]
+        own.append(rows(0, heads))
+        cut = rng.randint(1, heads - 1)
+        pairs.append(rows(0, cut) + rows(cut, heads - cut))
+        want.append(0)
+        pairs.append(rows(0, -(-heads // 2), 2) + rows(1, heads // 2, 2))
+        want.append(0)
+        pairs.append(rows(0, cut + 1) + rows(cut, heads - cut))
+        want.append(1)
+    assert not any(_ask(tmp_path, own))
+    assert _ask(tmp_path, pairs, "two") == want
+
+
 def test_outputs_that_share_rows_are_refused():
     # (rows of 256 bytes, 2 x 4 x 4 of them, 8 KB to a batch; in is 1 << 20, out 1 << 30)
     at = 1 << 21
